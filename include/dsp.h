@@ -23,7 +23,7 @@
  *     average pool (N x C) and the loss are always float.
  *   - Parameters cross the boundary on the HOST as float in "layer order": for each layer in
  *     turn, conv: w[cout][cin][r][s]; bn: gamma[c], beta[c]; linear: W[cout][cin], c[cout].
- *   - The library allocates device memory only in the *_init calls and in
+ *   - The library allocates device memory only in the *_init calls, in dsp_block_set_adamw and in
  *     dsp_pipeline_attach_gradient_probe / dsp_pipeline_set_forward_streams (first step after it);
  *     the step calls launch kernels asynchronously on the given stream and allocate nothing.
  *   - Arguments are checked before anything is launched: DSP_EINVAL and DSP_ESTATE leave the
@@ -101,6 +101,7 @@ typedef struct dsp_block_desc {
 
 typedef struct dsp_block dsp_block;
 typedef struct dsp_pipeline dsp_pipeline;
+typedef struct dsp_adamw dsp_adamw;
 
 /* ---- schedule (host only; Section 3.3 and Appendix A) ------------------------------------ */
 
@@ -240,6 +241,72 @@ int dsp_block_get_momentum(dsp_block* b, float* h_dst, size_t n);
 int dsp_block_set_momentum(dsp_block* b, const float* h_src, size_t n);
 int dsp_block_get_grads(dsp_block* b, float* h_dst, size_t n);
 
+/* ---- AdamW over many tensors at once (an update beside Eq. (3)) --------------------------- */
+
+/*
+ * One tensor of an AdamW update.  All buffers are the caller's, in device memory, aligned to their elements and no more,
+ * and stay in place while the object lives; those that are written may overlap no other buffer of the object.
+ */
+typedef struct dsp_adamw_tensor {
+    float* d_param;      /* n parameters, updated in place */
+    const void* d_grad;  /* n gradients of type grad_dtype, read by every step */
+    void* d_copy;        /* n bfloat16 that receive the new parameters, rounded; or NULL */
+    void* d_m;           /* first moment: n floats, or n bytes (e4m3) with states of 8 bits */
+    void* d_v;           /* second moment: n floats, or n bytes (e5m2) */
+    uint8_t* d_m_exp;    /* states of 8 bits: ceil(n / 256) bytes each; ignored with 32 bits */
+    uint8_t* d_v_exp;
+    int64_t n;           /* elements; a tensor of none is passed over */
+    int32_t grad_dtype;  /* dsp_dtype */
+    int32_t decay;       /* != 0: weight decay applies to it (matrices; not gains, biases) */
+} dsp_adamw_tensor;
+
+/*
+ * Builds the update of n_tensors tensors (the array is not kept).  A new optimizer starts from states of zero bytes and step 0.
+ *
+ * state_bits = 8: element i of a moment stands for its 8-bit float (OCP e4m3 for m, e5m2 for v) times 2^(exp[i / 256] - 127).
+ * The step forms the new moments in 32 bits, updates the parameters with them and stores them rounded STOCHASTICALLY: up with
+ * the probability of what lies above the value below, from 16 random bits that are a function of seed, step number, place of
+ * the tensor in the array and element alone.  (To nearest, v would stand still: one step moves it by 1 - beta2, far less than
+ * half a step of any 8-bit float.)  A v > 0 is never stored as 0.  A value that is no finite number is stored as the format's
+ * NaN and leaves the other 255 of its block alone.
+ */
+int dsp_adamw_init(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t state_bits, uint64_t seed, dsp_adamw** out);
+int dsp_adamw_destroy(dsp_adamw* o);
+
+/*
+ * One step on all tensors, with t = number of this step (from 1 on), c = 1 or, for max_norm > 0, min(1, max_norm / norm) with
+ * norm the root of the sum of squares of all gradients, and g = c * gradient:
+ *     m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *     x <- x - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay x)    (the last term where decay != 0)
+ * (beta^t: the product over the steps taken, should beta change.)  d_norm, unless NULL, receives the norm, also without a clip.
+ * With max_norm > 0 a step whose norm is no finite number changes nothing but d_norm and is not counted.
+ * Wants lr, weight_decay, max_norm >= 0, 0 <= beta < 1, eps > 0 and the object's device to be the current one.  Launches one
+ * kernel, or two with the norm; the step number is kept on the device, so that a captured step counts on in every replay (its
+ * hyperparameters stay those of the capture).  Steps of one object must be ordered by the caller, on whatever streams.
+ */
+int dsp_adamw_step(dsp_adamw* o, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm,
+                   float* d_norm, void* stream);
+/* Steps taken so far, and setting it when training is resumed (beta^steps then counts as their product).  Both synchronise
+ * the device. */
+int dsp_adamw_get_steps(dsp_adamw* o, int64_t* steps);
+int dsp_adamw_set_steps(dsp_adamw* o, int64_t steps, double beta1, double beta2);
+
+/*
+ * The same as a block's update.  dsp_block_set_adamw allocates the moments (zero, of 32 or 8 bits) of block b's parameters; weight
+ * decay applies to conv and linear weights.  dsp_param_update_adamw consumes the pending G_{x_k} exactly as
+ * dsp_param_update_sum does (DSP_ESTATE if there is none, or without dsp_block_set_adamw); max_norm bounds the norm of this
+ * block's gradient (the blocks of a pipeline do not wait for each other, so there is no norm over all of them).  A block
+ * may change between the two updates; each keeps its own state.  A second dsp_block_set_adamw: DSP_ESTATE.
+ */
+int dsp_block_set_adamw(dsp_block* b, int32_t state_bits, uint64_t seed);
+int dsp_param_update_adamw(dsp_block* b, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm,
+                           void* stream);
+/* The moments and the step number as they lie, for a checkpoint (host memory; they synchronise the device first); only for a
+ * block of the same layers, dtype and state_bits. */
+int dsp_block_adamw_state_bytes(const dsp_block* b, size_t* bytes);
+int dsp_block_get_adamw_state(dsp_block* b, void* h_dst, size_t bytes);
+int dsp_block_set_adamw_state(dsp_block* b, const void* h_src, size_t bytes);
+
 /* ---- K blocks on K HIP streams of one GPU (Section 3.3) ---------------------------------- */
 
 /*
@@ -278,6 +345,12 @@ int dsp_pipeline_step(dsp_pipeline* pl, const void* d_batch, const int32_t* d_la
  * later ticks (a step learning-rate schedule calls this between steps; dsp_pipeline_init sets s = 0).
  */
 int dsp_pipeline_set_optimizer(dsp_pipeline* pl, float lr, float momentum, int32_t s, float weight_decay);
+/*
+ * The updates of all later ticks are dsp_param_update_adamw's with these arguments (every block must have had
+ * dsp_block_set_adamw: DSP_ESTATE otherwise); dsp_pipeline_set_optimizer goes back to Eq. (3).  A pipeline with a gradient
+ * probe attached may use it; the probe pipeline itself may not (its step size is 0).
+ */
+int dsp_pipeline_set_adamw(dsp_pipeline* pl, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm);
 
 /*
  * Gradient-difference diagnostic (Lemma 1; the quantity plotted in Section 5.4).  `probe` is a second
@@ -472,6 +545,57 @@ int dsp_linear_backward(const float* d_x, const float* d_w, const float* d_dz, f
 /* L(h_K, l) of Eq. (1): *d_loss = mean_n -log softmax(z_n)[label_n], d_dz = dL/dz; d_row_loss: N floats of scratch. */
 int dsp_softmax_ce(const float* d_z, const int32_t* d_labels, float* d_loss, float* d_dz, float* d_row_loss, int32_t N,
                    int32_t C, void* stream);
+
+/*
+ * What joins two residual blocks: the norm behind a block's branch, its gate, the residual sum and the norm in front of the next
+ * block, over M rows of C elements (C <= 16384) in `dtype`, in one pass:
+ *     n = N_post(z),   y = alpha x + beta act(gate) n,   h = N_pre(y)
+ *     N(u) = (u - mean) / sqrt(mean((u - mean)^2) + eps) * gain + bias,  mean = 0 for DSP_NORM_RMS,  N(u) = u for DSP_NORM_NONE
+ * x: the residual stream, z: the branch's output, y: the new residual stream, h: what the next branch reads (not formed with
+ * pre = DSP_NORM_NONE).  Row r takes row r / gate_rows of the gate: gate_rows >= M is one vector (a learned scale), gate_rows =
+ * positions of a sequence one row each (conditioning), gate_rows = 1 a gate of every element; gate_rows = 0: no gate.  Everything
+ * is computed in float; h is normed before y is rounded to its type.
+ * d_z = NULL is the first norm of a stack, h = N_pre(x): post = NONE, no gate, alpha = 1, d_y = NULL (the backward pass takes x
+ * in the place of y).
+ * Strides are the elements from one row to the next (0: C); a gradient has the stride of its tensor (dx: x, dz: z, dy: y,
+ * dh: h, dgate: gate).  Buffers are aligned to their elements and no more.
+ */
+typedef enum dsp_norm_kind { DSP_NORM_NONE = 0, DSP_NORM_RMS = 1, DSP_NORM_LAYER = 2 } dsp_norm_kind;
+typedef enum dsp_gate_kind { DSP_GATE_IDENTITY = 0, DSP_GATE_SIGMOID = 1, DSP_GATE_TANH = 2 } dsp_gate_kind;
+typedef struct dsp_norm_residual_desc {
+    int64_t M;
+    int32_t C;
+    int32_t dtype;      /* dsp_dtype of x, z, y, h and their gradients */
+    int32_t post, pre;  /* dsp_norm_kind */
+    int32_t gate_act;   /* dsp_gate_kind */
+    int32_t gate_dtype; /* type of the gate and its gradient: DSP_FP32, or dtype */
+    int64_t gate_rows;
+    float alpha, beta, eps;
+    int64_t x_stride, z_stride, y_stride, h_stride, gate_stride;
+} dsp_norm_residual_desc;
+
+/*
+ * Gains and biases: C floats each, NULL = 1 and 0 (those of a norm that is NONE are ignored).  d_post_stats, d_pre_stats: 2 * M
+ * floats each, the rows' means (0 for RMS) and behind them 1 / sqrt(var + eps), for the backward pass; NULL: not kept.
+ * d_y may be d_x (with the same stride).
+ */
+int dsp_norm_residual_forward(const dsp_norm_residual_desc* desc, const void* d_x, const void* d_z, const void* d_gate,
+                              const float* d_post_gain, const float* d_post_bias, const float* d_pre_gain, const float* d_pre_bias,
+                              void* d_y, void* d_h, float* d_post_stats, float* d_pre_stats, void* stream);
+/*
+ * Given dh and dy (NULL: y is read by the norm alone), with D = dy + N_pre'(dh): dx = alpha D, dz = N_post'(beta act(gate) D),
+ * dgate = sum beta act'(gate) n D over the rows of each row of the gate, and the gradients of gains and biases; of these outputs
+ * NULL ones are not formed.  d_y: y as the forward pass left it; d_z is needed for dgate and with a norm behind the branch.
+ * d_dx may be d_dy, d_dz may be d_z (same strides).  d_workspace: dsp_norm_residual_workspace_bytes() bytes (whatever is asked
+ * for: that many are enough), 16-byte aligned, contents unspecified before and after; NULL and 0 if no gradient of a
+ * parameter is asked for.  Sums are taken in a fixed order: the same call gives the same bits.
+ */
+int dsp_norm_residual_workspace_bytes(const dsp_norm_residual_desc* desc, size_t* bytes);
+int dsp_norm_residual_backward(const dsp_norm_residual_desc* desc, const void* d_dh, const void* d_dy, const void* d_y,
+                               const void* d_z, const void* d_gate, const float* d_post_gain, const float* d_post_bias,
+                               const float* d_pre_gain, const float* d_post_stats, const float* d_pre_stats, void* d_dx, void* d_dz,
+                               void* d_dgate, float* d_dpost_gain, float* d_dpost_bias, float* d_dpre_gain, float* d_dpre_bias,
+                               void* d_workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Test support: copies what layer `layer` of the block left in the buffers the backward sweep reads (the

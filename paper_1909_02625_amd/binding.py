@@ -13,6 +13,12 @@ import numpy as np
 __all__ = [
     "DSP_FP32", "DSP_BF16", "DSPError", "lib", "lib_path", "check",
     "dsp_layer_desc", "dsp_block_desc", "make_block_desc",
+    "DSP_NORM_NONE", "DSP_NORM_RMS", "DSP_NORM_LAYER", "DSP_GATE_IDENTITY", "DSP_GATE_SIGMOID", "DSP_GATE_TANH",
+    "dsp_adamw_tensor", "dsp_adamw_init", "dsp_adamw_destroy", "dsp_adamw_step", "dsp_adamw_get_steps", "dsp_adamw_set_steps",
+    "dsp_block_set_adamw", "dsp_param_update_adamw", "dsp_block_adamw_state_bytes", "dsp_block_get_adamw_state",
+    "dsp_block_set_adamw_state", "dsp_pipeline_set_adamw",
+    "dsp_norm_residual_desc", "make_norm_residual_desc", "dsp_norm_residual_forward", "dsp_norm_residual_workspace_bytes",
+    "dsp_norm_residual_backward",
     "dsp_schedule_validate", "dsp_schedule_index", "dsp_schedule_queue_elems", "dsp_schedule_waits",
     "dsp_block_init", "dsp_block_destroy", "dsp_block_forward", "dsp_block_recompute_backward",
     "dsp_param_update", "dsp_param_update_sum", "dsp_pipeline_set_optimizer", "dsp_block_input_slot",
@@ -36,6 +42,8 @@ __all__ = [
 ]
 
 DSP_FP32, DSP_BF16 = 0, 1
+DSP_NORM_NONE, DSP_NORM_RMS, DSP_NORM_LAYER = 0, 1, 2
+DSP_GATE_IDENTITY, DSP_GATE_SIGMOID, DSP_GATE_TANH = 0, 1, 2
 _OPS = {"conv": 0, "bn": 1, "maxpool": 2, "gap": 3, "linear": 4, "softmax_ce": 5, "add": 6}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -58,6 +66,17 @@ class dsp_block_desc(C.Structure):
                 ("N", C.c_int32), ("C", C.c_int32), ("H", C.c_int32), ("W", C.c_int32),
                 ("dtype", C.c_int32), ("k", C.c_int32), ("K", C.c_int32), ("m_k", C.c_int32),
                 ("p_prev", C.c_int32), ("needs_input_grad", C.c_int32), ("bn_eps", C.c_float)]
+
+
+class dsp_adamw_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_param", "d_grad", "d_copy", "d_m", "d_v", "d_m_exp", "d_v_exp")] + \
+               [("n", C.c_int64), ("grad_dtype", C.c_int32), ("decay", C.c_int32)]
+
+
+class dsp_norm_residual_desc(C.Structure):
+    _fields_ = [("M", C.c_int64)] + [(n, C.c_int32) for n in ("C", "dtype", "post", "pre", "gate_act", "gate_dtype")] + \
+               [("gate_rows", C.c_int64)] + [(n, C.c_float) for n in ("alpha", "beta", "eps")] + \
+               [(n, C.c_int64) for n in ("x_stride", "z_stride", "y_stride", "h_stride", "gate_stride")]
 
 
 def lib_path():
@@ -155,6 +174,20 @@ _SIGNATURES = {
     "dsp_linear_forward": [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp],
     "dsp_linear_backward": [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp],
     "dsp_softmax_ce": [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp],
+    "dsp_adamw_init": [_i32, C.POINTER(dsp_adamw_tensor), _i32, C.c_uint64, C.POINTER(_vp)],
+    "dsp_adamw_destroy": [_vp],
+    "dsp_adamw_step": [_vp] + [C.c_double] * 6 + [_vp, _vp],
+    "dsp_adamw_get_steps": [_vp, _pi64],
+    "dsp_adamw_set_steps": [_vp, _i64, C.c_double, C.c_double],
+    "dsp_block_set_adamw": [_vp, _i32, C.c_uint64],
+    "dsp_param_update_adamw": [_vp] + [C.c_double] * 6 + [_vp],
+    "dsp_block_adamw_state_bytes": [_vp, C.POINTER(_sz)],
+    "dsp_block_get_adamw_state": [_vp, _vp, _sz],
+    "dsp_block_set_adamw_state": [_vp, _vp, _sz],
+    "dsp_pipeline_set_adamw": [_vp] + [C.c_double] * 6,
+    "dsp_norm_residual_forward": [C.POINTER(dsp_norm_residual_desc)] + [_vp] * 12,
+    "dsp_norm_residual_workspace_bytes": [C.POINTER(dsp_norm_residual_desc), C.POINTER(_sz)],
+    "dsp_norm_residual_backward": [C.POINTER(dsp_norm_residual_desc)] + [_vp] * 18 + [_sz, _vp],
     "dsp_block_get_activation": [_vp, _i32, _vp, _sz],
     "dsp_block_get_pool_argmax": [_vp, _i32, _vp, _sz],
     "dsp_conv_backward_weight_static_bytes": [C.POINTER(_sz)],
@@ -304,6 +337,77 @@ def dsp_pipeline_gradient_difference(pl, K):
     diff, ref = (C.c_double * K)(), (C.c_double * K)()
     check(lib().dsp_pipeline_gradient_difference(pl, C.byref(bid), diff, ref), "dsp_pipeline_gradient_difference")
     return bid.value, np.array(diff[:], np.float64), np.array(ref[:], np.float64)
+
+
+# ---- AdamW ---------------------------------------------------------------------------------------------
+def dsp_adamw_init(tensors, state_bits=32, seed=0):
+    """``tensors``: dicts of contiguous device tensors param, grad, m, v and, as they apply, copy, m_exp, v_exp; decay (default True).
+    They have to outlive the object."""
+    import torch
+    arr = (dsp_adamw_tensor * max(1, len(tensors)))()
+    state = 1 if state_bits == 8 else 4
+    for a, t in zip(arr, tensors):
+        n = t["param"].numel()
+        sizes = {"param": (4, n), "grad": (2 if t["grad"].dtype == torch.bfloat16 else 4, n), "copy": (2, n), "m": (state, n), "v": (state, n)}
+        for name in ("param", "grad", "copy", "m", "v", "m_exp", "v_exp"):
+            x = t.get(name)
+            size, count = sizes.get(name, (1, -(-n // 256)))
+            if x is not None and (x.element_size() != size or x.numel() != count or not x.is_contiguous()):
+                raise ValueError("dsp_adamw_init: %s: %d contiguous elements of %d bytes are wanted" % (name, count, size))
+            setattr(a, "d_" + name, _ptr(x))
+        a.n, a.decay = n, int(bool(t.get("decay", True)))
+        a.grad_dtype = DSP_BF16 if t["grad"].dtype == torch.bfloat16 else DSP_FP32
+    out = C.c_void_p()
+    check(lib().dsp_adamw_init(len(tensors), arr, state_bits, seed, C.byref(out)), "dsp_adamw_init")
+    return out.value
+
+
+def dsp_adamw_destroy(o):
+    check(lib().dsp_adamw_destroy(o), "dsp_adamw_destroy")
+
+
+def dsp_adamw_step(o, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, max_norm=0.0, d_norm=None, stream=None):
+    check(lib().dsp_adamw_step(o, lr, beta1, beta2, eps, weight_decay, max_norm, _ptr(d_norm), _stream(stream)), "dsp_adamw_step")
+
+
+def dsp_adamw_get_steps(o):
+    out = C.c_int64()
+    check(lib().dsp_adamw_get_steps(o, C.byref(out)), "dsp_adamw_get_steps")
+    return out.value
+
+
+def dsp_adamw_set_steps(o, steps, beta1=0.9, beta2=0.999):
+    check(lib().dsp_adamw_set_steps(o, steps, beta1, beta2), "dsp_adamw_set_steps")
+
+
+def dsp_block_set_adamw(b, state_bits=32, seed=0):
+    check(lib().dsp_block_set_adamw(b, state_bits, seed), "dsp_block_set_adamw")
+
+
+def dsp_param_update_adamw(b, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, max_norm=0.0, stream=None):
+    check(lib().dsp_param_update_adamw(b, lr, beta1, beta2, eps, weight_decay, max_norm, _stream(stream)), "dsp_param_update_adamw")
+
+
+def dsp_block_adamw_state_bytes(b):
+    out = C.c_size_t()
+    check(lib().dsp_block_adamw_state_bytes(b, C.byref(out)), "dsp_block_adamw_state_bytes")
+    return out.value
+
+
+def dsp_block_get_adamw_state(b):
+    """Moments and step number as they lie (numpy uint8)."""
+    out = np.empty(dsp_block_adamw_state_bytes(b), np.uint8)
+    check(lib().dsp_block_get_adamw_state(b, out.ctypes.data, out.size), "dsp_block_get_adamw_state")
+    return out
+
+
+def dsp_block_set_adamw_state(b, h_src):
+    src = np.ascontiguousarray(h_src, np.uint8)
+    check(lib().dsp_block_set_adamw_state(b, src.ctypes.data, src.size), "dsp_block_set_adamw_state")
+
+
+def dsp_pipeline_set_adamw(pl, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, max_norm=0.0):
+    check(lib().dsp_pipeline_set_adamw(pl, lr, beta1, beta2, eps, weight_decay, max_norm), "dsp_pipeline_set_adamw")
 
 
 def dsp_block_input_slot(b, batch_id):
@@ -601,6 +705,36 @@ def dsp_linear_backward(d_x, d_w, d_dz, d_dx, d_dw, d_dbias, N, cin, cout, strea
 def dsp_softmax_ce(d_z, d_labels, d_loss, d_dz, d_row_loss, N, C_, stream=None):
     check(lib().dsp_softmax_ce(_ptr(d_z), _ptr(d_labels), _ptr(d_loss), _ptr(d_dz), _ptr(d_row_loss), N, C_, _stream(stream)),
           "dsp_softmax_ce")
+
+
+# ---- norms, gate and residual sum between two blocks --------------------------------------------------
+def make_norm_residual_desc(M, C_, dtype, post=0, pre=0, alpha=1.0, beta=1.0, eps=1e-5, gate_rows=0, gate_act=0, gate_dtype=None,
+                            x_stride=0, z_stride=0, y_stride=0, h_stride=0, gate_stride=0):
+    return dsp_norm_residual_desc(M, C_, dtype, post, pre, gate_act, dtype if gate_dtype is None else gate_dtype, gate_rows, alpha,
+                                  beta, eps, x_stride, z_stride, y_stride, h_stride, gate_stride)
+
+
+def dsp_norm_residual_forward(desc, d_x, d_z=None, d_gate=None, d_post_gain=None, d_post_bias=None, d_pre_gain=None, d_pre_bias=None,
+                              d_y=None, d_h=None, d_post_stats=None, d_pre_stats=None, stream=None):
+    check(lib().dsp_norm_residual_forward(C.byref(desc), _ptr(d_x), _ptr(d_z), _ptr(d_gate), _ptr(d_post_gain), _ptr(d_post_bias),
+                                          _ptr(d_pre_gain), _ptr(d_pre_bias), _ptr(d_y), _ptr(d_h), _ptr(d_post_stats),
+                                          _ptr(d_pre_stats), _stream(stream)), "dsp_norm_residual_forward")
+
+
+def dsp_norm_residual_workspace_bytes(desc):
+    out = C.c_size_t()
+    check(lib().dsp_norm_residual_workspace_bytes(C.byref(desc), C.byref(out)), "dsp_norm_residual_workspace_bytes")
+    return out.value
+
+
+def dsp_norm_residual_backward(desc, d_dh, d_dy, d_y, d_z, d_gate, d_post_gain, d_post_bias, d_pre_gain, d_post_stats, d_pre_stats, d_dx,
+                               d_dz, d_dgate=None, d_dpost_gain=None, d_dpost_bias=None, d_dpre_gain=None, d_dpre_bias=None,
+                               d_workspace=None, workspace_bytes=0, stream=None):
+    check(lib().dsp_norm_residual_backward(C.byref(desc), _ptr(d_dh), _ptr(d_dy), _ptr(d_y), _ptr(d_z), _ptr(d_gate),
+                                           _ptr(d_post_gain), _ptr(d_post_bias), _ptr(d_pre_gain), _ptr(d_post_stats),
+                                           _ptr(d_pre_stats), _ptr(d_dx), _ptr(d_dz), _ptr(d_dgate), _ptr(d_dpost_gain),
+                                           _ptr(d_dpost_bias), _ptr(d_dpre_gain), _ptr(d_dpre_bias), _ptr(d_workspace),
+                                           workspace_bytes, _stream(stream)), "dsp_norm_residual_backward")
 
 
 def dsp_block_get_activation(b, layer, nbytes):

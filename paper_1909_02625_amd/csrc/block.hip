@@ -128,6 +128,12 @@ struct Layer {
 
 using namespace dsp;
 
+// A run of parameters to which weight decay applies or not.
+struct ParamRun {
+    size_t p0, n;
+    bool decay;
+};
+
 // A second set of the buffers a forward pass writes (activations, batch-norm statistics and scratch,
 // pooling indices), so that the forward pass of the current mini-batch can run on another stream
 // while the recompute / backward of a stale one uses the primary set.
@@ -175,6 +181,10 @@ struct dsp_block {
     float* loss_sink = nullptr;
 
     float last_lr = 0.f;  // step size of the latest update (the velocity is stored in its units)
+    std::vector<ParamRun> runs;   // the parameters, cut where weight decay begins or ends
+    dsp_adamw* adamw = nullptr;   // set by dsp_block_set_adamw
+    char* adamw_state = nullptr;  // its moments: [m][v] and, with 8 bits, their exponents
+    size_t adamw_bytes = 0;
     void* wgrad_ws = nullptr;  // per-slice partial weight gradients, one region per conv layer
     size_t wgrad_ws_bytes = 0;
     WgradReduceSet* wgrad_set = nullptr;  // sums all regions in one launch at the end of the backward sweep
@@ -504,6 +514,11 @@ static int build_graph(dsp_block* b)
             flat_task(L.p0, nw, true);
             flat_task(L.p0 + nw, (size_t)L.d.cout, false);
         }
+    }
+    b->runs.clear();
+    for (const UpdateTask& t : tasks) {
+        if (!b->runs.empty() && b->runs.back().decay == (t.decay != 0) && b->runs.back().p0 + b->runs.back().n == t.p0) b->runs.back().n += t.n;
+        else b->runs.push_back({t.p0, t.n, t.decay != 0});
     }
     DSP_TRY(update_plan_finish(tasks, b->dtype, &b->upd_blocks));
     b->upd_n_tasks = (int)tasks.size();
@@ -929,6 +944,8 @@ static int run_backward(dsp_block* b, const void* in, const void* gout, void* gi
 
 void block_set_dry(dsp_block* b, bool dry) { b->dry = dry; }
 
+bool block_has_adamw(const dsp_block* b) { return b->adamw != nullptr; }
+
 BlockArrays block_arrays(dsp_block* b) { return BlockArrays{b->x, b->g, b->nP}; }
 
 int block_load_params_device(dsp_block* b, const float* d_src, hipStream_t st)
@@ -979,6 +996,7 @@ int dsp_block_destroy(dsp_block* b)
 {
     if (!b) return DSP_OK;
     (void)hipDeviceSynchronize();
+    (void)dsp_adamw_destroy(b->adamw);
     for (void* p : b->allocs) (void)hipFree(p);
     wgrad_reduce_set_destroy(b->wgrad_set);
     wgrad_reduce_set_destroy(b->wgrad_set_odd);
@@ -1187,6 +1205,97 @@ int dsp_param_update_sum(dsp_block* b, float lr, float momentum, int32_t s, floa
 int dsp_param_update(dsp_block* b, float lr, float momentum, float weight_decay, void* stream)
 {
     return dsp_param_update_sum(b, lr, momentum, 0, weight_decay, stream);
+}
+
+int dsp_block_set_adamw(dsp_block* b, int32_t state_bits, uint64_t seed)
+{
+    DSP_REQUIRE(b && (state_bits == 32 || state_bits == 8), DSP_EINVAL, "dsp_block_set_adamw: bad argument (states of 32 or 8 bits)");
+    DSP_REQUIRE(!b->adamw, DSP_ESTATE, "dsp_block_set_adamw: the block has its moments already");
+    DSP_REQUIRE(b->nP > 0, DSP_EINVAL, "dsp_block_set_adamw: the block has no parameters");
+    constexpr size_t kBlock = 256;
+    const size_t es = state_bits == 8 ? 1 : 4;
+    try {
+        std::vector<dsp_adamw_tensor> t;
+        std::vector<size_t> at;
+        size_t blocks = 0;
+        for (const ParamRun& r : b->runs) {  // (whole blocks of the 8-bit states for every run)
+            at.push_back(blocks);
+            blocks += (r.n + kBlock - 1) / kBlock;
+        }
+        const size_t moment = blocks * kBlock * es, bytes = 2 * moment + (state_bits == 8 ? 2 * blocks : 0);
+        char* state = nullptr;
+        DSP_TRY(dev_alloc(b, (void**)&state, bytes, &b->param_bytes));
+        DSP_HIP(hipMemset(state, 0, bytes));
+        for (size_t i = 0; i < b->runs.size(); ++i) {
+            const ParamRun& r = b->runs[i];
+            dsp_adamw_tensor a = {};
+            a.d_param = b->x + r.p0;
+            a.d_grad = b->g + r.p0;
+            a.d_m = state + at[i] * kBlock * es;
+            a.d_v = state + moment + at[i] * kBlock * es;
+            if (state_bits == 8) {
+                a.d_m_exp = (uint8_t*)state + 2 * moment + at[i];
+                a.d_v_exp = a.d_m_exp + blocks;
+            }
+            a.n = (int64_t)r.n;
+            a.grad_dtype = DSP_FP32;
+            a.decay = r.decay ? 1 : 0;
+            t.push_back(a);
+        }
+        DSP_HIP(hipDeviceSynchronize());
+        DSP_TRY(dsp_adamw_init((int32_t)t.size(), t.data(), state_bits, seed, &b->adamw));
+        b->adamw_state = state;
+        b->adamw_bytes = bytes;
+    } catch (const std::bad_alloc&) {
+        set_error("dsp_block_set_adamw: out of host memory");
+        return DSP_ENOMEM;
+    }
+    return DSP_OK;
+}
+
+int dsp_param_update_adamw(dsp_block* b, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm,
+                           void* stream)
+{
+    DSP_REQUIRE(b, DSP_EINVAL, "dsp_param_update_adamw: null block");
+    DSP_REQUIRE(b->adamw, DSP_ESTATE, "dsp_param_update_adamw: dsp_block_set_adamw has not been called");
+    DSP_TRY(adamw_check_hyper(lr, beta1, beta2, eps, weight_decay, max_norm, "dsp_param_update_adamw"));
+    DSP_REQUIRE(b->pending, DSP_ESTATE, "dsp_param_update_adamw: no pending gradient");
+    if (!b->dry) {
+        DSP_TRY(dsp_adamw_step(b->adamw, lr, beta1, beta2, eps, weight_decay, max_norm, nullptr, stream));
+        DSP_TRY(launch_refresh_shadows(b->dtype, b->x, b->upd_tasks, b->upd_n_tasks, b->upd_blocks, b->tmap, b->tap_tab, b->wf16, b->wt,
+                                       b->nP, (hipStream_t)stream));
+    }
+    b->pending = false;
+    b->version += 1;
+    return DSP_OK;
+}
+
+// The moments as they lie and, behind them, the clock.
+int dsp_block_adamw_state_bytes(const dsp_block* b, size_t* bytes)
+{
+    DSP_REQUIRE(b && bytes, DSP_EINVAL, "dsp_block_adamw_state_bytes: bad argument");
+    DSP_REQUIRE(b->adamw, DSP_ESTATE, "dsp_block_adamw_state_bytes: dsp_block_set_adamw has not been called");
+    *bytes = b->adamw_bytes + kAdamwClockBytes;
+    return DSP_OK;
+}
+int dsp_block_get_adamw_state(dsp_block* b, void* h_dst, size_t bytes)
+{
+    DSP_REQUIRE(b && h_dst, DSP_EINVAL, "dsp_block_get_adamw_state: bad argument");
+    DSP_REQUIRE(b->adamw, DSP_ESTATE, "dsp_block_get_adamw_state: dsp_block_set_adamw has not been called");
+    DSP_REQUIRE(bytes == b->adamw_bytes + kAdamwClockBytes, DSP_EINVAL, "dsp_block_get_adamw_state: bad size");
+    DSP_HIP(hipDeviceSynchronize());
+    DSP_HIP(hipMemcpy(h_dst, b->adamw_state, b->adamw_bytes, hipMemcpyDeviceToHost));
+    return adamw_clock_read(b->adamw, (char*)h_dst + b->adamw_bytes);
+}
+int dsp_block_set_adamw_state(dsp_block* b, const void* h_src, size_t bytes)
+{
+    DSP_REQUIRE(b && h_src, DSP_EINVAL, "dsp_block_set_adamw_state: bad argument");
+    DSP_REQUIRE(b->adamw, DSP_ESTATE, "dsp_block_set_adamw_state: dsp_block_set_adamw has not been called");
+    DSP_REQUIRE(bytes == b->adamw_bytes + kAdamwClockBytes, DSP_EINVAL, "dsp_block_set_adamw_state: bad size");
+    DSP_HIP(hipDeviceSynchronize());
+    DSP_TRY(adamw_clock_write(b->adamw, (const char*)h_src + b->adamw_bytes));
+    DSP_HIP(hipMemcpy(b->adamw_state, h_src, b->adamw_bytes, hipMemcpyHostToDevice));
+    return DSP_OK;
 }
 
 int dsp_block_query(const dsp_block* b, int64_t out[8])

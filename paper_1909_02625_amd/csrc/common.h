@@ -30,6 +30,7 @@ struct BlockArrays {
     size_t n;
 };
 BlockArrays block_arrays(dsp_block* b);
+bool block_has_adamw(const dsp_block* b);
 // Overwrites the parameters with n floats in the library layout (device memory) and refreshes the
 // storage-type copies the kernels read; ordered on st.
 int block_load_params_device(dsp_block* b, const float* d_src, hipStream_t st);
@@ -318,6 +319,12 @@ int launch_sgd_update(int dtype, float* x, float* v, const float* g, const Updat
 // Same refresh of the copies without an update (after init / set_params).
 int launch_refresh_shadows(int dtype, const float* x, const UpdateTask* tasks, int n_tasks, int blocks, const int32_t* tmap,
                            const int32_t* tap_tab, void* wf16, void* wt, size_t n, hipStream_t st);
+// ---- AdamW (adamw.hip) ----
+int adamw_check_hyper(double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm, const char* who);
+// What an optimizer counts on the device -- steps and the products of its betas -- as it is kept in a checkpoint.
+constexpr size_t kAdamwClockBytes = 24;
+int adamw_clock_read(dsp_adamw* o, void* h_dst);
+int adamw_clock_write(dsp_adamw* o, const void* h_src);
 int launch_spin(int microseconds, hipStream_t st);
 // dst[p][0..Cp) = {src[p][0..C), 0...}: channel padding of an NHWC tensor (pixels rows) up to a whole 16-byte run.
 // y = a + b over n elements; backward of the sum: dx0 (and dx1, unless null) = dy or += dy, one read of dy

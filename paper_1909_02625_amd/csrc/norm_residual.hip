@@ -1,0 +1,742 @@
+// The joint between two residual blocks, in one pass over the rows:
+//
+//   n = N_post(z),  y = alpha x + beta act(gate) n,  h = N_pre(y)
+//
+// with N none, RMS or layer norm (gain, bias), and its backward pass, in which the gradient of every parameter is a sum over rows.
+#include "common.h"
+
+#include <algorithm>
+
+namespace dsp {
+namespace {
+
+constexpr int kMaxC = 16384;
+constexpr int kSubThreads = 256;  // workgroup of the kernels whose rows are shorter than a wave
+constexpr int kParts = 1024;      // workgroups of the backward kernel = rows of partial sums
+
+struct NormArgs {
+    const void *x, *z, *gate;
+    const float *post_gain, *post_bias, *pre_gain, *pre_bias;
+    void *y, *h;
+    float *post_stats, *pre_stats;
+    int64_t xs, zs, ys, hs, gs;
+    int M, C, post, pre, act, gate_f32, gate_rows;  // gate_rows = 0: no gate
+    float alpha, beta, eps;
+};
+
+struct NormBackArgs {
+    const void *dh, *dy, *y, *z, *gate;
+    const float *post_gain, *post_bias, *pre_gain, *post_stats, *pre_stats;
+    void *dx, *dz, *dgate;
+    float* partial;  // [P1, S1 (, P2, S2)][parts][C]
+    int64_t xs, zs, ys, hs, gs;
+    int M, C, post, pre, act, gate_f32, gate_rows;
+    int parts, groups, parts_per_group, rows_per_part;  // fold: rows_per_part = groups of a workgroup
+    float alpha, beta;
+};
+
+// Runs of 16 bytes on addresses of the element's size: rows may begin at any element (an odd C, a stride of the caller's).
+template <typename T>
+struct RowIO;
+template <>
+struct RowIO<float> {
+    static constexpr int VW = 4;
+    typedef float Raw __attribute__((ext_vector_type(4), aligned(4)));
+    __device__ static inline void unpack(const Raw& r, float (&v)[VW])
+    {
+#pragma unroll
+        for (int e = 0; e < VW; ++e) v[e] = r[e];
+    }
+    __device__ static inline Raw pack(const float (&v)[VW]) { return Raw{v[0], v[1], v[2], v[3]}; }
+};
+template <>
+struct RowIO<bf16_t> {
+    static constexpr int VW = 8;
+    typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(2)));
+    __device__ static inline void unpack(const Raw& r, float (&v)[VW])
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(r[e] << 16);
+            v[2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u);
+        }
+    }
+    __device__ static inline Raw pack(const float (&v)[VW])
+    {
+        return Raw{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    }
+};
+
+// VW elements from column c on; those behind the row are `rest`.
+template <typename T>
+__device__ inline void load_run(const T* row, int c, int C, float (&v)[RowIO<T>::VW], float rest = 0.f)
+{
+    constexpr int VW = RowIO<T>::VW;
+    if (c + VW <= C) {
+        RowIO<T>::unpack(*(const typename RowIO<T>::Raw*)(row + c), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VW; ++e) v[e] = c + e < C ? to_float<T>(row[c + e]) : rest;
+    }
+}
+template <typename T>
+__device__ inline void store_run(T* row, int c, int C, const float (&v)[RowIO<T>::VW])
+{
+    constexpr int VW = RowIO<T>::VW;
+    if (c + VW <= C) {
+        *(typename RowIO<T>::Raw*)(row + c) = RowIO<T>::pack(v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VW; ++e)
+            if (c + e < C) row[c + e] = from_float<T>(v[e]);
+    }
+}
+// A vector of floats (gains, biases) at the columns of a run of N elements; `rest` where there is no vector or no column.
+template <int N>
+__device__ inline void load_vector(const float* p, int c, int C, float (&v)[N], float rest)
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = p && c + e < C ? p[c + e] : rest;
+}
+// A run of one row of the gate, as floats.
+template <typename T>
+__device__ inline void load_gate(const void* gate, int gate_f32, int64_t at, int c, int C, float (&v)[RowIO<T>::VW])
+{
+    if (sizeof(T) == 4 || !gate_f32) {
+        load_run<T>((const T*)gate + at, c, C, v);
+    } else {
+        load_vector(((const float*)gate) + at, c, C, v, 0.f);
+    }
+}
+
+__device__ inline float gate_act(int act, float g)
+{
+    return act == DSP_GATE_IDENTITY ? g : act == DSP_GATE_SIGMOID ? 1.f / (1.f + expf(-g)) : tanhf(g);
+}
+__device__ inline float gate_slope(int act, float g)
+{
+    // sigmoid' = e / (1 + e)^2 with e = exp(-|g|), tanh' = 4 sigmoid'(2 g): no difference of nearly equal numbers
+    if (act == DSP_GATE_IDENTITY) return 1.f;
+    const float e = expf(-fabsf(act == DSP_GATE_SIGMOID ? g : 2.f * g)), q = 1.f / (1.f + e);
+    return (act == DSP_GATE_SIGMOID ? 1.f : 4.f) * e * q * q;
+}
+
+// Sums of K values over the TPR lanes of a row (TPR = 0: over the workgroup, through `red`, one barrier), in every lane.  The
+// two halves of `red` are used in turn: what a half held has been read by everyone once the other half's barrier is passed.
+template <int TPR, int K>
+struct RowSum {
+    float (*red)[16][K];
+    int turn = 0;
+    __device__ inline void operator()(float (&v)[K])
+    {
+        constexpr int LANES = TPR ? TPR : 64;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#define STEP(ctrl) v[k] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v[k]), ctrl, 0xf, 0xf, true))
+            STEP(0xB1);                      // quad_perm 1,0,3,2
+            STEP(0x4E);                      // quad_perm 2,3,0,1
+            STEP(0x141);                     // row_half_mirror
+            if (LANES >= 16) STEP(0x140);    // row_mirror
+#undef STEP
+        }
+#pragma unroll
+        for (int off = 16; off < LANES; off *= 2)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], off, 64);
+        if (TPR == 0) {
+            const int waves = blockDim.x / 64;
+            if (waves == 1) return;
+            if (threadIdx.x % 64 == 0)
+#pragma unroll
+                for (int k = 0; k < K; ++k) red[turn][threadIdx.x / 64][k] = v[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = 0.f;
+            for (int w = 0; w < waves; ++w)
+#pragma unroll
+                for (int k = 0; k < K; ++k) v[k] += red[turn][w][k];
+            turn ^= 1;
+        }
+    }
+};
+
+// Mean (layer norm; else 0) and 1 / deviation of a row whose runs a thread holds; columns behind the row hold 0.  Centred
+// before it is squared: a row far from zero keeps its variance.
+template <int TPR, int NV, int VW>
+__device__ inline void row_stats(int kind, const float (&a)[NV][VW], const bool (&in)[NV][VW], float inv_c, float eps, RowSum<TPR, 1>& sum,
+                                 float& mean, float& inv)
+{
+    mean = 0.f;
+    float s[1];
+    if (kind == DSP_NORM_LAYER) {
+        s[0] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) s[0] += a[k][e];
+        sum(s);
+        mean = s[0] * inv_c;
+    }
+    s[0] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+            const float d = in[k][e] ? a[k][e] - mean : 0.f;
+            s[0] += d * d;
+        }
+    sum(s);
+    inv = 1.f / sqrtf(s[0] * inv_c + eps);
+}
+
+// TPR lanes a row and 256 / TPR rows a workgroup, or (TPR = 0) a row a workgroup of whole waves; NV runs a thread.
+template <typename T, int TPR, int NV, int MAXT>
+__global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
+{
+    constexpr int VW = RowIO<T>::VW;
+    __shared__ float red[2][16][1];
+    RowSum<TPR, 1> sum{red};
+    const int tid = threadIdx.x;
+    const int t = TPR ? tid % (TPR ? TPR : 1) : tid, threads = TPR ? TPR : (int)blockDim.x;
+    const int rows = TPR ? kSubThreads / (TPR ? TPR : 1) : 1, slot = TPR ? tid / (TPR ? TPR : 1) : 0;
+    const float inv_c = 1.f / (float)a.C;
+    const bool row_gate = a.gate_rows > 0 && a.gate_rows < a.M;
+    int c[NV];
+    bool in[NV][VW];
+    float gpost[NV][VW], gpre[NV][VW], w[NV][VW];  // w: beta, times the gate where one row of it serves all
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        c[k] = (t + k * threads) * VW;
+#pragma unroll
+        for (int e = 0; e < VW; ++e) in[k][e] = c[k] + e < a.C;
+        load_vector(a.post_gain, c[k], a.C, gpost[k], 1.f);
+        load_vector(a.pre_gain, c[k], a.C, gpre[k], 1.f);
+        if (a.gate_rows && !row_gate) load_gate<T>(a.gate, a.gate_f32, 0, c[k], a.C, w[k]);
+#pragma unroll
+        for (int e = 0; e < VW; ++e) w[k][e] = a.gate_rows && !row_gate ? a.beta * gate_act(a.act, w[k][e]) : a.beta;
+    }
+    for (int64_t base = (int64_t)blockIdx.x * rows; base < a.M; base += (int64_t)gridDim.x * rows) {
+        const bool live = base + slot < a.M;
+        const int64_t row = live ? base + slot : a.M - 1;
+        float z[NV][VW], y[NV][VW];
+        float mean = 0.f, inv = 1.f;
+        if (a.z) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) load_run<T>((const T*)a.z + row * a.zs, c[k], a.C, z[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) load_run<T>((const T*)a.x + row * a.xs, c[k], a.C, y[k]);
+        if (a.z) {
+            if (a.post != DSP_NORM_NONE) {
+                row_stats<TPR, NV, VW>(a.post, z, in, inv_c, a.eps, sum, mean, inv);
+                if (t == 0 && live && a.post_stats) {
+                    a.post_stats[row] = mean;
+                    a.post_stats[a.M + row] = inv;
+                }
+            }
+            const int64_t group = row_gate ? (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) : 0;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float g[VW];
+                if (row_gate) load_gate<T>(a.gate, a.gate_f32, group * a.gs, c[k], a.C, g);
+#pragma unroll
+                for (int e = 0; e < VW; ++e) {
+                    const float act = row_gate ? w[k][e] * gate_act(a.act, g[e]) : w[k][e];
+                    float n = (z[k][e] - mean) * inv * gpost[k][e];
+                    if (a.post_bias && in[k][e]) n += a.post_bias[c[k] + e];
+                    y[k][e] = in[k][e] ? a.alpha * y[k][e] + act * n : 0.f;
+                }
+                if (live) store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k]);
+            }
+        }
+        if (a.pre == DSP_NORM_NONE) continue;
+        row_stats<TPR, NV, VW>(a.pre, y, in, inv_c, a.eps, sum, mean, inv);
+        if (t == 0 && live && a.pre_stats) {
+            a.pre_stats[row] = mean;
+            a.pre_stats[a.M + row] = inv;
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                y[k][e] = (y[k][e] - mean) * inv * gpre[k][e];
+                if (a.pre_bias && in[k][e]) y[k][e] += a.pre_bias[c[k] + e];
+            }
+            if (live) store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k]);
+        }
+    }
+}
+
+// ---- backward ------------------------------------------------------------------------------------
+// With yhat, zhat the normalised rows, r their 1 / deviation, w = beta act(gate) gain_post and q = dy + r_y dh gain_pre, the
+// gradient of y is D = q - r_y (s0 + yhat s1) with s1 = mean(dh gain_pre yhat), s0 = mean(dh gain_pre) (layer norm only), and
+// the sums that z's gradient needs are linear in D: sum w zhat D = sum w zhat q - r_y (s0 sum w zhat + s1 sum w zhat yhat).
+// All sums of a row are taken in ONE round, the elements are finished behind it.
+//
+// Parameters: P1 = sum dh yhat, P2 = sum dh; S1 = sum zhat D, S2 = sum D over the rows of one row of the gate, from which
+// dgain_post = beta act S1, dbias_post = beta act S2 and dgate = beta act' (gain_post S1 + bias_post S2) follow per column.
+// A thread keeps its columns' sums in registers over all rows of its workgroup.  FOLD (a gate with more rows than there are
+// workgroups): a workgroup takes whole rows of the gate, writes their dgate at once and folds the rest into sums of its own.
+template <typename T, int TPR, int NV, int MAXT, bool FULL, bool FOLD>
+__global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
+{
+    constexpr int VW = RowIO<T>::VW, K = FULL ? 8 : 3, ACC = FULL ? 4 : 2;
+    __shared__ float red[2][16][K];
+    __shared__ float fold[TPR ? kSubThreads * VW : 1];
+    RowSum<TPR, K> sum{red};
+    const int tid = threadIdx.x;
+    const int t = TPR ? tid % (TPR ? TPR : 1) : tid, threads = TPR ? TPR : (int)blockDim.x;
+    const int slots = TPR ? kSubThreads / (TPR ? TPR : 1) : 1, slot = TPR ? tid / (TPR ? TPR : 1) : 0;
+    const float inv_c = 1.f / (float)a.C;
+    const bool pre = a.pre != DSP_NORM_NONE, post = a.post != DSP_NORM_NONE;
+    int c[NV];
+    float w[NV][VW], gpre[NV][VW], p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        c[k] = (t + k * threads) * VW;
+        load_vector(a.pre_gain, c[k], a.C, gpre[k], 1.f);
+#pragma unroll
+        for (int e = 0; e < VW; ++e) p1[k][e] = p2[k][e] = s1[k][e] = s2[k][e] = f1[k][e] = f2[k][e] = 0.f;
+    }
+    // w of a row of the gate
+    auto weights = [&](int64_t group) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float g[VW];
+            load_vector(a.post_gain, c[k], a.C, w[k], 1.f);
+            if (a.gate_rows) load_gate<T>(a.gate, a.gate_f32, group * a.gs, c[k], a.C, g);
+#pragma unroll
+            for (int e = 0; e < VW; ++e) w[k][e] *= a.gate_rows ? a.beta * gate_act(a.act, g[e]) : a.beta;
+        }
+    };
+    auto one_row = [&](int64_t at, bool live) {
+        const int64_t row = live ? at : a.M - 1;
+        float zh[NV][VW], yh[NV][VW], q[NV][VW], dh[NV][VW];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (pre) {
+                load_run<T>((const T*)a.dh + row * a.hs, c[k], a.C, dh[k]);
+                load_run<T>((const T*)a.y + row * a.ys, c[k], a.C, yh[k]);
+            }
+            if (a.z) load_run<T>((const T*)a.z + row * a.zs, c[k], a.C, zh[k]);
+            if (a.dy) load_run<T>((const T*)a.dy + row * a.ys, c[k], a.C, q[k]);
+        }
+        const float my = pre ? a.pre_stats[row] : 0.f, ry = pre ? a.pre_stats[a.M + row] : 0.f;
+        const float mz = post ? a.post_stats[row] : 0.f, rz = post ? a.post_stats[a.M + row] : 1.f;
+        float s[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[k] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                const bool in = c[k] + e < a.C;
+                if (!a.dy) q[k][e] = 0.f;
+                if (!pre) dh[k][e] = yh[k][e] = 0.f;
+                if (!a.z) zh[k][e] = 0.f;
+                yh[k][e] = in ? (yh[k][e] - my) * ry : 0.f;
+                zh[k][e] = in ? (zh[k][e] - mz) * rz : 0.f;
+                const float b = dh[k][e] * gpre[k][e], wz = w[k][e] * zh[k][e];
+                q[k][e] += ry * b;
+                s[0] += b * yh[k][e];
+                s[1] += wz * q[k][e];
+                s[2] += wz * yh[k][e];
+                if (FULL) {
+                    const float wi = in ? w[k][e] : 0.f;
+                    s[3 % K] += b;
+                    s[4 % K] += wz;
+                    s[5 % K] += wi * q[k][e];
+                    s[6 % K] += wi * yh[k][e];
+                    s[7 % K] += wi;
+                }
+            }
+        if (pre || post) sum(s);
+        const float m1 = pre ? s[0] * inv_c : 0.f, m0 = FULL && a.pre == DSP_NORM_LAYER ? s[3 % K] * inv_c : 0.f;
+        float t1 = 0.f, t0 = 0.f;
+        if (post) {
+            t1 = (s[1] - ry * (m1 * s[2] + (FULL ? m0 * s[4 % K] : 0.f))) * inv_c;
+            if (FULL && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - ry * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float dz[VW];
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                const float D = c[k] + e < a.C ? q[k][e] - ry * (m0 + yh[k][e] * m1) : 0.f;
+                if (live) {
+                    p1[k][e] += dh[k][e] * yh[k][e];
+                    s1[k][e] += zh[k][e] * D;
+                    if (FULL) {
+                        p2[k][e] += dh[k][e];
+                        s2[k][e] += D;
+                    }
+                }
+                dz[e] = post ? rz * (w[k][e] * D - t0 - zh[k][e] * t1) : w[k][e] * D;
+                q[k][e] = a.alpha * D;
+            }
+            if (live && a.dx) store_run<T>((T*)a.dx + row * a.xs, c[k], a.C, q[k]);
+            if (live && a.dz) store_run<T>((T*)a.dz + row * a.zs, c[k], a.C, dz);
+        }
+    };
+
+    if (FOLD) {
+        const int64_t g0 = (int64_t)blockIdx.x * a.rows_per_part, g1 = min(g0 + a.rows_per_part, (int64_t)a.groups);
+        for (int64_t gb = g0; gb < g1; gb += slots) {
+            const bool mine = gb + slot < g1;
+            const int64_t group = mine ? gb + slot : g1 - 1;
+            weights(group);
+            for (int i = 0; i < a.gate_rows; ++i) {
+                const int64_t row = group * a.gate_rows + i;
+                one_row(row, mine && row < a.M);
+            }
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float g[VW], gain[VW], bias[VW];
+                load_gate<T>(a.gate, a.gate_f32, group * a.gs, c[k], a.C, g);
+                load_vector(a.post_gain, c[k], a.C, gain, 1.f);
+                load_vector(a.post_bias, c[k], a.C, bias, 0.f);
+#pragma unroll
+                for (int e = 0; e < VW; ++e) {
+                    const float act = a.beta * gate_act(a.act, g[e]);
+                    const float d = a.beta * gate_slope(a.act, g[e]) * (gain[e] * s1[k][e] + (FULL ? bias[e] * s2[k][e] : 0.f));
+                    f1[k][e] += act * s1[k][e];
+                    f2[k][e] += act * s2[k][e];
+                    s1[k][e] = s2[k][e] = 0.f;
+                    g[e] = d;
+                }
+                if (mine && a.dgate) {
+                    if (sizeof(T) == 4 || !a.gate_f32) {
+                        store_run<T>((T*)a.dgate + group * a.gs, c[k], a.C, g);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VW; ++e)
+                            if (c[k] + e < a.C) ((float*)a.dgate)[group * a.gs + c[k] + e] = g[e];
+                    }
+                }
+            }
+        }
+    } else {
+        const int group = blockIdx.x / a.parts_per_group, part = blockIdx.x % a.parts_per_group;
+        const int64_t rows = a.gate_rows ? a.gate_rows : a.M;
+        const int64_t r0 = group * rows + (int64_t)part * a.rows_per_part;
+        const int64_t r1 = min(min(r0 + a.rows_per_part, (group + 1) * rows), (int64_t)a.M);
+        weights(group);
+        for (int64_t r = r0; r < r1; r += slots) one_row(r + slot, r + slot < r1);
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int acc = 0; acc < ACC; ++acc) {
+        float* out = a.partial + ((size_t)acc * a.parts + blockIdx.x) * a.C;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float v[VW];
+#pragma unroll
+            for (int e = 0; e < VW; ++e)
+                v[e] = acc == 0 ? p1[k][e] : acc == 2 ? p2[k][e] : acc == 1 ? (FOLD ? f1 : s1)[k][e] : (FOLD ? f2 : s2)[k][e];
+            if (TPR) {  // the workgroup's rows side by side: their sums in the order of the slots (NV = 1)
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < VW; ++e) fold[tid * VW + e] = v[e];
+                __syncthreads();
+                if (slot == 0)
+                    for (int r = 1; r < slots; ++r)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) v[e] += fold[(r * threads + t) * VW + e];
+            }
+            if (slot == 0) store_run<float>(out, c[k], a.C, *(float(*)[4])v);
+            if (slot == 0 && VW == 8) store_run<float>(out, c[k] + 4, a.C, *(float(*)[4])(v + VW - 4));
+        }
+    }
+}
+
+struct NormFinalArgs {
+    const float* partial;
+    const void* gate;
+    const float *post_gain, *post_bias;
+    void* dgate;
+    float *dpost_gain, *dpost_bias, *dpre_gain, *dpre_bias;
+    int64_t gs;
+    int C, parts, groups, parts_per_group, full, fold, act, gate_f16, gate_any;
+    float beta;
+};
+
+// 64 columns a workgroup, a wave each for every sixteenth part; partial sums are added in a fixed order.
+constexpr int kFinalWaves = 16;
+__global__ __launch_bounds__(64 * kFinalWaves) void norm_residual_final_kernel(NormFinalArgs a)
+{
+    __shared__ float red[kFinalWaves][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    const bool in = c < a.C;
+    auto total = [&](float v) -> float {  // over the waves, in all of them
+        __syncthreads();
+        red[wave][lane] = v;
+        __syncthreads();
+        v = 0.f;
+        for (int w = 0; w < kFinalWaves; ++w) v += red[w][lane];
+        return v;
+    };
+    auto parts_of = [&](int acc, int first, int n, int step) -> float {  // parts first, first + step .. of n
+        float v = 0.f;
+        if (!in) return v;
+        const float* p = a.partial + ((size_t)acc * a.parts + first) * a.C + c;
+#pragma unroll 8
+        for (int i = 0; i < n; i += step) v += p[(size_t)i * a.C];
+        return v;
+    };
+    auto gate_of = [&](int g) -> float {
+        return a.gate_f16 ? bf16_to_float(((const bf16_t*)a.gate)[g * a.gs + c]) : ((const float*)a.gate)[g * a.gs + c];
+    };
+    const float gain = in && a.post_gain ? a.post_gain[c] : 1.f, bias = in && a.post_bias ? a.post_bias[c] : 0.f;
+    // gradient of the gate's row g from its sums; returns what the row gives to the gain and the bias behind it
+    auto gate_row = [&](int g, float s1, float s2, bool write, float& d1, float& d2) {
+        float act = a.beta;
+        if (in && a.gate_any) {
+            const float v = gate_of(g);
+            act *= gate_act(a.act, v);
+            if (write && a.dgate) {
+                const float d = a.beta * gate_slope(a.act, v) * (gain * s1 + bias * s2);
+                if (a.gate_f16) ((bf16_t*)a.dgate)[g * a.gs + c] = float_to_bf16(d);
+                else ((float*)a.dgate)[g * a.gs + c] = d;
+            }
+        }
+        d1 += act * s1;
+        d2 += act * s2;
+    };
+
+    if (a.dpre_gain || a.dpre_bias) {
+        const float p1 = total(wave < a.parts ? parts_of(0, wave, a.parts - wave, kFinalWaves) : 0.f);
+        const float p2 = a.full ? total(wave < a.parts ? parts_of(2, wave, a.parts - wave, kFinalWaves) : 0.f) : 0.f;
+        if (wave == 0 && in) {
+            if (a.dpre_gain) a.dpre_gain[c] = p1;
+            if (a.dpre_bias) a.dpre_bias[c] = p2;
+        }
+    }
+    if (!a.dpost_gain && !a.dpost_bias && !(a.dgate && !a.fold)) return;
+    float d1 = 0.f, d2 = 0.f;
+    if (a.fold) {
+        d1 = total(wave < a.parts ? parts_of(1, wave, a.parts - wave, kFinalWaves) : 0.f);
+        d2 = a.full ? total(wave < a.parts ? parts_of(3, wave, a.parts - wave, kFinalWaves) : 0.f) : 0.f;
+    } else if (a.parts_per_group >= kFinalWaves || a.groups == 1) {  // few rows of the gate: the waves share the parts of each
+        for (int g = 0; g < a.groups; ++g) {
+            const int n = a.parts_per_group - wave;
+            const float s1 = total(n > 0 ? parts_of(1, g * a.parts_per_group + wave, n, kFinalWaves) : 0.f);
+            const float s2 = a.full ? total(n > 0 ? parts_of(3, g * a.parts_per_group + wave, n, kFinalWaves) : 0.f) : 0.f;
+            gate_row(g, s1, s2, wave == 0, d1, d2);
+        }
+    } else {  // many: every wave takes rows of its own
+        for (int g = wave; g < a.groups; g += kFinalWaves) {
+            const float s1 = parts_of(1, g * a.parts_per_group, a.parts_per_group, 1);
+            const float s2 = a.full ? parts_of(3, g * a.parts_per_group, a.parts_per_group, 1) : 0.f;
+            gate_row(g, s1, s2, true, d1, d2);
+        }
+        d1 = total(d1);
+        d2 = total(d2);
+    }
+    if (wave == 0 && in) {
+        if (a.dpost_gain) a.dpost_gain[c] = d1;
+        if (a.dpost_bias) a.dpost_bias[c] = d2;
+    }
+}
+
+bool kind_ok(int32_t k) { return k == DSP_NORM_NONE || k == DSP_NORM_RMS || k == DSP_NORM_LAYER; }
+
+int64_t stride_of(int64_t s, int32_t C) { return s ? s : C; }
+
+int check_desc(const dsp_norm_residual_desc* d, const char* who)
+{
+    DSP_REQUIRE(d, DSP_EINVAL, "%s: null descriptor", who);
+    DSP_REQUIRE((d->dtype == DSP_FP32 || d->dtype == DSP_BF16) && kind_ok(d->post) && kind_ok(d->pre), DSP_EINVAL,
+                "%s: bad type or norm", who);
+    DSP_REQUIRE(d->M > 0 && d->M < (1ll << 31) && d->C > 0 && d->C <= kMaxC, DSP_EINVAL, "%s: bad shape (rows of at most %d elements)",
+                who, kMaxC);
+    DSP_REQUIRE(d->eps > 0.f && d->eps < INFINITY, DSP_EINVAL, "%s: eps must be > 0", who);
+    DSP_REQUIRE(d->gate_rows >= 0, DSP_EINVAL, "%s: bad gate_rows", who);
+    DSP_REQUIRE(!d->gate_rows || ((d->gate_dtype == DSP_FP32 || d->gate_dtype == d->dtype) &&
+                                  (d->gate_act == DSP_GATE_IDENTITY || d->gate_act == DSP_GATE_SIGMOID || d->gate_act == DSP_GATE_TANH)),
+                DSP_EINVAL, "%s: bad gate (float or the rows' type; identity, sigmoid or tanh)", who);
+    const int64_t strides[5] = {d->x_stride, d->z_stride, d->y_stride, d->h_stride, d->gate_rows ? d->gate_stride : 0};
+    for (int64_t s : strides)
+        DSP_REQUIRE(s == 0 || (s >= d->C && s < (1ll << 31)), DSP_EINVAL, "%s: a row stride is shorter than the row", who);
+    return DSP_OK;
+}
+
+bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+
+// Threads and runs a thread that hold a row of C elements.
+struct RowShape {
+    int tpr;   // lanes of a row that is shorter than a wave; 0: `waves` waves
+    int waves, nv;
+};
+RowShape row_shape(int dtype, int C)
+{
+    const int vw = dtype == DSP_BF16 ? 8 : 4, runs = ceil_div(C, vw);
+    if (runs <= 8) return {8, 1, 1};
+    if (runs <= 16) return {16, 1, 1};
+    if (runs <= 32) return {32, 1, 1};
+    const int nv = runs <= 1024 ? 1 : runs <= 2048 ? 2 : 4;
+    return {0, ceil_div(runs, 64 * nv), nv};
+}
+
+// How the backward kernel's workgroups share the rows.
+struct BackPlan {
+    bool full, fold;
+    int parts, groups, parts_per_group, rows_per_part;
+    size_t bytes;
+};
+BackPlan back_plan(const dsp_norm_residual_desc* d, bool biased)
+{
+    BackPlan p;
+    const RowShape s = row_shape(d->dtype, d->C);
+    const int slots = s.tpr ? kSubThreads / s.tpr : 1;
+    const int64_t rows = d->gate_rows && d->gate_rows < d->M ? d->gate_rows : d->M;
+    const int64_t groups = (d->M + rows - 1) / rows;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kParts, (d->M + slots - 1) / slots));
+    p.full = biased || d->post == DSP_NORM_LAYER || d->pre == DSP_NORM_LAYER;
+    p.fold = groups > want;
+    p.groups = (int)groups;
+    if (p.fold) {
+        p.rows_per_part = (int)((groups + want - 1) / want);
+        p.parts = (int)((groups + p.rows_per_part - 1) / p.rows_per_part);
+        p.parts_per_group = 1;
+    } else {
+        const int64_t per = std::max<int64_t>(1, std::min<int64_t>(want / groups, (rows + slots - 1) / slots));
+        p.rows_per_part = (int)((rows + per - 1) / per);
+        p.parts_per_group = (int)((rows + p.rows_per_part - 1) / p.rows_per_part);
+        p.parts = (int)(groups * p.parts_per_group);
+    }
+    p.bytes = (size_t)p.parts * (p.full ? 4 : 2) * d->C * sizeof(float);
+    return p;
+}
+
+template <typename T>
+int forward_t(const NormArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
+{
+    const int rows = s.tpr ? kSubThreads / s.tpr : 1;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.M, rows), 4096)), block(s.tpr ? kSubThreads : 64 * s.waves);
+    if (s.tpr == 8) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 8, 1, kSubThreads>), grid, block, 0, st, a);
+    else if (s.tpr == 16) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 16, 1, kSubThreads>), grid, block, 0, st, a);
+    else if (s.tpr == 32) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 32, 1, kSubThreads>), grid, block, 0, st, a);
+    else if (s.nv == 1) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 0, 1, 1024>), grid, block, 0, st, a);
+    else if (s.nv == 2) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 0, 2, 1024>), grid, block, 0, st, a);
+    else DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 0, 4, 1024>), grid, block, 0, st, a);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+template <typename T, bool FULL, bool FOLD>
+int backward_t(const NormBackArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
+{
+    const dim3 grid(a.parts), block(s.tpr ? kSubThreads : 64 * s.waves);
+    if (s.tpr == 8) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 8, 1, kSubThreads, FULL, FOLD>), grid, block, 0, st, a);
+    else if (s.tpr == 16) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 16, 1, kSubThreads, FULL, FOLD>), grid, block, 0, st, a);
+    else if (s.tpr == 32) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 32, 1, kSubThreads, FULL, FOLD>), grid, block, 0, st, a);
+    else if (s.nv == 1) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 0, 1, 1024, FULL, FOLD>), grid, block, 0, st, a);
+    else if (s.nv == 2) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 0, 2, 1024, FULL, FOLD>), grid, block, 0, st, a);
+    else DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 0, 4, 1024, FULL, FOLD>), grid, block, 0, st, a);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+}  // namespace
+}  // namespace dsp
+
+using namespace dsp;
+
+extern "C" {
+
+int dsp_norm_residual_forward(const dsp_norm_residual_desc* d, const void* d_x, const void* d_z, const void* d_gate,
+                              const float* d_post_gain, const float* d_post_bias, const float* d_pre_gain, const float* d_pre_bias,
+                              void* d_y, void* d_h, float* d_post_stats, float* d_pre_stats, void* stream)
+{
+    DSP_TRY(check_desc(d, "dsp_norm_residual_forward"));
+    const bool pre = d->pre != DSP_NORM_NONE, post = d->post != DSP_NORM_NONE;
+    DSP_REQUIRE(d_x && (!pre || d_h) && (!d->gate_rows || d_gate), DSP_EINVAL, "dsp_norm_residual_forward: null buffer");
+    if (d_z) DSP_REQUIRE(d_y, DSP_EINVAL, "dsp_norm_residual_forward: null buffer");
+    else DSP_REQUIRE(pre && !post && !d->gate_rows && !d_y && d->alpha == 1.f, DSP_EINVAL,
+                     "dsp_norm_residual_forward: without a branch there is the norm in front of the next block alone (d_y NULL, alpha 1)");
+    const size_t e = dtype_size(d->dtype);
+    DSP_REQUIRE(aligned_to(d_x, e) && aligned_to(d_z, e) && aligned_to(d_y, e) && aligned_to(d_h, e) &&
+                    aligned_to(d_gate, dtype_size(d->gate_dtype)), DSP_EINVAL, "dsp_norm_residual_forward: misaligned buffer");
+    NormArgs a;
+    a.x = d_x; a.z = d_z; a.gate = d_gate;
+    a.post_gain = post ? d_post_gain : nullptr; a.post_bias = post ? d_post_bias : nullptr;
+    a.pre_gain = d_pre_gain; a.pre_bias = d_pre_bias;
+    a.y = d_y; a.h = d_h; a.post_stats = d_post_stats; a.pre_stats = d_pre_stats;
+    a.xs = stride_of(d->x_stride, d->C); a.zs = stride_of(d->z_stride, d->C); a.ys = stride_of(d->y_stride, d->C);
+    a.hs = stride_of(d->h_stride, d->C); a.gs = stride_of(d->gate_stride, d->C);
+    a.M = (int)d->M; a.C = d->C; a.post = d->post; a.pre = d->pre; a.act = d->gate_act; a.gate_f32 = d->gate_dtype == DSP_FP32;
+    a.gate_rows = (int)std::min<int64_t>(d->gate_rows, d->M);
+    a.alpha = d->alpha; a.beta = d->beta; a.eps = d->eps;
+    const double n = (double)d->M * d->C;
+    ProfScope ps("norm_residual_fwd", n * e * (d_z ? (pre ? 4 : 3) : 2), 1);
+    const RowShape s = row_shape(d->dtype, d->C);
+    return d->dtype == DSP_BF16 ? forward_t<bf16_t>(a, s, (hipStream_t)stream, ps)
+                                : forward_t<float>(a, s, (hipStream_t)stream, ps);
+}
+
+int dsp_norm_residual_workspace_bytes(const dsp_norm_residual_desc* d, size_t* bytes)
+{
+    DSP_REQUIRE(bytes, DSP_EINVAL, "dsp_norm_residual_workspace_bytes: null argument");
+    DSP_TRY(check_desc(d, "dsp_norm_residual_workspace_bytes"));
+    *bytes = back_plan(d, true).bytes;
+    return DSP_OK;
+}
+
+int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh, const void* d_dy, const void* d_y, const void* d_z,
+                               const void* d_gate, const float* d_post_gain, const float* d_post_bias, const float* d_pre_gain,
+                               const float* d_post_stats, const float* d_pre_stats, void* d_dx, void* d_dz, void* d_dgate,
+                               float* d_dpost_gain, float* d_dpost_bias, float* d_dpre_gain, float* d_dpre_bias,
+                               void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    DSP_TRY(check_desc(d, "dsp_norm_residual_backward"));
+    const bool pre = d->pre != DSP_NORM_NONE, post = d->post != DSP_NORM_NONE;
+    DSP_REQUIRE((d_dx || d_dz || d_dgate || d_dpost_gain || d_dpost_bias || d_dpre_gain || d_dpre_bias) && (pre ? d_dh && d_y && d_pre_stats : d_dy != nullptr) && (!d->gate_rows || d_gate) &&
+                    (!post || (d_z && d_post_stats)) && (!d_dgate || (d->gate_rows && d_z)),
+                DSP_EINVAL, "dsp_norm_residual_backward: null buffer");
+    DSP_REQUIRE((pre || (!d_dpre_gain && !d_dpre_bias)) && (post || (!d_dpost_gain && !d_dpost_bias)), DSP_EINVAL,
+                "dsp_norm_residual_backward: gradient of a norm that is not there");
+    const size_t e = dtype_size(d->dtype);
+    DSP_REQUIRE(aligned_to(d_dh, e) && aligned_to(d_dy, e) && aligned_to(d_y, e) && aligned_to(d_z, e) && aligned_to(d_dx, e) &&
+                    aligned_to(d_dz, e) && aligned_to(d_gate, dtype_size(d->gate_dtype)) && aligned_to(d_dgate, dtype_size(d->gate_dtype)),
+                DSP_EINVAL, "dsp_norm_residual_backward: misaligned buffer");
+    const BackPlan p = back_plan(d, d_dpre_bias || d_dpost_bias || (d_dgate && d_post_bias && post));
+    const bool sums = d_dpre_gain || d_dpre_bias || d_dpost_gain || d_dpost_bias || (d_dgate && !p.fold);
+    DSP_REQUIRE(!sums || (d_workspace && workspace_bytes >= p.bytes && ((uintptr_t)d_workspace % 16) == 0), DSP_EINVAL,
+                "dsp_norm_residual_backward: workspace too small or not 16-byte aligned (%zu < %zu)", workspace_bytes, p.bytes);
+    NormBackArgs a;
+    a.dh = d_dh; a.dy = d_dy; a.y = d_y; a.z = post || d_dgate ? d_z : nullptr; a.gate = d_gate;
+    a.post_gain = post ? d_post_gain : nullptr; a.post_bias = post ? d_post_bias : nullptr; a.pre_gain = pre ? d_pre_gain : nullptr;
+    a.post_stats = d_post_stats; a.pre_stats = d_pre_stats;
+    a.dx = d_dx; a.dz = d_dz; a.dgate = d_dgate; a.partial = sums ? (float*)d_workspace : nullptr;
+    a.xs = stride_of(d->x_stride, d->C); a.zs = stride_of(d->z_stride, d->C); a.ys = stride_of(d->y_stride, d->C);
+    a.hs = stride_of(d->h_stride, d->C); a.gs = stride_of(d->gate_stride, d->C);
+    a.M = (int)d->M; a.C = d->C; a.post = d->post; a.pre = d->pre; a.act = d->gate_act; a.gate_f32 = d->gate_dtype == DSP_FP32;
+    a.gate_rows = (int)std::min<int64_t>(d->gate_rows, d->M);
+    a.parts = p.parts; a.groups = p.groups; a.parts_per_group = p.parts_per_group; a.rows_per_part = p.rows_per_part;
+    a.alpha = d->alpha; a.beta = d->beta;
+    const RowShape s = row_shape(d->dtype, d->C);
+    hipStream_t st = (hipStream_t)stream;
+    {
+        const double n = (double)d->M * d->C;
+        ProfScope ps("norm_residual_bwd", n * e * ((pre ? 2 : 0) + (d_dy ? 1 : 0) + (a.z ? 1 : 0) + (d_dx ? 1 : 0) + (d_dz ? 1 : 0)), 1);
+        const bool bf = d->dtype == DSP_BF16;
+        int rc;
+        if (p.full) rc = p.fold ? (bf ? backward_t<bf16_t, true, true>(a, s, st, ps) : backward_t<float, true, true>(a, s, st, ps))
+                                : (bf ? backward_t<bf16_t, true, false>(a, s, st, ps) : backward_t<float, true, false>(a, s, st, ps));
+        else rc = p.fold ? (bf ? backward_t<bf16_t, false, true>(a, s, st, ps) : backward_t<float, false, true>(a, s, st, ps))
+                         : (bf ? backward_t<bf16_t, false, false>(a, s, st, ps) : backward_t<float, false, false>(a, s, st, ps));
+        DSP_TRY(rc);
+    }
+    if (!sums) return DSP_OK;
+    NormFinalArgs f;
+    f.partial = a.partial; f.gate = d_gate; f.post_gain = a.post_gain; f.post_bias = a.post_bias; f.dgate = d_dgate;
+    f.dpost_gain = d_dpost_gain; f.dpost_bias = d_dpost_bias; f.dpre_gain = d_dpre_gain; f.dpre_bias = d_dpre_bias;
+    f.gs = a.gs; f.C = d->C; f.parts = p.parts; f.groups = p.groups; f.parts_per_group = p.parts_per_group; f.full = p.full; f.fold = p.fold;
+    f.act = d->gate_act; f.gate_f16 = d->gate_dtype == DSP_BF16; f.gate_any = d->gate_rows > 0; f.beta = d->beta;
+    ProfScope ps("norm_residual_final", (double)p.bytes, 1);
+    DSP_LAUNCH(ps, norm_residual_final_kernel, dim3(ceil_div(d->C, 64)), dim3(64 * kFinalWaves), 0, st, f);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+}  // extern "C"

@@ -114,6 +114,8 @@ struct dsp_pipeline {
     std::vector<int32_t> p, m, q, P;  // P[k] = sum_{j<k} p_j
     float lr = 0, momentum = 0, wd = 0;
     int sum_s = 0;        // Eq. (3): 0 heavy ball, 1 Nesterov
+    bool adamw = false;   // the updates are AdamW's, with:
+    double adamw_lr = 0, beta1 = 0, beta2 = 0, adamw_eps = 0, adamw_wd = 0, max_norm = 0;
     int eager_ticks = 0;  // ticks to run unrecorded (the update after a step-size change rescales the velocity once)
     std::vector<hipStream_t> streams;
     std::vector<int32_t> spare;       // spare[k], k >= 1: entries beyond the minimum in the two queues between blocks k-1 and k
@@ -156,6 +158,7 @@ struct dsp_pipeline {
     // blocks of the same architecture re-runs each mini-batch as ordinary backpropagation at the
     // parameters every block held when it ran the forward pass of that mini-batch.
     dsp_pipeline* probe = nullptr;
+    bool is_probe = false;
     std::vector<float*> xsnap, gstash;      // per block: rings of parameter snapshots / DSP gradients, by mini-batch
     std::vector<int> xsnap_n, gstash_n;     // their entry counts
     int32_t* probe_labels = nullptr;        // labels of the last 1 + m_0 mini-batches
@@ -500,8 +503,27 @@ int dsp_pipeline_set_optimizer(dsp_pipeline* pl, float lr, float momentum, int32
     pl->momentum = momentum;
     pl->sum_s = s;
     pl->wd = weight_decay;
+    pl->adamw = false;
     drop_graphs(pl);  // recorded ticks hold the old constants
     pl->eager_ticks = 1;
+    return DSP_OK;
+}
+
+int dsp_pipeline_set_adamw(dsp_pipeline* pl, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm)
+{
+    DSP_REQUIRE(pl, DSP_EINVAL, "dsp_pipeline_set_adamw: null pipeline");
+    DSP_TRY(adamw_check_hyper(lr, beta1, beta2, eps, weight_decay, max_norm, "dsp_pipeline_set_adamw"));
+    for (dsp_block* b : pl->blocks)
+        DSP_REQUIRE(block_has_adamw(b), DSP_ESTATE, "dsp_pipeline_set_adamw: a block without dsp_block_set_adamw");
+    DSP_REQUIRE(!pl->is_probe, DSP_ESTATE, "dsp_pipeline_set_adamw: the pipeline is a gradient probe");
+    pl->adamw = true;
+    pl->adamw_lr = lr;
+    pl->beta1 = beta1;
+    pl->beta2 = beta2;
+    pl->adamw_eps = eps;
+    pl->adamw_wd = weight_decay;
+    pl->max_norm = max_norm;
+    drop_graphs(pl);  // recorded ticks hold the old constants
     return DSP_OK;
 }
 
@@ -513,7 +535,7 @@ int dsp_pipeline_attach_gradient_probe(dsp_pipeline* pl, dsp_pipeline* probe)
     DSP_REQUIRE(!pl->serial && pl->K >= 2, DSP_EINVAL, "dsp_pipeline_attach_gradient_probe: the pipeline has no staleness to measure");
     DSP_REQUIRE(probe->serial && probe->K == pl->K && probe->N == pl->N && probe->in_bytes == pl->in_bytes, DSP_EINVAL,
                 "dsp_pipeline_attach_gradient_probe: the probe must be an all-zero-schedule pipeline over the same K blocks");
-    DSP_REQUIRE(probe->lr == 0.f, DSP_EINVAL, "dsp_pipeline_attach_gradient_probe: the probe must have step size 0");
+    DSP_REQUIRE(probe->lr == 0.f && !probe->adamw, DSP_EINVAL, "dsp_pipeline_attach_gradient_probe: the probe must have step size 0");
     DSP_REQUIRE(probe->max_ticks >= pl->max_ticks, DSP_EINVAL, "dsp_pipeline_attach_gradient_probe: probe max_ticks too small");
     const int K = pl->K;
     for (int k = 0; k < K; ++k)
@@ -539,6 +561,7 @@ int dsp_pipeline_attach_gradient_probe(dsp_pipeline* pl, dsp_pipeline* probe)
     pl->probe_diff.assign(K, 0.0);
     pl->probe_ref.assign(K, 0.0);
     pl->probe = probe;
+    probe->is_probe = true;
     return DSP_OK;
 }
 
@@ -652,6 +675,8 @@ static int tick_step(dsp_pipeline* pl, int k, int64_t tau, hipStream_t st, bool 
 // and the update that consumes that gradient.
 static int tick_update(dsp_pipeline* pl, int k, hipStream_t st)
 {
+    if (pl->adamw)
+        return dsp_param_update_adamw(pl->blocks[k], pl->adamw_lr, pl->beta1, pl->beta2, pl->adamw_eps, pl->adamw_wd, pl->max_norm, st);
     return dsp_param_update_sum(pl->blocks[k], pl->lr, pl->momentum, pl->sum_s, pl->wd, st);
 }
 
