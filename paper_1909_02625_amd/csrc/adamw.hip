@@ -18,11 +18,15 @@ namespace dsp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kQuads = 4;                             // runs of four elements a thread has in flight
-constexpr int kChunk = kThreads * 4 * kQuads;         // elements of one workgroup: whole blocks of the 8-bit states
 constexpr int kStateBlock = 256;                      // elements that share a power of two: one wave, four elements a lane
-static_assert(kStateBlock == 64 * 4 && kChunk % kStateBlock == 0, "a wave's quad is a block of the 8-bit states");
-constexpr int kNormBlocks = 2048;                     // most partial sums of the gradient norm
+constexpr int kRow = kThreads * 4;                    // elements of a workgroup's quads side by side: four of those blocks
+static_assert(kStateBlock == 64 * 4, "a wave's quad is a block of the 8-bit states");
+// Quads a thread has in flight.
+constexpr int quads(int bits) { return bits == 8 ? 8 : 4; }
+constexpr int chunk_elems(int bits) { return kRow * quads(bits); }
+constexpr int kNormThreads = 1024;                    // workgroup of the gradient norm
+constexpr int kNormBlocks = 512;                      // most of its workgroups: two fill a compute unit
+constexpr int kNormRows = 4;                          // chunks it has in flight
 
 struct AdamwChunk {
     float* x;
@@ -30,7 +34,7 @@ struct AdamwChunk {
     bf16_t* copy;
     void *m, *v;
     uint8_t *m_exp, *v_exp;
-    int32_t n;       // 1 .. kChunk
+    int32_t n;       // 1 .. chunk_elems()
     int32_t flags;   // kDecay, kGradBf16
     uint32_t tensor;
     uint32_t first_lo, first_hi;  // element of its tensor that the chunk begins with
@@ -42,21 +46,33 @@ constexpr int kDecay = 1, kGradBf16 = 2;
 struct AdamwClock {
     int64_t steps;
     double p1, p2;  // products of b1 and b2 over the steps taken: b1^t, b2^t while they stay the same
-    uint32_t done_update, done_norm;
-    float clip;     // of the step at hand
-    int32_t skip;   // its gradient norm is no finite number: nothing is updated
+    uint32_t done;  // workgroups of the step at hand that have ended
+    uint32_t pad;
 };
 
 struct AdamwHyper {
     float lr, b1, r1, b2, r2, eps, wd;  // r = 1 - b, rounded once
     double d1, d2;
-    int clipped;
+    float max_norm;  // > 0: clipped
     uint32_t seed;
+    const double* partial;  // sums of squares of the gradients, or nullptr: no norm is wanted
+    int n_partial;
+    float* norm_out;
 };
 
-typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));        // (tensors may begin at any element: loads of 16
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));     //  bytes on addresses of their element's size)
+// (Tensors may begin at any element: loads of 16 bytes on addresses of their element's size, through global memory's pointers.)
+#define GLOBAL __attribute__((address_space(1)))
+typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32u __attribute__((aligned(1)));
+
+// What a step touches once: a model's parameters and states pass through the caches, nothing of them is there at the next step.
+template <typename V>
+__device__ inline V stream_load(const void* p) { return __builtin_nontemporal_load((const GLOBAL V*)p); }
+template <typename V>
+__device__ inline void stream_store(void* p, V v) { __builtin_nontemporal_store(v, (GLOBAL V*)p); }
 
 // A bijection of the 32-bit numbers that spreads each bit over all of them: two odd multipliers (the fractions of the golden
 // ratio and of the square root of two) between shifts.  The random bits of an element are a function of seed, step, tensor
@@ -84,31 +100,283 @@ __device__ inline uint32_t wave_max(uint32_t v)
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// |v| as ordered bits, 0 where it is no finite number (such an element keeps its code of its own and leaves its block alone)
-__device__ inline uint32_t finite_bits(float v)
-{
-    const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
-    return u < 0x7f800000u ? u : 0u;
-}
-
 struct Quad {
     float x[4], g[4], m[4], v[4];
+    uint32_t mc, vc;  // 8-bit codes of m and v
+    int me, ve;       // and their block's exponents
 };
+
+// Gradients i .. i + 3 of a chunk of n, 0 behind it.
+template <bool WHOLE>
+__device__ inline void load_gradient(const void* gp, bool g16, int i, int n, float (&g)[4])
+{
+    if (WHOLE || i + 4 <= n) {
+        if (g16) {
+            const u32x2 w = stream_load<u32x2>((const bf16_t*)gp + i);
+            g[0] = __uint_as_float(w.x << 16);
+            g[1] = __uint_as_float(w.x & 0xffff0000u);
+            g[2] = __uint_as_float(w.y << 16);
+            g[3] = __uint_as_float(w.y & 0xffff0000u);
+        } else {
+            const f32x4 w = stream_load<f32x4>((const float*)gp + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[e] = w[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            g[e] = i + e >= n ? 0.f : g16 ? __uint_as_float((uint32_t)((const GLOBAL uint16_t*)gp)[i + e] << 16) : ((const GLOBAL float*)gp)[i + e];
+    }
+}
+
+// Elements i .. i + 3 of a chunk (WHOLE: all of them are in it).
+template <int BITS, bool WHOLE>
+__device__ inline void load_quad(const AdamwChunk& c, int i, Quad& q)
+{
+    load_gradient<WHOLE>(c.g, (c.flags & kGradBf16) != 0, i, c.n, q.g);
+    if (BITS == 8) {
+        const int b = __builtin_amdgcn_readfirstlane(i / kStateBlock);
+        q.me = WHOLE || i < c.n ? ((const GLOBAL uint8_t*)c.m_exp)[b] : 0;
+        q.ve = WHOLE || i < c.n ? ((const GLOBAL uint8_t*)c.v_exp)[b] : 0;
+    }
+    if (WHOLE || i + 4 <= c.n) {
+        const f32x4 x = stream_load<f32x4>(c.x + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q.x[e] = x[e];
+        if (BITS == 32) {
+            const f32x4 m = stream_load<f32x4>((const float*)c.m + i), v = stream_load<f32x4>((const float*)c.v + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                q.m[e] = m[e];
+                q.v[e] = v[e];
+            }
+        } else {
+            q.mc = stream_load<u32u>((const uint8_t*)c.m + i);
+            q.vc = stream_load<u32u>((const uint8_t*)c.v + i);
+        }
+    } else {
+        q.mc = q.vc = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = i + e < c.n;
+            q.x[e] = in ? ((const GLOBAL float*)c.x)[i + e] : 0.f;
+            if (BITS == 32) {
+                q.m[e] = in ? ((const GLOBAL float*)c.m)[i + e] : 0.f;
+                q.v[e] = in ? ((const GLOBAL float*)c.v)[i + e] : 0.f;
+            } else {
+                q.mc |= in ? (uint32_t)((const GLOBAL uint8_t*)c.m)[i + e] << (8 * e) : 0u;
+                q.vc |= in ? (uint32_t)((const GLOBAL uint8_t*)c.v)[i + e] << (8 * e) : 0u;
+            }
+        }
+    }
+}
+
+template <int BITS, bool WHOLE>
+__device__ inline void store_quad(const AdamwChunk& c, int i, const Quad& q)
+{
+    if (WHOLE || i + 4 <= c.n) {
+        stream_store<f32x4>(c.x + i, f32x4{q.x[0], q.x[1], q.x[2], q.x[3]});
+        if (c.copy) stream_store<u32x2>(c.copy + i, u32x2{pack_bf16x2(q.x[0], q.x[1]), pack_bf16x2(q.x[2], q.x[3])});
+        if (BITS == 32) {
+            stream_store<f32x4>((float*)c.m + i, f32x4{q.m[0], q.m[1], q.m[2], q.m[3]});
+            stream_store<f32x4>((float*)c.v + i, f32x4{q.v[0], q.v[1], q.v[2], q.v[3]});
+        } else {
+            stream_store<u32u>((uint8_t*)c.m + i, q.mc);
+            stream_store<u32u>((uint8_t*)c.v + i, q.vc);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (i + e >= c.n) continue;
+            ((GLOBAL float*)c.x)[i + e] = q.x[e];
+            if (c.copy) ((GLOBAL uint16_t*)c.copy)[i + e] = float_to_bf16(q.x[e]).bits;
+            if (BITS == 32) {
+                ((GLOBAL float*)c.m)[i + e] = q.m[e];
+                ((GLOBAL float*)c.v)[i + e] = q.v[e];
+            } else {
+                ((GLOBAL uint8_t*)c.m)[i + e] = (uint8_t)(q.mc >> (8 * e));
+                ((GLOBAL uint8_t*)c.v)[i + e] = (uint8_t)(q.vc >> (8 * e));
+            }
+        }
+    }
+    if (BITS == 8 && threadIdx.x % 64 == 0 && (WHOLE || i < c.n)) {
+        ((GLOBAL uint8_t*)c.m_exp)[i / kStateBlock] = (uint8_t)q.me;
+        ((GLOBAL uint8_t*)c.v_exp)[i / kStateBlock] = (uint8_t)q.ve;
+    }
+}
 
 struct StepFactors {
     float c1, c2;  // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
-    float clip;
+    float clip, wd;
 };
 
-// One rounding per operation, as the formula reads: the same bits whatever the compiler would fuse.
-__device__ inline void adamw_element(float& x, float g, float& m, float& v, const AdamwHyper& h, const StepFactors& f, float wd)
+// The moments with one rounding per operation, as the formula reads: the same bits whatever the compiler would fuse.  With states
+// of 8 bits the root is the hardware's, within one unit of its last place, and 0 where v < 2^-126: the true root, below 1.1e-19, is
+// nothing beside an eps of at least 1e-15.  (270 M parameters: 934 -> 907 us with the norm.  32 bits wait for memory either way.)
+template <int BITS>
+__device__ inline void adamw_element(float& x, float g, float& m, float& v, const AdamwHyper& h, const StepFactors& f)
 {
+    {
 #pragma clang fp contract(off)
-    g = g * f.clip;
-    m = m * h.b1 + g * h.r1;
-    v = v * h.b2 + g * g * h.r2;
-    const float d = (m * f.c1) / (sqrtf(v) * f.c2 + h.eps);
-    x = x - h.lr * (d + wd * x);
+        g = g * f.clip;
+        m = m * h.b1 + g * h.r1;
+        v = v * h.b2 + g * g * h.r2;
+    }
+    const float d = (m * f.c1) * __builtin_amdgcn_rcpf((BITS == 8 ? __builtin_amdgcn_sqrtf(v) : sqrtf(v)) * f.c2 + h.eps);
+    x = x - h.lr * (d + f.wd * x);
+}
+
+__device__ inline void decode_quad(Quad& q)
+{
+    const f32x2 m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.mc, false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)q.mc, true);
+    const f32x2 v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)q.vc, false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)q.vc, true);
+    const float m[4] = {m0.x, m0.y, m1.x, m1.y}, v[4] = {v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        q.m[e] = ldexpf(m[e], q.me - 127);
+        q.v[e] = ldexpf(v[e], q.ve - 127);
+    }
+}
+
+// The moments of a wave's quads, one block of the 8-bit states, as codes.
+//
+// The block's power of two puts its largest m into [2^7, 2^8) and its largest v into [2^14, 2^15): half of the formats' range is
+// left, so that rounding up never leaves it.  A float's leading bits, its exponent moved to the format's, are the code; random
+// bits added below them round up with the probability of what they drop.  `at`: the first element's number, of its key's tensor.
+__device__ inline void encode_quad(Quad& q, uint32_t key, uint32_t at)
+{
+    uint32_t um[4], uv[4], am = 0u, av = 0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        um[e] = __float_as_uint(q.m[e]) << 1;  // without its sign
+        uv[e] = __float_as_uint(q.v[e]);
+        am = max(am, um[e]);
+        av = max(av, uv[e]);
+    }
+    am = wave_max(am);
+    av = wave_max(av);
+    const bool odd = am >= 0xff000000u || av >= 0x7f800000u;  // (the whole wave) something is no finite number
+    if (odd) {  // the exponents of what is
+        am = av = 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            am = max(am, um[e] < 0xff000000u ? um[e] : 0u);
+            av = max(av, uv[e] < 0x7f800000u ? uv[e] : 0u);
+        }
+        am = wave_max(am);
+        av = wave_max(av);
+    }
+    q.me = max((int)(am >> 24) - 7, 0);
+    q.ve = max((int)(av >> 23) - 14, 0);
+    uint32_t km[4], kv[4];  // the code in byte 2
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t r = mix32(key ^ (at + (uint32_t)e));
+        km[e] = (__float_as_uint(ldexpf(fabsf(q.m[e]), 7 - q.me)) >> 4) + (r & 0xffffu);
+        kv[e] = (__float_as_uint(ldexpf(q.v[e], 15 - q.ve)) >> 5) + (r >> 16);
+        km[e] = (km[e] & 0x7fffffu) | (__float_as_uint(q.m[e]) >> 8 & 0x800000u);
+    }
+    if (odd) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (um[e] >= 0xff000000u) km[e] |= 0x7f0000u;
+            if (uv[e] >= 0x7f800000u) kv[e] = 0x7f0000u;
+        }
+    }
+    auto bytes2 = [](const uint32_t (&k)[4]) -> uint32_t {
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(k[3], k[2], 0x0c0c0602u), __builtin_amdgcn_perm(k[1], k[0], 0x0c0c0602u), 0x05040100u);
+    };
+    q.mc = bytes2(km);
+    q.vc = bytes2(kv);
+    if ((q.vc - 0x01010101u) & ~q.vc & 0x80808080u) {  // v > 0 stays so: m over the root of a lost v has no bound
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if ((q.vc >> (8 * e) & 0xffu) == 0u && (uv[e] & 0x7fffffffu) != 0u) q.vc |= 1u << (8 * e);
+    }
+}
+
+template <int BITS>
+__device__ inline void update_quad(Quad& q, const AdamwHyper& h, const StepFactors& f, uint32_t key, uint32_t at)
+{
+    if (BITS == 8) decode_quad(q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) adamw_element<BITS>(q.x[e], q.g[e], q.m[e], q.v[e], h, f);
+    if (BITS == 8) encode_quad(q, key, at);
+}
+
+template <int WAVES>
+__device__ inline double block_sum(double v, double (&red)[WAVES])
+{
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = red[0];
+    for (int w = 1; w < WAVES; ++w) v += red[w];
+    return v;
+}
+
+// Partial sums of squares of all gradients.  Squares are exact in fp64 and every workgroup takes its chunks in order, as the
+// update kernel takes the partial sums: the same bits every time.
+template <int BITS>
+__global__ __launch_bounds__(kNormThreads) void adamw_norm_kernel(const AdamwChunk* __restrict__ chunks, int n_chunks,
+                                                                  double* __restrict__ partial)
+{
+    __shared__ double red[kNormThreads / 64];
+    double s = 0.0;
+    constexpr int kRuns = chunk_elems(BITS) * 4 / (kNormThreads * 16);  // of 16 bytes a thread, at most
+    for (int k = blockIdx.x; k < n_chunks; k += gridDim.x * kNormRows) {
+        u32x4 raw[kNormRows][kRuns];
+        int left[kNormRows][kRuns];  // elements of the run in the chunk
+        bool g16[kNormRows];
+#pragma unroll
+        for (int r = 0; r < kNormRows; ++r) {
+            const int at = k + r * (int)gridDim.x;
+            const AdamwChunk& c = chunks[min(at, n_chunks - 1)];
+            g16[r] = (c.flags & kGradBf16) != 0;
+            const int per = g16[r] ? 8 : 4, n = at < n_chunks ? c.n : 0;
+#pragma unroll
+            for (int u = 0; u < kRuns; ++u) {
+                const int i = (u * kNormThreads + (int)threadIdx.x) * per;
+                left[r][u] = n - i;
+                raw[r][u] = u32x4{0u, 0u, 0u, 0u};
+                if (left[r][u] >= per) {
+                    raw[r][u] = *(const GLOBAL u32x4*)((const char*)c.g + (size_t)i * (16 / per));
+                } else if (left[r][u] > 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (e >= left[r][u]) continue;
+                        if (g16[r]) raw[r][u][e / 2] |= (uint32_t)((const GLOBAL uint16_t*)c.g)[i + e] << (16 * (e & 1));
+                        else raw[r][u][e & 3] = ((const GLOBAL uint32_t*)c.g)[i + e];
+                    }
+                }
+            }
+        }
+        auto add = [&](float v) { s += (double)v * (double)v; };
+#pragma unroll
+        for (int r = 0; r < kNormRows; ++r)
+#pragma unroll
+            for (int u = 0; u < kRuns; ++u)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if (g16[r]) {
+                        add(__uint_as_float(raw[r][u][w] << 16));
+                        add(__uint_as_float(raw[r][u][w] & 0xffff0000u));
+                    } else {
+                        add(__uint_as_float(raw[r][u][w]));
+                    }
+                }
+    }
+    s = block_sum(s, red);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+// The root of their sum, in every thread of a workgroup.
+__device__ inline float gradient_norm(const double* __restrict__ partial, int n)
+{
+    __shared__ double red[kThreads / 64];
+    double s = 0.0;
+    for (int k = threadIdx.x; k < n; k += kThreads) s += partial[k];
+    return (float)sqrt(block_sum(s, red));
 }
 
 template <int BITS>
@@ -117,150 +385,50 @@ __global__ __launch_bounds__(kThreads) void adamw_update_kernel(const AdamwChunk
 {
     const AdamwChunk c = chunks[blockIdx.x];
     const int tid = threadIdx.x;
+    constexpr int kQuads = quads(BITS);
+    const bool whole = c.n == chunk_elems(BITS);
+    Quad q[kQuads];
+    if (whole) {  // on their way while the step's factors are formed
+#pragma unroll
+        for (int u = 0; u < kQuads; ++u) load_quad<BITS, true>(c, u * kRow + tid * 4, q[u]);
+    }
     const int64_t steps = clock->steps + 1;
-    const bool skip = h.clipped && clock->skip;
     StepFactors f;
-    f.c1 = (float)(1.0 / (1.0 - clock->p1 * h.d1));
-    f.c2 = (float)(1.0 / sqrt(1.0 - clock->p2 * h.d2));
-    f.clip = h.clipped ? clock->clip : 1.f;
-    const float wd = (c.flags & kDecay) ? h.wd : 0.f;
-    const bool g16 = (c.flags & kGradBf16) != 0;
-
-    if (!skip) {
-        Quad q[kQuads];
-        uint32_t mc[kQuads], vc[kQuads];
-        int me[kQuads], ve[kQuads];
-#pragma unroll
-        for (int u = 0; u < kQuads; ++u) {
-            const int i = u * kThreads * 4 + tid * 4;
-            if (BITS == 8) {
-                const int b = __builtin_amdgcn_readfirstlane(i / kStateBlock);
-                me[u] = i < c.n ? c.m_exp[b] : 0;
-                ve[u] = i < c.n ? c.v_exp[b] : 0;
-                mc[u] = vc[u] = 0u;
-            }
-            if (i + 4 <= c.n) {
-                *(f32x4*)q[u].x = *(const f32x4*)(c.x + i);
-                if (g16) {
-                    const u32x2 w = *(const u32x2*)((const bf16_t*)c.g + i);
-                    q[u].g[0] = __uint_as_float(w.x << 16);
-                    q[u].g[1] = __uint_as_float(w.x & 0xffff0000u);
-                    q[u].g[2] = __uint_as_float(w.y << 16);
-                    q[u].g[3] = __uint_as_float(w.y & 0xffff0000u);
-                } else {
-                    *(f32x4*)q[u].g = *(const f32x4*)((const float*)c.g + i);
-                }
-                if (BITS == 32) {
-                    *(f32x4*)q[u].m = *(const f32x4*)((const float*)c.m + i);
-                    *(f32x4*)q[u].v = *(const f32x4*)((const float*)c.v + i);
-                } else {
-                    mc[u] = *(const u32u*)((const uint8_t*)c.m + i);
-                    vc[u] = *(const u32u*)((const uint8_t*)c.v + i);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool in = i + e < c.n;
-                    q[u].x[e] = in ? c.x[i + e] : 0.f;
-                    q[u].g[e] = !in ? 0.f : g16 ? bf16_to_float(((const bf16_t*)c.g)[i + e]) : ((const float*)c.g)[i + e];
-                    if (BITS == 32) {
-                        q[u].m[e] = in ? ((const float*)c.m)[i + e] : 0.f;
-                        q[u].v[e] = in ? ((const float*)c.v)[i + e] : 0.f;
-                    } else {
-                        mc[u] |= in ? (uint32_t)((const uint8_t*)c.m)[i + e] << (8 * e) : 0u;
-                        vc[u] |= in ? (uint32_t)((const uint8_t*)c.v)[i + e] << (8 * e) : 0u;
-                    }
-                }
-            }
+    f.c1 = 1.f / (float)(1.0 - clock->p1 * h.d1);
+    f.c2 = 1.f / sqrtf((float)(1.0 - clock->p2 * h.d2));
+    f.clip = 1.f;
+    f.wd = (c.flags & kDecay) ? h.wd : 0.f;
+    bool skip = false;
+    if (h.partial && (h.max_norm > 0.f || blockIdx.x == 0)) {
+        const float norm = gradient_norm(h.partial, h.n_partial);
+        if (h.max_norm > 0.f) {
+            skip = !(norm < INFINITY);
+            if (norm > h.max_norm) f.clip = h.max_norm / norm;
         }
-        // (uniform over the workgroup)
-        const uint32_t key = BITS == 8 ? mix32(mix32(mix32(h.seed ^ (uint32_t)steps) ^ c.tensor) ^ c.first_hi) : 0u;
+        if (h.norm_out && blockIdx.x == 0 && tid == 0) *h.norm_out = norm;
+    }
+    const uint32_t key = BITS == 8 ? mix32(mix32(mix32(h.seed ^ (uint32_t)steps) ^ c.tensor) ^ c.first_hi) : 0u;
+    if (skip) {
+    } else if (whole) {
 #pragma unroll
         for (int u = 0; u < kQuads; ++u) {
-            const int i = u * kThreads * 4 + tid * 4;
-            if (BITS == 8) {
-                typedef float f32x2 __attribute__((ext_vector_type(2)));
-                const f32x2 m0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[u], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mc[u], true);
-                const f32x2 v0 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vc[u], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8((int)vc[u], true);
-                const float m[4] = {m0.x, m0.y, m1.x, m1.y}, v[4] = {v0.x, v0.y, v1.x, v1.y};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    q[u].m[e] = ldexpf(m[e], me[u] - 127);
-                    q[u].v[e] = ldexpf(v[e], ve[u] - 127);
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) adamw_element(q[u].x[e], q[u].g[e], q[u].m[e], q[u].v[e], h, f, wd);
-            if (BITS == 8) {
-                // The block's power of two puts its largest m into [2^7, 2^8) and its largest v into [2^14, 2^15): half of the
-                // formats' range is left, so that rounding up never leaves it.  A float's leading bits, its exponent moved to
-                // the format's, are the code; random bits added below them round up with the probability of what they drop.
-                uint32_t am = 0u, av = 0u;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    am = max(am, finite_bits(q[u].m[e]));
-                    av = max(av, finite_bits(q[u].v[e]));
-                }
-                const int em = max((int)(wave_max(am) >> 23) - 7, 0), ev = max((int)(wave_max(av) >> 23) - 14, 0);
-                uint32_t cm = 0u, cv = 0u;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t r = mix32(key ^ (c.first_lo + (uint32_t)(i + e)));
-                    const uint32_t um = __float_as_uint(q[u].m[e]), uv = __float_as_uint(q[u].v[e]);
-                    uint32_t km = (__float_as_uint(ldexpf(__uint_as_float(um & 0x7fffffffu), 7 - em)) + ((r & 0xffffu) << 4)) >> 20;
-                    uint32_t kv = (__float_as_uint(ldexpf(__uint_as_float(uv & 0x7fffffffu), 15 - ev)) + (r >> 16 << 5)) >> 21;
-                    if (kv == 0u && (uv & 0x7fffffffu) != 0u) kv = 1u;  // v > 0 stays so: m over the root of a lost v has no bound
-                    if ((um & 0x7f800000u) == 0x7f800000u) km = 0x7fu;
-                    if ((uv & 0x7f800000u) == 0x7f800000u) kv = 0x7fu;
-                    cm |= (km | (um >> 24 & 0x80u)) << (8 * e);
-                    cv |= kv << (8 * e);
-                }
-                mc[u] = cm;
-                vc[u] = cv;
-                me[u] = em;
-                ve[u] = ev;
-            }
+            const int i = u * kRow + tid * 4;
+            update_quad<BITS>(q[u], h, f, key, c.first_lo + (uint32_t)i);
+            store_quad<BITS, true>(c, i, q[u]);
         }
-#pragma unroll
-        for (int u = 0; u < kQuads; ++u) {
-            const int i = u * kThreads * 4 + tid * 4;
-            if (i + 4 <= c.n) {
-                *(f32x4*)(c.x + i) = *(const f32x4*)q[u].x;
-                if (c.copy)
-                    *(u32x2*)(c.copy + i) = u32x2{pack_bf16x2(q[u].x[0], q[u].x[1]), pack_bf16x2(q[u].x[2], q[u].x[3])};
-                if (BITS == 32) {
-                    *(f32x4*)((float*)c.m + i) = *(const f32x4*)q[u].m;
-                    *(f32x4*)((float*)c.v + i) = *(const f32x4*)q[u].v;
-                } else {
-                    *(u32u*)((uint8_t*)c.m + i) = mc[u];
-                    *(u32u*)((uint8_t*)c.v + i) = vc[u];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (i + e >= c.n) continue;
-                    c.x[i + e] = q[u].x[e];
-                    if (c.copy) c.copy[i + e] = float_to_bf16(q[u].x[e]);
-                    if (BITS == 32) {
-                        ((float*)c.m)[i + e] = q[u].m[e];
-                        ((float*)c.v)[i + e] = q[u].v[e];
-                    } else {
-                        ((uint8_t*)c.m)[i + e] = (uint8_t)(mc[u] >> (8 * e));
-                        ((uint8_t*)c.v)[i + e] = (uint8_t)(vc[u] >> (8 * e));
-                    }
-                }
-            }
-            if (BITS == 8 && tid % 64 == 0 && i < c.n) {
-                c.m_exp[i / kStateBlock] = (uint8_t)me[u];
-                c.v_exp[i / kStateBlock] = (uint8_t)ve[u];
-            }
+    } else {
+#pragma unroll 1
+        for (int i = tid * 4; i - tid * 4 < c.n; i += kRow) {
+            load_quad<BITS, false>(c, i, q[0]);
+            update_quad<BITS>(q[0], h, f, key, c.first_lo + (uint32_t)i);
+            store_quad<BITS, false>(c, i, q[0]);
         }
     }
 
     // The workgroup that ends last counts the step: every other one has read the clock by then.
     __syncthreads();
-    if (tid == 0 && atomicAdd(&clock->done_update, 1u) == gridDim.x - 1) {
-        clock->done_update = 0u;
+    if (tid == 0 && atomicAdd(&clock->done, 1u) == gridDim.x - 1) {
+        clock->done = 0u;
         if (!skip) {
             clock->steps = steps;
             clock->p1 *= h.d1;
@@ -269,88 +437,14 @@ __global__ __launch_bounds__(kThreads) void adamw_update_kernel(const AdamwChunk
     }
 }
 
-__device__ inline double wave_sum(double v)
-{
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
-
-// Sum of the four waves' values, in thread 0.
-__device__ inline double block_sum(double v, double (&red)[kThreads / 64])
-{
-    v = wave_sum(v);
-    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
-    __syncthreads();
-    return red[0] + red[1] + red[2] + red[3];
-}
-
-// Squares are exact in fp64 and every workgroup takes its chunks in order, as the last one takes the partial sums: the same
-// bits every time.
-__global__ __launch_bounds__(kThreads) void adamw_norm_kernel(const AdamwChunk* __restrict__ chunks, int n_chunks,
-                                                              AdamwClock* __restrict__ clock, double* __restrict__ partial,
-                                                              float max_norm, float* __restrict__ norm_out)
-{
-    __shared__ double red[2][kThreads / 64];
-    __shared__ int last;
-    const int tid = threadIdx.x;
-    double s = 0.0;
-    for (int k = blockIdx.x; k < n_chunks; k += gridDim.x) {
-        const void* gp = chunks[k].g;
-        const int n = chunks[k].n;
-        const bool g16 = (chunks[k].flags & kGradBf16) != 0;
-        float g[kQuads][4];
-#pragma unroll
-        for (int u = 0; u < kQuads; ++u) {
-            const int i = u * kThreads * 4 + tid * 4;
-            if (i + 4 <= n) {
-                if (g16) {
-                    const u32x2 w = *(const u32x2*)((const bf16_t*)gp + i);
-                    g[u][0] = __uint_as_float(w.x << 16);
-                    g[u][1] = __uint_as_float(w.x & 0xffff0000u);
-                    g[u][2] = __uint_as_float(w.y << 16);
-                    g[u][3] = __uint_as_float(w.y & 0xffff0000u);
-                } else {
-                    *(f32x4*)g[u] = *(const f32x4*)((const float*)gp + i);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    g[u][e] = i + e >= n ? 0.f : g16 ? bf16_to_float(((const bf16_t*)gp)[i + e]) : ((const float*)gp)[i + e];
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kQuads; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s += (double)g[u][e] * (double)g[u][e];
-    }
-    s = block_sum(s, red[0]);
-    if (tid == 0) {
-        __hip_atomic_store(&partial[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(&clock->done_norm, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    s = 0.0;
-    for (int k = tid; k < (int)gridDim.x; k += kThreads) s += __hip_atomic_load(&partial[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s = block_sum(s, red[1]);
-    if (tid == 0) {
-        const float norm = (float)sqrt(s);
-        const bool finite = norm < INFINITY;
-        clock->done_norm = 0u;
-        clock->clip = max_norm > 0.f && max_norm < norm ? max_norm / norm : 1.f;
-        clock->skip = finite ? 0 : 1;
-        if (norm_out) *norm_out = norm;
-    }
-}
-
 }  // namespace
 
 int adamw_check_hyper(double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm, const char* who)
 {
     auto in = [](double v, double lo) { return v >= lo && (float)v < INFINITY; };
-    DSP_REQUIRE(in(lr, 0.0) && beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && in(eps, 0.0) && (float)eps > 0.f &&
-                    in(weight_decay, 0.0) && in(max_norm, 0.0),
-                DSP_EINVAL, "%s: lr, weight_decay, max_norm >= 0, 0 <= beta < 1 and eps > 0 are wanted", who);
+    DSP_REQUIRE(in(lr, 0.0) && beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && in(eps, 1e-15) && in(weight_decay, 0.0) &&
+                    in(max_norm, 0.0) && (max_norm == 0.0 || (float)max_norm > 0.f),
+                DSP_EINVAL, "%s: lr, weight_decay, max_norm >= 0, 0 <= beta < 1 and eps >= 1e-15 are wanted", who);
     return DSP_OK;
 }
 
@@ -384,13 +478,12 @@ int adamw_upload(dsp_adamw* o, const std::vector<AdamwChunk>& chunks)
     DSP_HIP(hipGetDevice(&o->device));
     DSP_REQUIRE(hipMalloc((void**)&o->clock, sizeof(AdamwClock)) == hipSuccess &&
                     hipMalloc((void**)&o->partial, kNormBlocks * sizeof(double)) == hipSuccess &&
-                    hipMalloc((void**)&o->chunks, std::max<size_t>(1, chunks.size()) * sizeof(AdamwChunk)) == hipSuccess,
+                    hipMalloc((void**)&o->chunks, chunks.size() * sizeof(AdamwChunk)) == hipSuccess,
                 DSP_ENOMEM, "dsp_adamw_init: out of device memory");
     AdamwClock clock = {};
     clock.p1 = clock.p2 = 1.0;
-    clock.clip = 1.f;
     DSP_HIP(hipMemcpy(o->clock, &clock, sizeof(clock), hipMemcpyHostToDevice));
-    if (!chunks.empty()) DSP_HIP(hipMemcpy(o->chunks, chunks.data(), chunks.size() * sizeof(AdamwChunk), hipMemcpyHostToDevice));
+    DSP_HIP(hipMemcpy(o->chunks, chunks.data(), chunks.size() * sizeof(AdamwChunk), hipMemcpyHostToDevice));
     return DSP_OK;
 }
 
@@ -430,7 +523,7 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
                         (uintptr_t)t.d_m % ss == 0 && (uintptr_t)t.d_v % ss == 0,
                     DSP_EINVAL, "dsp_adamw_init: a buffer of tensor %d is not aligned to its elements", (int)j);
         DSP_REQUIRE(t.n < (1ll << 40), DSP_EINVAL, "dsp_adamw_init: tensor %d is too large", (int)j);
-        const size_t n = (size_t)t.n, blocks = (n + kStateBlock - 1) / kStateBlock;
+        const size_t n = (size_t)t.n, blocks = (n + kStateBlock - 1) / kStateBlock, chunk = chunk_elems(state_bits);
         auto range = [&](const void* p, size_t bytes, bool written) {
             if (p) ranges.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written});
         };
@@ -443,7 +536,7 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
             range(t.d_m_exp, blocks, true);
             range(t.d_v_exp, blocks, true);
         }
-        for (size_t at = 0; at < n; at += kChunk) {
+        for (size_t at = 0; at < n; at += chunk) {
             AdamwChunk c = {};
             c.x = t.d_param + at;
             c.g = (const char*)t.d_grad + gs * at;
@@ -454,7 +547,7 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
                 c.m_exp = t.d_m_exp + at / kStateBlock;
                 c.v_exp = t.d_v_exp + at / kStateBlock;
             }
-            c.n = (int32_t)std::min<size_t>(kChunk, n - at);
+            c.n = (int32_t)std::min(chunk, n - at);
             c.flags = (t.decay ? kDecay : 0) | (t.grad_dtype == DSP_BF16 ? kGradBf16 : 0);
             c.tensor = (uint32_t)j;
             c.first_lo = (uint32_t)at;
@@ -465,7 +558,8 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
         o->grad_bytes += (double)gs * n;
         o->update_bytes += (double)n * (8 + gs + (t.d_copy ? 2 : 0)) + (state_bits == 8 ? 4.0 * n + 4.0 * blocks : 16.0 * n);
     }
-    DSP_REQUIRE(chunks.size() < (size_t)1 << 31, DSP_EINVAL, "dsp_adamw_init: too many elements");
+    if (chunks.empty()) chunks.push_back(AdamwChunk{});  // (nothing but a step to count)
+    DSP_REQUIRE(chunks.size() < (size_t)1 << 29, DSP_EINVAL, "dsp_adamw_init: too many elements");
     DSP_REQUIRE(!ranges_clash(ranges), DSP_EINVAL, "dsp_adamw_init: a buffer that is written overlaps another one (the same tensor twice?)");
     o->n_chunks = (int)chunks.size();
     return adamw_upload(o, chunks);
@@ -475,7 +569,7 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
 
 namespace dsp {
 
-static_assert(offsetof(AdamwClock, done_update) == kAdamwClockBytes, "steps, p1, p2 lead the clock");
+static_assert(offsetof(AdamwClock, done) == kAdamwClockBytes, "steps, p1, p2 lead the clock");
 
 int adamw_clock_read(dsp_adamw* o, void* h_dst)
 {
@@ -534,15 +628,14 @@ int dsp_adamw_step(dsp_adamw* o, double lr, double beta1, double beta2, double e
     DSP_HIP(hipGetDevice(&device));
     DSP_REQUIRE(device == o->device, DSP_EINVAL, "dsp_adamw_step: the object belongs to device %d, the current one is %d", o->device, device);
     hipStream_t st = (hipStream_t)stream;
-    const bool clipped = max_norm > 0.0;
-    if (clipped || d_norm) {
+    const bool norm = max_norm > 0.0 || d_norm;
+    const int norm_blocks = std::min(o->n_chunks, kNormBlocks);
+    if (norm) {
         ProfScope ps("adamw_norm", o->grad_bytes, 1);
-        const int grid = std::max(1, std::min(o->n_chunks, kNormBlocks));
-        DSP_LAUNCH(ps, adamw_norm_kernel, dim3(grid), dim3(kThreads), 0, st, o->chunks, o->n_chunks, o->clock, o->partial,
-                   (float)max_norm, d_norm);
+        if (o->bits == 8) DSP_LAUNCH(ps, adamw_norm_kernel<8>, dim3(norm_blocks), dim3(kNormThreads), 0, st, o->chunks, o->n_chunks, o->partial);
+        else DSP_LAUNCH(ps, adamw_norm_kernel<32>, dim3(norm_blocks), dim3(kNormThreads), 0, st, o->chunks, o->n_chunks, o->partial);
         DSP_HIP(hipGetLastError());
     }
-    if (o->n_chunks == 0) return DSP_OK;
     AdamwHyper h;
     h.lr = (float)lr;
     h.b1 = (float)beta1;
@@ -553,8 +646,11 @@ int dsp_adamw_step(dsp_adamw* o, double lr, double beta1, double beta2, double e
     h.wd = (float)weight_decay;
     h.d1 = beta1;
     h.d2 = beta2;
-    h.clipped = clipped ? 1 : 0;
+    h.max_norm = (float)max_norm;
     h.seed = o->seed;
+    h.partial = norm ? o->partial : nullptr;
+    h.n_partial = norm_blocks;
+    h.norm_out = d_norm;
     ProfScope ps(o->bits == 8 ? "adamw_update<8>" : "adamw_update<32>", o->update_bytes, 1);
     if (o->bits == 8)
         DSP_LAUNCH(ps, adamw_update_kernel<8>, dim3(o->n_chunks), dim3(kThreads), 0, st, o->chunks, o->clock, h);
@@ -581,7 +677,6 @@ int dsp_adamw_set_steps(dsp_adamw* o, int64_t steps, double beta1, double beta2)
     c.steps = steps;
     c.p1 = pow(beta1, (double)steps);
     c.p2 = pow(beta2, (double)steps);
-    c.clip = 1.f;
     DSP_HIP(hipMemcpy(o->clock, &c, sizeof(c), hipMemcpyHostToDevice));
     return DSP_OK;
 }

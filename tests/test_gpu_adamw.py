@@ -239,6 +239,31 @@ def test_the_same_call_gives_the_same_bits_on_another_stream():
             assert torch.equal(p[name], q[name])
 
 
+def test_hyperparameters_that_are_refused():
+    m = Model([10], 32, torch.float32)
+    nan, inf = float("nan"), float("inf")
+    for bad in ({"lr": -1e-3}, {"lr": nan}, {"lr": inf}, {"beta1": 1.0}, {"beta1": -0.1}, {"beta2": 1.0}, {"beta2": nan}, {"eps": 0.0}, {"eps": 1e-16},
+                {"eps": nan}, {"weight_decay": -1.0}, {"weight_decay": inf}, {"max_norm": -1.0}, {"max_norm": nan}, {"max_norm": 1e-60}):
+        with pytest.raises(D.DSPError) as e:
+            D.dsp_adamw_step(m.opt, **{**HYPER, **bad})
+        assert e.value.status == 1
+    for steps, b1 in ((-1, 0.9), (3, 1.0)):
+        with pytest.raises(D.DSPError):
+            D.dsp_adamw_set_steps(m.opt, steps, b1)
+    assert D.dsp_adamw_get_steps(m.opt) == 0
+    D.dsp_adamw_step(m.opt, **HYPER)
+    m.check(1)
+
+
+def test_tensors_of_no_elements():
+    z = lambda n: torch.zeros(n, device="cuda")  # noqa: E731
+    o = D.dsp_adamw_init([{"param": z(0), "grad": z(0), "m": z(0), "v": z(0)}])
+    norm = torch.ones(1, device="cuda")
+    D.dsp_adamw_step(o, 1e-3, d_norm=norm)
+    assert float(norm) == 0 and D.dsp_adamw_get_steps(o) == 1
+    D.dsp_adamw_destroy(o)
+
+
 def test_betas_that_change():
     """beta^t is the product over the steps taken."""
     n = 512
