@@ -12,7 +12,8 @@ namespace {
 
 constexpr int kMaxC = 16384;
 constexpr int kSubThreads = 256;  // workgroup of the kernels whose rows are shorter than a wave
-constexpr int kParts = 1024;      // workgroups of the backward kernel = rows of partial sums
+constexpr int kBackWaves = 8;     // waves a workgroup of the backward kernel fills with rows side by side
+constexpr int kParts = 512;       // most workgroups of the backward kernel = rows of partial sums
 
 struct NormArgs {
     const void *x, *z, *gate;
@@ -21,6 +22,7 @@ struct NormArgs {
     float *post_stats, *pre_stats;
     int64_t xs, zs, ys, hs, gs;
     int M, C, post, pre, act, gate_f32, gate_rows;  // gate_rows = 0: no gate
+    int waves;                                      // of a row
     float alpha, beta, eps;
 };
 
@@ -30,18 +32,19 @@ struct NormBackArgs {
     void *dx, *dz, *dgate;
     float* partial;  // [P1, S1 (, P2, S2)][parts][C]
     int64_t xs, zs, ys, hs, gs;
-    int M, C, post, pre, act, gate_f32, gate_rows;
-    int parts, groups, parts_per_group, rows_per_part;  // fold: rows_per_part = groups of a workgroup
+    int M, C, post, pre, act, gate_f32, gate_rows, waves;
+    int parts, groups, parts_per_group, rows_per_part;  // fold: rows_per_part = rows of the gate of a workgroup
     float alpha, beta;
 };
 
 // Runs of 16 bytes on addresses of the element's size: rows may begin at any element (an odd C, a stride of the caller's).
+typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
 struct RowIO;
 template <>
 struct RowIO<float> {
     static constexpr int VW = 4;
-    typedef float Raw __attribute__((ext_vector_type(4), aligned(4)));
+    typedef F4 Raw;
     __device__ static inline void unpack(const Raw& r, float (&v)[VW])
     {
 #pragma unroll
@@ -66,47 +69,69 @@ struct RowIO<bf16_t> {
         return Raw{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
     }
 };
-
-// VW elements from column c on; those behind the row are `rest`.
 template <typename T>
-__device__ inline void load_run(const T* row, int c, int C, float (&v)[RowIO<T>::VW], float rest = 0.f)
+using Raw = typename RowIO<T>::Raw;
+
+// VW elements from column c on, as they lie in memory; those behind the row are 0.
+template <typename T>
+__device__ inline Raw<T> load_raw(const T* row, int c, int C)
 {
     constexpr int VW = RowIO<T>::VW;
-    if (c + VW <= C) {
-        RowIO<T>::unpack(*(const typename RowIO<T>::Raw*)(row + c), v);
-    } else {
+    if (c + VW <= C) return *(const Raw<T>*)(row + c);
+    float v[VW] = {};
+    if (c < C) {
 #pragma unroll
-        for (int e = 0; e < VW; ++e) v[e] = c + e < C ? to_float<T>(row[c + e]) : rest;
+        for (int e = 0; e < VW; ++e) v[e] = c + e < C ? to_float<T>(row[c + e]) : 0.f;
     }
+    return RowIO<T>::pack(v);
 }
 template <typename T>
 __device__ inline void store_run(T* row, int c, int C, const float (&v)[RowIO<T>::VW])
 {
     constexpr int VW = RowIO<T>::VW;
     if (c + VW <= C) {
-        *(typename RowIO<T>::Raw*)(row + c) = RowIO<T>::pack(v);
-    } else {
+        *(Raw<T>*)(row + c) = RowIO<T>::pack(v);
+    } else if (c < C) {
 #pragma unroll
         for (int e = 0; e < VW; ++e)
             if (c + e < C) row[c + e] = from_float<T>(v[e]);
     }
 }
-// A vector of floats (gains, biases) at the columns of a run of N elements; `rest` where there is no vector or no column.
+// A vector of floats (gains, biases) at the columns of a run: `rest` where there is no vector, 0 behind the row.  (With gains of
+// 0 there, whatever else a thread holds behind the row stays out of every sum.)
 template <int N>
 __device__ inline void load_vector(const float* p, int c, int C, float (&v)[N], float rest)
 {
+    if (p && c + N <= C) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = p && c + e < C ? p[c + e] : rest;
+        for (int e = 0; e < N; e += 4) {
+            const F4 f = *(const F4*)(p + c + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[e + i] = f[i];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = c + e >= C ? 0.f : p ? p[c + e] : rest;
+    }
+}
+template <int N>
+__device__ inline void store_vector(float* p, int c, int C, const float (&v)[N])
+{
+    if (c + N <= C) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) *(F4*)(p + c + e) = F4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    } else if (c < C) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (c + e < C) p[c + e] = v[e];
+    }
 }
 // A run of one row of the gate, as floats.
 template <typename T>
 __device__ inline void load_gate(const void* gate, int gate_f32, int64_t at, int c, int C, float (&v)[RowIO<T>::VW])
 {
-    if (sizeof(T) == 4 || !gate_f32) {
-        load_run<T>((const T*)gate + at, c, C, v);
-    } else {
-        load_vector(((const float*)gate) + at, c, C, v, 0.f);
-    }
+    if (sizeof(T) == 4 || !gate_f32) RowIO<T>::unpack(load_raw<T>((const T*)gate + at, c, C), v);
+    else load_vector((const float*)gate + at, c, C, v, 0.f);
 }
 
 __device__ inline float gate_act(int act, float g)
@@ -121,12 +146,38 @@ __device__ inline float gate_slope(int act, float g)
     return (act == DSP_GATE_SIGMOID ? 1.f : 4.f) * e * q * q;
 }
 
-// Sums of K values over the TPR lanes of a row (TPR = 0: over the workgroup, through `red`, one barrier), in every lane.  The
-// two halves of `red` are used in turn: what a half held has been read by everyone once the other half's barrier is passed.
+// How a workgroup's threads hold rows: TPR lanes a row and 256 / TPR rows, or (TPR = 0) `waves` waves a row and as many rows as the
+// workgroup has waves for.
+template <int TPR>
+struct Place {
+    int t, threads;  // thread of its row, threads of a row
+    int slot, slots;
+    __device__ inline Place(int waves)
+    {
+        const int tid = threadIdx.x;
+        if (TPR) {
+            t = tid % (TPR ? TPR : 1);
+            threads = TPR;
+            slot = tid / (TPR ? TPR : 1);
+            slots = kSubThreads / (TPR ? TPR : 1);
+        } else {
+            threads = 64 * waves;
+            slot = __builtin_amdgcn_readfirstlane(tid / threads);
+            t = tid - slot * threads;
+            slots = blockDim.x / threads;
+        }
+    }
+};
+
+// Sums of K values over the threads of a row, in all of them (TPR = 0 and several waves: through `red`, one barrier of the
+// workgroup).  The two halves of `red` are used in turn: what a half held has been read by everyone once the other half's barrier
+// is passed.
 template <int TPR, int K>
 struct RowSum {
     float (*red)[16][K];
-    int turn = 0;
+    int waves, first;  // of the row, of the workgroup's waves
+    int turn;
+    __device__ inline RowSum(float (*r)[16][K], int w, int slot) : red(r), waves(w), first(slot * w), turn(0) {}
     __device__ inline void operator()(float (&v)[K])
     {
         constexpr int LANES = TPR ? TPR : 64;
@@ -143,18 +194,16 @@ struct RowSum {
         for (int off = 16; off < LANES; off *= 2)
 #pragma unroll
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], off, 64);
-        if (TPR == 0) {
-            const int waves = blockDim.x / 64;
-            if (waves == 1) return;
+        if (TPR == 0 && waves > 1) {
             if (threadIdx.x % 64 == 0)
 #pragma unroll
                 for (int k = 0; k < K; ++k) red[turn][threadIdx.x / 64][k] = v[k];
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < K; ++k) v[k] = 0.f;
-            for (int w = 0; w < waves; ++w)
+            for (int k = 0; k < K; ++k) v[k] = red[turn][first][k];
+            for (int w = 1; w < waves; ++w)
 #pragma unroll
-                for (int k = 0; k < K; ++k) v[k] += red[turn][w][k];
+                for (int k = 0; k < K; ++k) v[k] += red[turn][first + w][k];
             turn ^= 1;
         }
     }
@@ -163,7 +212,7 @@ struct RowSum {
 // Mean (layer norm; else 0) and 1 / deviation of a row whose runs a thread holds; columns behind the row hold 0.  Centred
 // before it is squared: a row far from zero keeps its variance.
 template <int TPR, int NV, int VW>
-__device__ inline void row_stats(int kind, const float (&a)[NV][VW], const bool (&in)[NV][VW], float inv_c, float eps, RowSum<TPR, 1>& sum,
+__device__ inline void row_stats(int kind, const float (&a)[NV][VW], const int (&c)[NV], int C, float inv_c, float eps, RowSum<TPR, 1>& sum,
                                  float& mean, float& inv)
 {
     mean = 0.f;
@@ -179,62 +228,79 @@ __device__ inline void row_stats(int kind, const float (&a)[NV][VW], const bool 
     }
     s[0] = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+        const float centre = c[k] + VW <= C ? mean : 0.f;
+        if (c[k] + VW <= C || c[k] >= C || kind != DSP_NORM_LAYER) {
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-            const float d = in[k][e] ? a[k][e] - mean : 0.f;
-            s[0] += d * d;
+            for (int e = 0; e < VW; ++e) s[0] += (a[k][e] - centre) * (a[k][e] - centre);
+        } else {  // the row ends inside the run
+#pragma unroll
+            for (int e = 0; e < VW; ++e) s[0] += c[k] + e < C ? (a[k][e] - mean) * (a[k][e] - mean) : 0.f;
         }
+    }
     sum(s);
     inv = 1.f / sqrtf(s[0] * inv_c + eps);
 }
 
-// TPR lanes a row and 256 / TPR rows a workgroup, or (TPR = 0) a row a workgroup of whole waves; NV runs a thread.
+// A workgroup goes through the rows with its grid; the next row's runs are on their way while this one's are summed.
 template <typename T, int TPR, int NV, int MAXT>
 __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 {
     constexpr int VW = RowIO<T>::VW;
     __shared__ float red[2][16][1];
-    RowSum<TPR, 1> sum{red};
-    const int tid = threadIdx.x;
-    const int t = TPR ? tid % (TPR ? TPR : 1) : tid, threads = TPR ? TPR : (int)blockDim.x;
-    const int rows = TPR ? kSubThreads / (TPR ? TPR : 1) : 1, slot = TPR ? tid / (TPR ? TPR : 1) : 0;
+    const Place<TPR> at(a.waves);
+    RowSum<TPR, 1> sum(red, a.waves, at.slot);
     const float inv_c = 1.f / (float)a.C;
-    const bool row_gate = a.gate_rows > 0 && a.gate_rows < a.M;
+    const bool row_gate = a.gate_rows > 0 && a.gate_rows < a.M, branch = a.z != nullptr;
+    const int64_t step = (int64_t)gridDim.x * at.slots;
     int c[NV];
-    bool in[NV][VW];
-    float gpost[NV][VW], gpre[NV][VW], w[NV][VW];  // w: beta, times the gate where one row of it serves all
+#pragma unroll
+    for (int k = 0; k < NV; ++k) c[k] = (at.t + k * at.threads) * VW;
+
+    Raw<T> rx[NV], rz[NV];
+    auto fetch = [&](int64_t row) {
+        row = min(row, (int64_t)a.M - 1);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C);
+            if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
+        }
+    };
+    int64_t base = (int64_t)blockIdx.x * at.slots;
+    if (base >= a.M) return;
+    fetch(base + at.slot);
+
+    float gpost[NV][VW], bpost[NV][VW], gpre[NV][VW], bpre[NV][VW], w[NV][VW];  // w: beta, times the gate where one row of it serves all
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        c[k] = (t + k * threads) * VW;
-#pragma unroll
-        for (int e = 0; e < VW; ++e) in[k][e] = c[k] + e < a.C;
         load_vector(a.post_gain, c[k], a.C, gpost[k], 1.f);
+        load_vector(a.post_bias, c[k], a.C, bpost[k], 0.f);
         load_vector(a.pre_gain, c[k], a.C, gpre[k], 1.f);
+        load_vector(a.pre_bias, c[k], a.C, bpre[k], 0.f);
         if (a.gate_rows && !row_gate) load_gate<T>(a.gate, a.gate_f32, 0, c[k], a.C, w[k]);
 #pragma unroll
         for (int e = 0; e < VW; ++e) w[k][e] = a.gate_rows && !row_gate ? a.beta * gate_act(a.act, w[k][e]) : a.beta;
     }
-    for (int64_t base = (int64_t)blockIdx.x * rows; base < a.M; base += (int64_t)gridDim.x * rows) {
-        const bool live = base + slot < a.M;
-        const int64_t row = live ? base + slot : a.M - 1;
+    for (; base < a.M; base += step) {
+        const int64_t row = base + at.slot;
+        const bool live = row < a.M;
         float z[NV][VW], y[NV][VW];
         float mean = 0.f, inv = 1.f;
-        if (a.z) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) load_run<T>((const T*)a.z + row * a.zs, c[k], a.C, z[k]);
+        for (int k = 0; k < NV; ++k) {
+            RowIO<T>::unpack(rx[k], y[k]);
+            if (branch) RowIO<T>::unpack(rz[k], z[k]);
         }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) load_run<T>((const T*)a.x + row * a.xs, c[k], a.C, y[k]);
-        if (a.z) {
+        if (base + step < a.M) fetch(row + step);
+        if (branch) {
             if (a.post != DSP_NORM_NONE) {
-                row_stats<TPR, NV, VW>(a.post, z, in, inv_c, a.eps, sum, mean, inv);
-                if (t == 0 && live && a.post_stats) {
+                row_stats<TPR, NV, VW>(a.post, z, c, a.C, inv_c, a.eps, sum, mean, inv);
+                if (at.t == 0 && live && a.post_stats) {
                     a.post_stats[row] = mean;
                     a.post_stats[a.M + row] = inv;
                 }
             }
-            const int64_t group = row_gate ? (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) : 0;
+            const int64_t group = row_gate && live ? (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) : 0;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float g[VW];
@@ -242,26 +308,22 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
                     const float act = row_gate ? w[k][e] * gate_act(a.act, g[e]) : w[k][e];
-                    float n = (z[k][e] - mean) * inv * gpost[k][e];
-                    if (a.post_bias && in[k][e]) n += a.post_bias[c[k] + e];
-                    y[k][e] = in[k][e] ? a.alpha * y[k][e] + act * n : 0.f;
+                    const float n = (z[k][e] - mean) * inv * gpost[k][e] + bpost[k][e];
+                    y[k][e] = a.alpha * y[k][e] + act * n;
                 }
                 if (live) store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k]);
             }
         }
         if (a.pre == DSP_NORM_NONE) continue;
-        row_stats<TPR, NV, VW>(a.pre, y, in, inv_c, a.eps, sum, mean, inv);
-        if (t == 0 && live && a.pre_stats) {
+        row_stats<TPR, NV, VW>(a.pre, y, c, a.C, inv_c, a.eps, sum, mean, inv);
+        if (at.t == 0 && live && a.pre_stats) {
             a.pre_stats[row] = mean;
             a.pre_stats[a.M + row] = inv;
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
 #pragma unroll
-            for (int e = 0; e < VW; ++e) {
-                y[k][e] = (y[k][e] - mean) * inv * gpre[k][e];
-                if (a.pre_bias && in[k][e]) y[k][e] += a.pre_bias[c[k] + e];
-            }
+            for (int e = 0; e < VW; ++e) y[k][e] = (y[k][e] - mean) * inv * gpre[k][e] + bpre[k][e];
             if (live) store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k]);
         }
     }
@@ -282,18 +344,16 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
 {
     constexpr int VW = RowIO<T>::VW, K = FULL ? 8 : 3, ACC = FULL ? 4 : 2;
     __shared__ float red[2][16][K];
-    __shared__ float fold[TPR ? kSubThreads * VW : 1];
-    RowSum<TPR, K> sum{red};
-    const int tid = threadIdx.x;
-    const int t = TPR ? tid % (TPR ? TPR : 1) : tid, threads = TPR ? TPR : (int)blockDim.x;
-    const int slots = TPR ? kSubThreads / (TPR ? TPR : 1) : 1, slot = TPR ? tid / (TPR ? TPR : 1) : 0;
+    __shared__ float fold[(TPR ? kSubThreads : 64 * kBackWaves) * VW];
+    const Place<TPR> at(a.waves);
+    RowSum<TPR, K> sum(red, a.waves, at.slot);
     const float inv_c = 1.f / (float)a.C;
-    const bool pre = a.pre != DSP_NORM_NONE, post = a.post != DSP_NORM_NONE;
+    const bool pre = a.pre != DSP_NORM_NONE, post = a.post != DSP_NORM_NONE, has_dy = a.dy != nullptr, has_z = a.z != nullptr;
     int c[NV];
     float w[NV][VW], gpre[NV][VW], p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        c[k] = (t + k * threads) * VW;
+        c[k] = (at.t + k * at.threads) * VW;
         load_vector(a.pre_gain, c[k], a.C, gpre[k], 1.f);
 #pragma unroll
         for (int e = 0; e < VW; ++e) p1[k][e] = p2[k][e] = s1[k][e] = s2[k][e] = f1[k][e] = f2[k][e] = 0.f;
@@ -309,60 +369,77 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
             for (int e = 0; e < VW; ++e) w[k][e] *= a.gate_rows ? a.beta * gate_act(a.act, g[e]) : a.beta;
         }
     };
-    auto one_row = [&](int64_t at, bool live) {
-        const int64_t row = live ? at : a.M - 1;
-        float zh[NV][VW], yh[NV][VW], q[NV][VW], dh[NV][VW];
+    Raw<T> rdh[NV], ry_[NV], rz_[NV], rdy[NV];
+    float my = 0.f, ry = 0.f, mz = 0.f, rz = 1.f;
+    auto fetch = [&](int64_t row) {
+        row = min(row, (int64_t)a.M - 1);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             if (pre) {
-                load_run<T>((const T*)a.dh + row * a.hs, c[k], a.C, dh[k]);
-                load_run<T>((const T*)a.y + row * a.ys, c[k], a.C, yh[k]);
+                rdh[k] = load_raw<T>((const T*)a.dh + row * a.hs, c[k], a.C);
+                ry_[k] = load_raw<T>((const T*)a.y + row * a.ys, c[k], a.C);
             }
-            if (a.z) load_run<T>((const T*)a.z + row * a.zs, c[k], a.C, zh[k]);
-            if (a.dy) load_run<T>((const T*)a.dy + row * a.ys, c[k], a.C, q[k]);
+            if (has_z) rz_[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
+            if (has_dy) rdy[k] = load_raw<T>((const T*)a.dy + row * a.ys, c[k], a.C);
         }
-        const float my = pre ? a.pre_stats[row] : 0.f, ry = pre ? a.pre_stats[a.M + row] : 0.f;
-        const float mz = post ? a.post_stats[row] : 0.f, rz = post ? a.post_stats[a.M + row] : 1.f;
+        if (pre) {
+            my = a.pre_stats[row];
+            ry = a.pre_stats[a.M + row];
+        }
+        if (post) {
+            mz = a.post_stats[row];
+            rz = a.post_stats[a.M + row];
+        }
+    };
+    // the fetched row; `next`, unless negative, is fetched while its sums are taken
+    auto one_row = [&](int64_t row, bool live, int64_t next) {
+        float zh[NV][VW], yh[NV][VW], q[NV][VW], dh[NV][VW];
         float s[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) s[k] = 0.f;
+        const float r_y = ry, r_z = rz;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) dh[k][e] = yh[k][e] = zh[k][e] = q[k][e] = 0.f;
+            if (pre) {
+                RowIO<T>::unpack(rdh[k], dh[k]);
+                RowIO<T>::unpack(ry_[k], yh[k]);
+            }
+            if (has_z) RowIO<T>::unpack(rz_[k], zh[k]);
+            if (has_dy) RowIO<T>::unpack(rdy[k], q[k]);
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
-                const bool in = c[k] + e < a.C;
-                if (!a.dy) q[k][e] = 0.f;
-                if (!pre) dh[k][e] = yh[k][e] = 0.f;
-                if (!a.z) zh[k][e] = 0.f;
-                yh[k][e] = in ? (yh[k][e] - my) * ry : 0.f;
-                zh[k][e] = in ? (zh[k][e] - mz) * rz : 0.f;
+                yh[k][e] = (yh[k][e] - my) * ry;
+                zh[k][e] = (zh[k][e] - mz) * rz;
                 const float b = dh[k][e] * gpre[k][e], wz = w[k][e] * zh[k][e];
                 q[k][e] += ry * b;
                 s[0] += b * yh[k][e];
                 s[1] += wz * q[k][e];
                 s[2] += wz * yh[k][e];
                 if (FULL) {
-                    const float wi = in ? w[k][e] : 0.f;
                     s[3 % K] += b;
                     s[4 % K] += wz;
-                    s[5 % K] += wi * q[k][e];
-                    s[6 % K] += wi * yh[k][e];
-                    s[7 % K] += wi;
+                    s[5 % K] += w[k][e] * q[k][e];
+                    s[6 % K] += w[k][e] * yh[k][e];
+                    s[7 % K] += w[k][e];
                 }
             }
+        }
+        if (next >= 0) fetch(next);
         if (pre || post) sum(s);
         const float m1 = pre ? s[0] * inv_c : 0.f, m0 = FULL && a.pre == DSP_NORM_LAYER ? s[3 % K] * inv_c : 0.f;
         float t1 = 0.f, t0 = 0.f;
         if (post) {
-            t1 = (s[1] - ry * (m1 * s[2] + (FULL ? m0 * s[4 % K] : 0.f))) * inv_c;
-            if (FULL && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - ry * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
+            t1 = (s[1] - r_y * (m1 * s[2] + (FULL ? m0 * s[4 % K] : 0.f))) * inv_c;
+            if (FULL && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - r_y * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float dz[VW];
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
-                const float D = c[k] + e < a.C ? q[k][e] - ry * (m0 + yh[k][e] * m1) : 0.f;
+                const float D = q[k][e] - r_y * (m0 + yh[k][e] * m1);
                 if (live) {
                     p1[k][e] += dh[k][e] * yh[k][e];
                     s1[k][e] += zh[k][e] * D;
@@ -371,7 +448,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
                         s2[k][e] += D;
                     }
                 }
-                dz[e] = post ? rz * (w[k][e] * D - t0 - zh[k][e] * t1) : w[k][e] * D;
+                dz[e] = post ? r_z * (w[k][e] * D - t0 - zh[k][e] * t1) : w[k][e] * D;
                 q[k][e] = a.alpha * D;
             }
             if (live && a.dx) store_run<T>((T*)a.dx + row * a.xs, c[k], a.C, q[k]);
@@ -381,18 +458,20 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
 
     if (FOLD) {
         const int64_t g0 = (int64_t)blockIdx.x * a.rows_per_part, g1 = min(g0 + a.rows_per_part, (int64_t)a.groups);
-        for (int64_t gb = g0; gb < g1; gb += slots) {
-            const bool mine = gb + slot < g1;
-            const int64_t group = mine ? gb + slot : g1 - 1;
-            weights(group);
+        fetch((g0 + at.slot) * a.gate_rows);
+        for (int64_t gb = g0; gb < g1; gb += at.slots) {
+            const int64_t group = gb + at.slot;
+            const bool mine = group < g1;
+            weights(mine ? group : g1 - 1);
             for (int i = 0; i < a.gate_rows; ++i) {
                 const int64_t row = group * a.gate_rows + i;
-                one_row(row, mine && row < a.M);
+                const bool last = i + 1 == a.gate_rows;
+                one_row(row, mine && row < a.M, !last ? row + 1 : gb + at.slots < g1 ? (group + at.slots) * a.gate_rows : -1);
             }
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float g[VW], gain[VW], bias[VW];
-                load_gate<T>(a.gate, a.gate_f32, group * a.gs, c[k], a.C, g);
+                load_gate<T>(a.gate, a.gate_f32, (mine ? group : g1 - 1) * a.gs, c[k], a.C, g);
                 load_vector(a.post_gain, c[k], a.C, gain, 1.f);
                 load_vector(a.post_bias, c[k], a.C, bias, 0.f);
 #pragma unroll
@@ -405,13 +484,8 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
                     g[e] = d;
                 }
                 if (mine && a.dgate) {
-                    if (sizeof(T) == 4 || !a.gate_f32) {
-                        store_run<T>((T*)a.dgate + group * a.gs, c[k], a.C, g);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < VW; ++e)
-                            if (c[k] + e < a.C) ((float*)a.dgate)[group * a.gs + c[k] + e] = g[e];
-                    }
+                    if (sizeof(T) == 4 || !a.gate_f32) store_run<T>((T*)a.dgate + group * a.gs, c[k], a.C, g);
+                    else store_vector((float*)a.dgate + group * a.gs, c[k], a.C, g);
                 }
             }
         }
@@ -420,8 +494,12 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
         const int64_t rows = a.gate_rows ? a.gate_rows : a.M;
         const int64_t r0 = group * rows + (int64_t)part * a.rows_per_part;
         const int64_t r1 = min(min(r0 + a.rows_per_part, (group + 1) * rows), (int64_t)a.M);
-        weights(group);
-        for (int64_t r = r0; r < r1; r += slots) one_row(r + slot, r + slot < r1);
+        if (r0 < r1) {
+            fetch(r0 + at.slot);
+            weights(group);
+        }
+        for (int64_t r = r0; r < r1; r += at.slots)
+            one_row(r + at.slot, r + at.slot < r1, r + at.slots < r1 ? r + at.slots + at.slot : -1);
     }
     if (!a.partial) return;
 #pragma unroll
@@ -433,18 +511,17 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
 #pragma unroll
             for (int e = 0; e < VW; ++e)
                 v[e] = acc == 0 ? p1[k][e] : acc == 2 ? p2[k][e] : acc == 1 ? (FOLD ? f1 : s1)[k][e] : (FOLD ? f2 : s2)[k][e];
-            if (TPR) {  // the workgroup's rows side by side: their sums in the order of the slots (NV = 1)
+            if (at.slots > 1) {  // the rows side by side: their sums in the order of the slots
                 __syncthreads();
 #pragma unroll
-                for (int e = 0; e < VW; ++e) fold[tid * VW + e] = v[e];
+                for (int e = 0; e < VW; ++e) fold[e * blockDim.x + threadIdx.x] = v[e];
                 __syncthreads();
-                if (slot == 0)
-                    for (int r = 1; r < slots; ++r)
+                if (at.slot == 0)
+                    for (int r = 1; r < at.slots; ++r)
 #pragma unroll
-                        for (int e = 0; e < VW; ++e) v[e] += fold[(r * threads + t) * VW + e];
+                        for (int e = 0; e < VW; ++e) v[e] += fold[e * blockDim.x + r * at.threads + at.t];
             }
-            if (slot == 0) store_run<float>(out, c[k], a.C, *(float(*)[4])v);
-            if (slot == 0 && VW == 8) store_run<float>(out, c[k] + 4, a.C, *(float(*)[4])(v + VW - 4));
+            if (at.slot == 0) store_vector(out, c[k], a.C, v);
         }
     }
 }
@@ -503,13 +580,15 @@ __global__ __launch_bounds__(64 * kFinalWaves) void norm_residual_final_kernel(N
         d2 += act * s2;
     };
 
-    if (a.dpre_gain || a.dpre_bias) {
+    if (blockIdx.y == 0) {
+        if (!a.dpre_gain && !a.dpre_bias) return;
         const float p1 = total(wave < a.parts ? parts_of(0, wave, a.parts - wave, kFinalWaves) : 0.f);
         const float p2 = a.full ? total(wave < a.parts ? parts_of(2, wave, a.parts - wave, kFinalWaves) : 0.f) : 0.f;
         if (wave == 0 && in) {
             if (a.dpre_gain) a.dpre_gain[c] = p1;
             if (a.dpre_bias) a.dpre_bias[c] = p2;
         }
+        return;
     }
     if (!a.dpost_gain && !a.dpost_bias && !(a.dgate && !a.fold)) return;
     float d1 = 0.f, d2 = 0.f;
@@ -573,7 +652,8 @@ RowShape row_shape(int dtype, int C)
     if (runs <= 8) return {8, 1, 1};
     if (runs <= 16) return {16, 1, 1};
     if (runs <= 32) return {32, 1, 1};
-    const int nv = runs <= 1024 ? 1 : runs <= 2048 ? 2 : 4;
+    // eight elements a thread while a workgroup of 16 waves holds the row, sixteen then
+    const int nv = (dtype == DSP_BF16 ? 1 : runs <= 64 ? 1 : 2) * (C <= 8192 ? 1 : 2);
     return {0, ceil_div(runs, 64 * nv), nv};
 }
 
@@ -587,10 +667,10 @@ BackPlan back_plan(const dsp_norm_residual_desc* d, bool biased)
 {
     BackPlan p;
     const RowShape s = row_shape(d->dtype, d->C);
-    const int slots = s.tpr ? kSubThreads / s.tpr : 1;
+    const int slots = s.tpr ? kSubThreads / s.tpr : std::max(1, kBackWaves / s.waves);
     const int64_t rows = d->gate_rows && d->gate_rows < d->M ? d->gate_rows : d->M;
     const int64_t groups = (d->M + rows - 1) / rows;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kParts, (d->M + slots - 1) / slots));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kParts, d->M / (4 * slots)));
     p.full = biased || d->post == DSP_NORM_LAYER || d->pre == DSP_NORM_LAYER;
     p.fold = groups > want;
     p.groups = (int)groups;
@@ -611,14 +691,17 @@ BackPlan back_plan(const dsp_norm_residual_desc* d, bool biased)
 template <typename T>
 int forward_t(const NormArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
 {
-    const int rows = s.tpr ? kSubThreads / s.tpr : 1;
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.M, rows), 4096)), block(s.tpr ? kSubThreads : 64 * s.waves);
-    if (s.tpr == 8) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 8, 1, kSubThreads>), grid, block, 0, st, a);
-    else if (s.tpr == 16) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 16, 1, kSubThreads>), grid, block, 0, st, a);
-    else if (s.tpr == 32) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 32, 1, kSubThreads>), grid, block, 0, st, a);
-    else if (s.nv == 1) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 0, 1, 1024>), grid, block, 0, st, a);
-    else if (s.nv == 2) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 0, 2, 1024>), grid, block, 0, st, a);
-    else DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, 0, 4, 1024>), grid, block, 0, st, a);
+    const int slots = s.tpr ? kSubThreads / s.tpr : std::max(1, 4 / s.waves);
+    const dim3 block(s.tpr ? kSubThreads : 64 * s.waves * slots);
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.M, slots), 256 * std::max(1, 2048 / (int)block.x)));
+#define FWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, TPR, NV, MAXT>), grid, block, 0, st, a)
+    if (s.tpr == 8) FWD(8, 1, kSubThreads);
+    else if (s.tpr == 16) FWD(16, 1, kSubThreads);
+    else if (s.tpr == 32) FWD(32, 1, kSubThreads);
+    else if (s.nv == 1) FWD(0, 1, 1024);
+    else if (s.nv == 2) FWD(0, 2, 1024);
+    else FWD(0, (sizeof(T) == 4 ? 4 : 2), 1024);
+#undef FWD
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
@@ -626,13 +709,17 @@ int forward_t(const NormArgs& a, const RowShape& s, hipStream_t st, ProfScope& p
 template <typename T, bool FULL, bool FOLD>
 int backward_t(const NormBackArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
 {
-    const dim3 grid(a.parts), block(s.tpr ? kSubThreads : 64 * s.waves);
-    if (s.tpr == 8) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 8, 1, kSubThreads, FULL, FOLD>), grid, block, 0, st, a);
-    else if (s.tpr == 16) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 16, 1, kSubThreads, FULL, FOLD>), grid, block, 0, st, a);
-    else if (s.tpr == 32) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 32, 1, kSubThreads, FULL, FOLD>), grid, block, 0, st, a);
-    else if (s.nv == 1) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 0, 1, 1024, FULL, FOLD>), grid, block, 0, st, a);
-    else if (s.nv == 2) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 0, 2, 1024, FULL, FOLD>), grid, block, 0, st, a);
-    else DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, 0, 4, 1024, FULL, FOLD>), grid, block, 0, st, a);
+    const dim3 grid(a.parts), block(s.tpr ? kSubThreads : 64 * s.waves * std::max(1, kBackWaves / s.waves));
+#define BWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, TPR, NV, MAXT, FULL, FOLD>), grid, block, 0, st, a)
+    constexpr int kNarrow = 64 * kBackWaves, kEight = sizeof(T) == 4 ? 2 : 1;  // kEight: runs of eight elements
+    if (s.tpr == 8) BWD(8, 1, kSubThreads);
+    else if (s.tpr == 16) BWD(16, 1, kSubThreads);
+    else if (s.tpr == 32) BWD(32, 1, kSubThreads);
+    else if (s.nv < kEight) BWD(0, 1, kNarrow);
+    else if (s.nv == kEight && (int)block.x <= kNarrow) BWD(0, kEight, kNarrow);
+    else if (s.nv == kEight) BWD(0, kEight, 1024);
+    else BWD(0, 2 * kEight, 1024);
+#undef BWD
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
@@ -667,9 +754,10 @@ int dsp_norm_residual_forward(const dsp_norm_residual_desc* d, const void* d_x, 
     a.M = (int)d->M; a.C = d->C; a.post = d->post; a.pre = d->pre; a.act = d->gate_act; a.gate_f32 = d->gate_dtype == DSP_FP32;
     a.gate_rows = (int)std::min<int64_t>(d->gate_rows, d->M);
     a.alpha = d->alpha; a.beta = d->beta; a.eps = d->eps;
+    const RowShape s = row_shape(d->dtype, d->C);
+    a.waves = s.waves;
     const double n = (double)d->M * d->C;
     ProfScope ps("norm_residual_fwd", n * e * (d_z ? (pre ? 4 : 3) : 2), 1);
-    const RowShape s = row_shape(d->dtype, d->C);
     return d->dtype == DSP_BF16 ? forward_t<bf16_t>(a, s, (hipStream_t)stream, ps)
                                 : forward_t<float>(a, s, (hipStream_t)stream, ps);
 }
@@ -715,6 +803,7 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh
     a.parts = p.parts; a.groups = p.groups; a.parts_per_group = p.parts_per_group; a.rows_per_part = p.rows_per_part;
     a.alpha = d->alpha; a.beta = d->beta;
     const RowShape s = row_shape(d->dtype, d->C);
+    a.waves = s.waves;
     hipStream_t st = (hipStream_t)stream;
     {
         const double n = (double)d->M * d->C;
@@ -734,7 +823,7 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh
     f.gs = a.gs; f.C = d->C; f.parts = p.parts; f.groups = p.groups; f.parts_per_group = p.parts_per_group; f.full = p.full; f.fold = p.fold;
     f.act = d->gate_act; f.gate_f16 = d->gate_dtype == DSP_BF16; f.gate_any = d->gate_rows > 0; f.beta = d->beta;
     ProfScope ps("norm_residual_final", (double)p.bytes, 1);
-    DSP_LAUNCH(ps, norm_residual_final_kernel, dim3(ceil_div(d->C, 64)), dim3(64 * kFinalWaves), 0, st, f);
+    DSP_LAUNCH(ps, norm_residual_final_kernel, dim3(ceil_div(d->C, 64), 2), dim3(64 * kFinalWaves), 0, st, f);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
