@@ -230,7 +230,8 @@ def _ptr(x):
 def _stream(s):
     if s is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.3 us; a Stream object costs 2.7
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     return s if isinstance(s, int) else s.cuda_stream
 
 

@@ -90,7 +90,7 @@ __device__ inline void store_run(T* row, int c, int C, const float (&v)[RowIO<T>
 {
     constexpr int VW = RowIO<T>::VW;
     if (c + VW <= C) {
-        *(Raw<T>*)(row + c) = RowIO<T>::pack(v);
+        __builtin_nontemporal_store(RowIO<T>::pack(v), (Raw<T>*)(row + c));
     } else if (c < C) {
 #pragma unroll
         for (int e = 0; e < VW; ++e)
@@ -134,15 +134,23 @@ __device__ inline void load_gate(const void* gate, int gate_f32, int64_t at, int
     else load_vector((const float*)gate + at, c, C, v, 0.f);
 }
 
+// exp(-g) from the hardware's power of two (within one unit of its last place) of a product that is rounded once: relative error
+// (|g| + 2) 2^-24.  Quotients from its reciprocal, within one unit too.
+__device__ inline float exp_of_minus(float g) { return __builtin_amdgcn_exp2f(g * -1.44269504f); }
+// tanh: (1 - e) / (1 + e) with e = exp(-2 |g|), below 1/4 its series up to g^9 (the next term is 1e-8 of it there).
 __device__ inline float gate_act(int act, float g)
 {
-    return act == DSP_GATE_IDENTITY ? g : act == DSP_GATE_SIGMOID ? 1.f / (1.f + expf(-g)) : tanhf(g);
+    if (act == DSP_GATE_IDENTITY) return g;
+    if (act == DSP_GATE_SIGMOID) return __builtin_amdgcn_rcpf(1.f + exp_of_minus(g));
+    const float e = exp_of_minus(2.f * fabsf(g)), far = (1.f - e) * __builtin_amdgcn_rcpf(1.f + e), s = g * g;
+    const float near = g + g * s * (-1.f / 3 + s * (2.f / 15 + s * (-17.f / 315 + s * (62.f / 2835))));
+    return fabsf(g) < 0.25f ? near : copysignf(far, g);
 }
 __device__ inline float gate_slope(int act, float g)
 {
     // sigmoid' = e / (1 + e)^2 with e = exp(-|g|), tanh' = 4 sigmoid'(2 g): no difference of nearly equal numbers
     if (act == DSP_GATE_IDENTITY) return 1.f;
-    const float e = expf(-fabsf(act == DSP_GATE_SIGMOID ? g : 2.f * g)), q = 1.f / (1.f + e);
+    const float e = exp_of_minus(fabsf(act == DSP_GATE_SIGMOID ? g : 2.f * g)), q = __builtin_amdgcn_rcpf(1.f + e);
     return (act == DSP_GATE_SIGMOID ? 1.f : 4.f) * e * q * q;
 }
 
@@ -183,17 +191,19 @@ struct RowSum {
         constexpr int LANES = TPR ? TPR : 64;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-#define STEP(ctrl) v[k] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v[k]), ctrl, 0xf, 0xf, true))
-            STEP(0xB1);                      // quad_perm 1,0,3,2
-            STEP(0x4E);                      // quad_perm 2,3,0,1
-            STEP(0x141);                     // row_half_mirror
-            if (LANES >= 16) STEP(0x140);    // row_mirror
+#define STEP(ctrl, rows) v[k] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v[k]), ctrl, rows, 0xf, true))
+            STEP(0xB1, 0xf);                      // quad_perm 1,0,3,2
+            STEP(0x4E, 0xf);                      // quad_perm 2,3,0,1
+            STEP(0x141, 0xf);                     // row_half_mirror
+            if (LANES >= 32) STEP(0x140, 0xf);    // row_mirror
+            if (LANES == 64) {                    // (the last lane has the whole sum: a scalar)
+                STEP(0x142, 0xa);                 // row_bcast:15
+                STEP(0x143, 0xc);                 // row_bcast:31
+                v[k] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v[k]), 63));
+            }
 #undef STEP
+            if (LANES == 32) v[k] += __shfl_xor(v[k], 16, 64);
         }
-#pragma unroll
-        for (int off = 16; off < LANES; off *= 2)
-#pragma unroll
-            for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], off, 64);
         if (TPR == 0 && waves > 1) {
             if (threadIdx.x % 64 == 0)
 #pragma unroll
@@ -209,33 +219,38 @@ struct RowSum {
     }
 };
 
-// Mean (layer norm; else 0) and 1 / deviation of a row whose runs a thread holds; columns behind the row hold 0.  Centred
-// before it is squared: a row far from zero keeps its variance.
-template <int TPR, int NV, int VW>
-__device__ inline void row_stats(int kind, const float (&a)[NV][VW], const int (&c)[NV], int C, float inv_c, float eps, RowSum<TPR, 1>& sum,
-                                 float& mean, float& inv)
+// Mean (layer norm; else 0) and 1 / deviation of a row; run(k, v) gives run k of the thread, 0 behind the row.  Centred before it is
+// squared: a row far from zero keeps its variance.
+template <int TPR, int NV, int VW, typename Run>
+__device__ inline void row_stats(int kind, Run run, const int (&c)[NV], int C, float inv_c, float eps, RowSum<TPR, 1>& sum, float& mean,
+                                 float& inv)
 {
     mean = 0.f;
-    float s[1];
+    float s[1], v[VW];
     if (kind == DSP_NORM_LAYER) {
         s[0] = 0.f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            run(k, v);
 #pragma unroll
-            for (int e = 0; e < VW; ++e) s[0] += a[k][e];
+            for (int e = 0; e < VW; ++e) s[0] += v[e];
+        }
         sum(s);
         mean = s[0] * inv_c;
     }
     s[0] = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const float centre = c[k] + VW <= C ? mean : 0.f;
-        if (c[k] + VW <= C || c[k] >= C || kind != DSP_NORM_LAYER) {
+        run(k, v);
+        if (kind != DSP_NORM_LAYER || c[k] >= C) {
 #pragma unroll
-            for (int e = 0; e < VW; ++e) s[0] += (a[k][e] - centre) * (a[k][e] - centre);
+            for (int e = 0; e < VW; ++e) s[0] += v[e] * v[e];
+        } else if (c[k] + VW <= C) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) s[0] += (v[e] - mean) * (v[e] - mean);
         } else {  // the row ends inside the run
 #pragma unroll
-            for (int e = 0; e < VW; ++e) s[0] += c[k] + e < C ? (a[k][e] - mean) * (a[k][e] - mean) : 0.f;
+            for (int e = 0; e < VW; ++e) s[0] += c[k] + e < C ? (v[e] - mean) * (v[e] - mean) : 0.f;
         }
     }
     sum(s);
@@ -257,13 +272,17 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 #pragma unroll
     for (int k = 0; k < NV; ++k) c[k] = (at.t + k * at.threads) * VW;
 
-    Raw<T> rx[NV], rz[NV];
+    const bool raw_gate = row_gate && (sizeof(T) == 4 || !a.gate_f32);  // its runs are fetched with the row's
+    Raw<T> rx[NV], rz[NV], rg[NV];
+    auto gate_row = [&](int64_t row) -> int64_t { return (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.gs; };
     auto fetch = [&](int64_t row) {
         row = min(row, (int64_t)a.M - 1);
+        const int64_t gate = raw_gate ? gate_row(row) : 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C);
             if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
+            if (raw_gate) rg[k] = load_raw<T>((const T*)a.gate + gate, c[k], a.C);
         }
     };
     int64_t base = (int64_t)blockIdx.x * at.slots;
@@ -284,38 +303,47 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
     for (; base < a.M; base += step) {
         const int64_t row = base + at.slot;
         const bool live = row < a.M;
-        float z[NV][VW], y[NV][VW];
+        float z[NV][VW], y[NV][VW], g[NV][VW];
         float mean = 0.f, inv = 1.f;
+        auto y_run = [&](int k, float (&v)[VW]) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) v[e] = y[k][e];
+        };
+        auto z_run = [&](int k, float (&v)[VW]) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) v[e] = z[k][e];
+        };
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             RowIO<T>::unpack(rx[k], y[k]);
             if (branch) RowIO<T>::unpack(rz[k], z[k]);
+            if (raw_gate) RowIO<T>::unpack(rg[k], g[k]);
         }
         if (base + step < a.M) fetch(row + step);
         if (branch) {
             if (a.post != DSP_NORM_NONE) {
-                row_stats<TPR, NV, VW>(a.post, z, c, a.C, inv_c, a.eps, sum, mean, inv);
+                row_stats<TPR, NV, VW>(a.post, z_run, c, a.C, inv_c, a.eps, sum, mean, inv);
                 if (at.t == 0 && live && a.post_stats) {
                     a.post_stats[row] = mean;
                     a.post_stats[a.M + row] = inv;
                 }
             }
-            const int64_t group = row_gate && live ? (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) : 0;
+            const int64_t gate = row_gate && !raw_gate ? gate_row(live ? row : a.M - 1) : 0;
+            const float shift = mean * inv;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                float g[VW];
-                if (row_gate) load_gate<T>(a.gate, a.gate_f32, group * a.gs, c[k], a.C, g);
+                if (row_gate && !raw_gate) load_gate<T>(a.gate, a.gate_f32, gate, c[k], a.C, g[k]);
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
-                    const float act = row_gate ? w[k][e] * gate_act(a.act, g[e]) : w[k][e];
-                    const float n = (z[k][e] - mean) * inv * gpost[k][e] + bpost[k][e];
+                    const float act = row_gate ? w[k][e] * gate_act(a.act, g[k][e]) : w[k][e];
+                    const float n = (z[k][e] * inv - shift) * gpost[k][e] + bpost[k][e];
                     y[k][e] = a.alpha * y[k][e] + act * n;
                 }
                 if (live) store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k]);
             }
         }
         if (a.pre == DSP_NORM_NONE) continue;
-        row_stats<TPR, NV, VW>(a.pre, y, c, a.C, inv_c, a.eps, sum, mean, inv);
+        row_stats<TPR, NV, VW>(a.pre, y_run, c, a.C, inv_c, a.eps, sum, mean, inv);
         if (at.t == 0 && live && a.pre_stats) {
             a.pre_stats[row] = mean;
             a.pre_stats[a.M + row] = inv;
@@ -323,8 +351,133 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
 #pragma unroll
-            for (int e = 0; e < VW; ++e) y[k][e] = (y[k][e] - mean) * inv * gpre[k][e] + bpre[k][e];
+            for (int e = 0; e < VW; ++e) y[k][e] = (y[k][e] * inv - mean * inv) * gpre[k][e] + bpre[k][e];
             if (live) store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k]);
+        }
+    }
+}
+
+// The same with a row a wave, NV runs a lane, where there are rows for all of them: no wave waits for another one.  Gains and
+// biases lie in LDS, four floats of neighbouring lanes side by side: beta act(gate) gain_post, the same times bias_post, gain_pre,
+// bias_pre (of the gate only where one row of it serves all).
+//
+// From 1024 rows on (us a call, this against rows of several waves; both at a call's cost below): 1024 x 2560 bf16 8.7 / 13.4,
+// 1024 x 4096 10.5 / 12.7, 512 x 4096 9.2 / 8.5; 8192 x 1152 18.8 / 28.3, 8192 x 2560 30.4 / 51.4, 8192 x 4096 52.3 / 54.0.
+constexpr int kWaveThreads = 512, kWaveRows = 1024;
+template <typename T, int NV, bool ROW_GATE>
+__global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(NormArgs a)
+{
+    constexpr int VW = RowIO<T>::VW, Q = VW / 4;
+    extern __shared__ float4 vectors[];
+    const int lane = threadIdx.x % 64, plane = 64 * NV;  // float4s
+    RowSum<0, 1> sum(nullptr, 1, 0);
+    const float inv_c = 1.f / (float)a.C;
+    const bool raw_gate = ROW_GATE && (sizeof(T) == 4 || !a.gate_f32);
+    const bool bpost = a.post_bias != nullptr, bpre = a.pre_bias != nullptr, branch = a.z != nullptr;
+    float4 *const vpost = vectors, *const vpre = vpost + Q * plane, *const vbpost = vpre + Q * plane, *const vbpre = vbpost + (bpost ? Q * plane : 0);
+    for (int run = threadIdx.x; run < plane; run += kWaveThreads) {
+        const int col = run * VW;
+        float g[VW], w[VW], b[VW];
+        auto put = [&](float4* to, const float (&v)[VW]) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) to[q * plane + run] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        };
+        load_vector(a.post_gain, col, a.C, g, 1.f);
+        if (a.gate_rows && !ROW_GATE) load_gate<T>(a.gate, a.gate_f32, 0, col, a.C, w);
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+            w[e] = a.gate_rows && !ROW_GATE ? a.beta * gate_act(a.act, w[e]) : a.beta;
+            g[e] *= w[e];
+        }
+        put(vpost, g);
+        if (bpost) {
+            load_vector(a.post_bias, col, a.C, b, 0.f);
+#pragma unroll
+            for (int e = 0; e < VW; ++e) b[e] *= w[e];
+            put(vbpost, b);
+        }
+        load_vector(a.pre_gain, col, a.C, g, 1.f);
+        put(vpre, g);
+        if (bpre) {
+            load_vector(a.pre_bias, col, a.C, b, 0.f);
+            put(vbpre, b);
+        }
+    }
+    __syncthreads();
+    auto get = [&](const float4* from, int k, float (&v)[VW]) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const float4 f = from[q * plane + k * 64 + lane];
+            v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
+        }
+    };
+    int c[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) c[k] = (k * 64 + lane) * VW;
+    const int waves = kWaveThreads / 64;
+    for (int64_t row = (int64_t)blockIdx.x * waves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); row < a.M; row += (int64_t)gridDim.x * waves) {
+        Raw<T> rx[NV], rz[NV], rg[NV];
+        const int64_t gate = ROW_GATE ? (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.gs : 0;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
+            rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C);
+            if (raw_gate) rg[k] = load_raw<T>((const T*)a.gate + gate, c[k], a.C);
+        }
+        float y[NV][VW];
+        float mean = 0.f, inv = 1.f;
+        if (branch) {
+            if (a.post != DSP_NORM_NONE) {
+                row_stats<0, NV, VW>(a.post, [&](int k, float (&v)[VW]) { RowIO<T>::unpack(rz[k], v); }, c, a.C, inv_c, a.eps, sum, mean, inv);
+                if (lane == 0 && a.post_stats) {
+                    a.post_stats[row] = mean;
+                    a.post_stats[a.M + row] = inv;
+                }
+            }
+            const float shift = mean * inv;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                float x[VW], z[VW], g[VW], w[VW], b[VW];
+                RowIO<T>::unpack(rz[k], z);
+                RowIO<T>::unpack(rx[k], x);
+                get(vpost, k, w);
+                if (bpost) get(vbpost, k, b);
+                if (raw_gate) RowIO<T>::unpack(rg[k], g);
+                else if (ROW_GATE) load_gate<T>(a.gate, a.gate_f32, gate, c[k], a.C, g);
+#pragma unroll
+                for (int e = 0; e < VW; ++e) {
+                    float n = (z[e] * inv - shift) * w[e];
+                    if (bpost) n += b[e];
+                    if (ROW_GATE) n *= gate_act(a.act, g[e]);
+                    y[k][e] = a.alpha * x[e] + n;
+                }
+                store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) RowIO<T>::unpack(rx[k], y[k]);
+        }
+        if (a.pre == DSP_NORM_NONE) continue;
+        row_stats<0, NV, VW>(a.pre, [&](int k, float (&v)[VW]) {
+#pragma unroll
+            for (int e = 0; e < VW; ++e) v[e] = y[k][e];
+        }, c, a.C, inv_c, a.eps, sum, mean, inv);
+        if (lane == 0 && a.pre_stats) {
+            a.pre_stats[row] = mean;
+            a.pre_stats[a.M + row] = inv;
+        }
+        const float shift = mean * inv;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float w[VW], b[VW];
+            get(vpre, k, w);
+            if (bpre) get(vbpre, k, b);
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+                y[k][e] = (y[k][e] * inv - shift) * w[e];
+                if (bpre) y[k][e] += b[e];
+            }
+            store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k]);
         }
     }
 }
@@ -339,16 +492,18 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 // dgain_post = beta act S1, dbias_post = beta act S2 and dgate = beta act' (gain_post S1 + bias_post S2) follow per column.
 // A thread keeps its columns' sums in registers over all rows of its workgroup.  FOLD (a gate with more rows than there are
 // workgroups): a workgroup takes whole rows of the gate, writes their dgate at once and folds the rest into sums of its own.
-template <typename T, int TPR, int NV, int MAXT, bool FULL, bool FOLD>
+constexpr int kPreOnly = 0, kRms = 1, kLayer = 2;  // SUMS: no norm behind the branch, none of the norms a layer norm, others
+template <typename T, int TPR, int NV, int MAXT, int SUMS, bool BIAS, bool FOLD>
 __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
 {
-    constexpr int VW = RowIO<T>::VW, K = FULL ? 8 : 3, ACC = FULL ? 4 : 2;
+    constexpr int VW = RowIO<T>::VW, K = SUMS == kPreOnly ? 2 : SUMS == kRms ? 3 : 8, ACC = BIAS ? 4 : 2;
+    constexpr bool LAYER = SUMS != kRms, POST = SUMS != kPreOnly;
     __shared__ float red[2][16][K];
     __shared__ float fold[(TPR ? kSubThreads : 64 * kBackWaves) * VW];
     const Place<TPR> at(a.waves);
     RowSum<TPR, K> sum(red, a.waves, at.slot);
     const float inv_c = 1.f / (float)a.C;
-    const bool pre = a.pre != DSP_NORM_NONE, post = a.post != DSP_NORM_NONE, has_dy = a.dy != nullptr, has_z = a.z != nullptr;
+    const bool pre = a.pre != DSP_NORM_NONE, post = POST && a.post != DSP_NORM_NONE, has_dy = a.dy != nullptr, has_z = a.z != nullptr;
     int c[NV];
     float w[NV][VW], gpre[NV][VW], p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
 #pragma unroll
@@ -370,7 +525,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
         }
     };
     Raw<T> rdh[NV], ry_[NV], rz_[NV], rdy[NV];
-    float my = 0.f, ry = 0.f, mz = 0.f, rz = 1.f;
+    float my = 0.f, ry = 0.f, mz = 0.f, rz = 1.f;  // 1 / deviations and the means times them
     auto fetch = [&](int64_t row) {
         row = min(row, (int64_t)a.M - 1);
 #pragma unroll
@@ -383,12 +538,12 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
             if (has_dy) rdy[k] = load_raw<T>((const T*)a.dy + row * a.ys, c[k], a.C);
         }
         if (pre) {
-            my = a.pre_stats[row];
             ry = a.pre_stats[a.M + row];
+            my = a.pre_stats[row] * ry;
         }
         if (post) {
-            mz = a.post_stats[row];
             rz = a.post_stats[a.M + row];
+            mz = a.post_stats[row] * rz;
         }
     };
     // the fetched row; `next`, unless negative, is fetched while its sums are taken
@@ -410,29 +565,34 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
             if (has_dy) RowIO<T>::unpack(rdy[k], q[k]);
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
-                yh[k][e] = (yh[k][e] - my) * ry;
-                zh[k][e] = (zh[k][e] - mz) * rz;
-                const float b = dh[k][e] * gpre[k][e], wz = w[k][e] * zh[k][e];
+                yh[k][e] = yh[k][e] * ry - my;
+                if (POST) zh[k][e] = zh[k][e] * rz - mz;
+                const float b = dh[k][e] * gpre[k][e];
                 q[k][e] += ry * b;
                 s[0] += b * yh[k][e];
-                s[1] += wz * q[k][e];
-                s[2] += wz * yh[k][e];
-                if (FULL) {
-                    s[3 % K] += b;
-                    s[4 % K] += wz;
-                    s[5 % K] += w[k][e] * q[k][e];
-                    s[6 % K] += w[k][e] * yh[k][e];
-                    s[7 % K] += w[k][e];
+                if (LAYER) s[1] += b;
+                if (POST) {
+                    const float wz = w[k][e] * zh[k][e];
+                    constexpr int o = LAYER ? 2 : 1;
+                    s[o % K] += wz * q[k][e];
+                    s[(o + 1) % K] += wz * yh[k][e];
+                    if (LAYER) {
+                        s[4 % K] += wz;
+                        s[5 % K] += w[k][e] * q[k][e];
+                        s[6 % K] += w[k][e] * yh[k][e];
+                        s[7 % K] += w[k][e];
+                    }
                 }
             }
         }
         if (next >= 0) fetch(next);
         if (pre || post) sum(s);
-        const float m1 = pre ? s[0] * inv_c : 0.f, m0 = FULL && a.pre == DSP_NORM_LAYER ? s[3 % K] * inv_c : 0.f;
+        const float m1 = pre ? s[0] * inv_c : 0.f, m0 = LAYER && a.pre == DSP_NORM_LAYER ? s[1] * inv_c : 0.f;
         float t1 = 0.f, t0 = 0.f;
         if (post) {
-            t1 = (s[1] - r_y * (m1 * s[2] + (FULL ? m0 * s[4 % K] : 0.f))) * inv_c;
-            if (FULL && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - r_y * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
+            constexpr int o = LAYER ? 2 : 1;
+            t1 = (s[o % K] - r_y * (m1 * s[(o + 1) % K] + (LAYER ? m0 * s[4 % K] : 0.f))) * inv_c;
+            if (LAYER && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - r_y * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -443,12 +603,12 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
                 if (live) {
                     p1[k][e] += dh[k][e] * yh[k][e];
                     s1[k][e] += zh[k][e] * D;
-                    if (FULL) {
+                    if (BIAS) {
                         p2[k][e] += dh[k][e];
                         s2[k][e] += D;
                     }
                 }
-                dz[e] = post ? r_z * (w[k][e] * D - t0 - zh[k][e] * t1) : w[k][e] * D;
+                dz[e] = POST ? r_z * (w[k][e] * D - t0 - zh[k][e] * t1) : w[k][e] * D;
                 q[k][e] = a.alpha * D;
             }
             if (live && a.dx) store_run<T>((T*)a.dx + row * a.xs, c[k], a.C, q[k]);
@@ -477,7 +637,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
                     const float act = a.beta * gate_act(a.act, g[e]);
-                    const float d = a.beta * gate_slope(a.act, g[e]) * (gain[e] * s1[k][e] + (FULL ? bias[e] * s2[k][e] : 0.f));
+                    const float d = a.beta * gate_slope(a.act, g[e]) * (gain[e] * s1[k][e] + (BIAS ? bias[e] * s2[k][e] : 0.f));
                     f1[k][e] += act * s1[k][e];
                     f2[k][e] += act * s2[k][e];
                     s1[k][e] = s2[k][e] = 0.f;
@@ -542,6 +702,7 @@ constexpr int kFinalWaves = 16;
 __global__ __launch_bounds__(64 * kFinalWaves) void norm_residual_final_kernel(NormFinalArgs a)
 {
     __shared__ float red[kFinalWaves][64];
+    __shared__ float rows[kFinalWaves][kFinalWaves][64];  // [row of the gate][wave]
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
     const bool in = c < a.C;
     auto total = [&](float v) -> float {  // over the waves, in all of them
@@ -565,12 +726,12 @@ __global__ __launch_bounds__(64 * kFinalWaves) void norm_residual_final_kernel(N
     };
     const float gain = in && a.post_gain ? a.post_gain[c] : 1.f, bias = in && a.post_bias ? a.post_bias[c] : 0.f;
     // gradient of the gate's row g from its sums; returns what the row gives to the gain and the bias behind it
-    auto gate_row = [&](int g, float s1, float s2, bool write, float& d1, float& d2) {
+    auto gate_row = [&](int g, float s1, float s2, float& d1, float& d2) {
         float act = a.beta;
         if (in && a.gate_any) {
             const float v = gate_of(g);
             act *= gate_act(a.act, v);
-            if (write && a.dgate) {
+            if (a.dgate) {
                 const float d = a.beta * gate_slope(a.act, v) * (gain * s1 + bias * s2);
                 if (a.gate_f16) ((bf16_t*)a.dgate)[g * a.gs + c] = float_to_bf16(d);
                 else ((float*)a.dgate)[g * a.gs + c] = d;
@@ -595,18 +756,36 @@ __global__ __launch_bounds__(64 * kFinalWaves) void norm_residual_final_kernel(N
     if (a.fold) {
         d1 = total(wave < a.parts ? parts_of(1, wave, a.parts - wave, kFinalWaves) : 0.f);
         d2 = a.full ? total(wave < a.parts ? parts_of(3, wave, a.parts - wave, kFinalWaves) : 0.f) : 0.f;
-    } else if (a.parts_per_group >= kFinalWaves || a.groups == 1) {  // few rows of the gate: the waves share the parts of each
-        for (int g = 0; g < a.groups; ++g) {
-            const int n = a.parts_per_group - wave;
-            const float s1 = total(n > 0 ? parts_of(1, g * a.parts_per_group + wave, n, kFinalWaves) : 0.f);
-            const float s2 = a.full ? total(n > 0 ? parts_of(3, g * a.parts_per_group + wave, n, kFinalWaves) : 0.f) : 0.f;
-            gate_row(g, s1, s2, wave == 0, d1, d2);
+    } else if (a.groups <= kFinalWaves) {  // few rows of the gate: the waves share the parts of each, then take a row each
+        float s[2] = {0.f, 0.f};
+        for (int which = 0; which <= a.full; ++which) {
+            const int acc = 1 + 2 * which, n = a.parts_per_group - wave;
+            if (a.parts_per_group <= kFinalWaves) {  // a part a wave: all of them on their way at once
+                float v[kFinalWaves];
+#pragma unroll
+                for (int g = 0; g < kFinalWaves; ++g) {
+                    const bool has = in && n > 0 && g < a.groups;
+                    v[g] = has ? a.partial[((size_t)acc * a.parts + g * a.parts_per_group + wave) * a.C + c] : 0.f;
+                }
+#pragma unroll
+                for (int g = 0; g < kFinalWaves; ++g) rows[g][wave][lane] = v[g];
+            } else {
+                for (int g = 0; g < a.groups; ++g)
+                    rows[g][wave][lane] = n > 0 ? parts_of(acc, g * a.parts_per_group + wave, n, kFinalWaves) : 0.f;
+            }
+            __syncthreads();
+            if (wave < a.groups)
+                for (int w = 0; w < kFinalWaves; ++w) s[which] += rows[wave][w][lane];
+            __syncthreads();
         }
+        if (wave < a.groups) gate_row(wave, s[0], s[1], d1, d2);
+        d1 = total(d1);
+        d2 = total(d2);
     } else {  // many: every wave takes rows of its own
         for (int g = wave; g < a.groups; g += kFinalWaves) {
             const float s1 = parts_of(1, g * a.parts_per_group, a.parts_per_group, 1);
             const float s2 = a.full ? parts_of(3, g * a.parts_per_group, a.parts_per_group, 1) : 0.f;
-            gate_row(g, s1, s2, true, d1, d2);
+            gate_row(g, s1, s2, d1, d2);
         }
         d1 = total(d1);
         d2 = total(d2);
@@ -650,7 +829,6 @@ RowShape row_shape(int dtype, int C)
 {
     const int vw = dtype == DSP_BF16 ? 8 : 4, runs = ceil_div(C, vw);
     if (runs <= 8) return {8, 1, 1};
-    if (runs <= 16) return {16, 1, 1};
     if (runs <= 32) return {32, 1, 1};
     // eight elements a thread while a workgroup of 16 waves holds the row, sixteen then
     const int nv = (dtype == DSP_BF16 ? 1 : runs <= 64 ? 1 : 2) * (C <= 8192 ? 1 : 2);
@@ -659,7 +837,8 @@ RowShape row_shape(int dtype, int C)
 
 // How the backward kernel's workgroups share the rows.
 struct BackPlan {
-    bool full, fold;
+    int sums;
+    bool biased, fold;
     int parts, groups, parts_per_group, rows_per_part;
     size_t bytes;
 };
@@ -671,7 +850,8 @@ BackPlan back_plan(const dsp_norm_residual_desc* d, bool biased)
     const int64_t rows = d->gate_rows && d->gate_rows < d->M ? d->gate_rows : d->M;
     const int64_t groups = (d->M + rows - 1) / rows;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(kParts, d->M / (4 * slots)));
-    p.full = biased || d->post == DSP_NORM_LAYER || d->pre == DSP_NORM_LAYER;
+    p.sums = d->post == DSP_NORM_NONE ? kPreOnly : d->post == DSP_NORM_LAYER || d->pre == DSP_NORM_LAYER ? kLayer : kRms;
+    p.biased = biased;
     p.fold = groups > want;
     p.groups = (int)groups;
     if (p.fold) {
@@ -684,19 +864,48 @@ BackPlan back_plan(const dsp_norm_residual_desc* d, bool biased)
         p.parts_per_group = (int)((rows + p.rows_per_part - 1) / p.rows_per_part);
         p.parts = (int)(groups * p.parts_per_group);
     }
-    p.bytes = (size_t)p.parts * (p.full ? 4 : 2) * d->C * sizeof(float);
+    p.bytes = (size_t)p.parts * (p.biased ? 4 : 2) * d->C * sizeof(float);
     return p;
+}
+
+// The forward pass with a row a wave.
+template <typename T>
+int forward_wave_t(const NormArgs& a, hipStream_t st, ProfScope& ps)
+{
+    constexpr int VW = RowIO<T>::VW;
+    const int nv = ceil_div(a.C, 64 * VW), waves = kWaveThreads / 64;
+    const size_t lds = (size_t)(2 + (a.post_bias ? 1 : 0) + (a.pre_bias ? 1 : 0)) * 64 * nv * VW * sizeof(float);
+    const int per_cu = std::max(1, std::min((int)(160 * 1024 / lds), 4));
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.M, waves), 256 * per_cu)), block(kWaveThreads);
+    const bool row_gate = a.gate_rows > 0 && a.gate_rows < a.M;
+#define WAVE(NV)                                                                                      \
+    if (row_gate) DSP_LAUNCH(ps, (norm_residual_fwd_wave_kernel<T, NV, true>), grid, block, lds, st, a); \
+    else DSP_LAUNCH(ps, (norm_residual_fwd_wave_kernel<T, NV, false>), grid, block, lds, st, a);         \
+    break
+    switch (nv) {
+    case 1: WAVE(1);
+    case 2: WAVE(2);
+    case 3: WAVE(3);
+    case 4: WAVE(4);
+    case 5: WAVE(5);
+    case 6: WAVE(6);
+    case 7: WAVE(7);
+    default: WAVE(8);
+    }
+#undef WAVE
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
 }
 
 template <typename T>
 int forward_t(const NormArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
 {
+    if (!s.tpr && a.C <= 512 * RowIO<T>::VW && a.M >= kWaveRows) return forward_wave_t<T>(a, st, ps);
     const int slots = s.tpr ? kSubThreads / s.tpr : std::max(1, 4 / s.waves);
     const dim3 block(s.tpr ? kSubThreads : 64 * s.waves * slots);
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.M, slots), 256 * std::max(1, 2048 / (int)block.x)));
 #define FWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, TPR, NV, MAXT>), grid, block, 0, st, a)
     if (s.tpr == 8) FWD(8, 1, kSubThreads);
-    else if (s.tpr == 16) FWD(16, 1, kSubThreads);
     else if (s.tpr == 32) FWD(32, 1, kSubThreads);
     else if (s.nv == 1) FWD(0, 1, 1024);
     else if (s.nv == 2) FWD(0, 2, 1024);
@@ -706,14 +915,13 @@ int forward_t(const NormArgs& a, const RowShape& s, hipStream_t st, ProfScope& p
     return DSP_OK;
 }
 
-template <typename T, bool FULL, bool FOLD>
+template <typename T, int SUMS, bool BIAS, bool FOLD>
 int backward_t(const NormBackArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
 {
     const dim3 grid(a.parts), block(s.tpr ? kSubThreads : 64 * s.waves * std::max(1, kBackWaves / s.waves));
-#define BWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, TPR, NV, MAXT, FULL, FOLD>), grid, block, 0, st, a)
+#define BWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, TPR, NV, MAXT, SUMS, BIAS, FOLD>), grid, block, 0, st, a)
     constexpr int kNarrow = 64 * kBackWaves, kEight = sizeof(T) == 4 ? 2 : 1;  // kEight: runs of eight elements
     if (s.tpr == 8) BWD(8, 1, kSubThreads);
-    else if (s.tpr == 16) BWD(16, 1, kSubThreads);
     else if (s.tpr == 32) BWD(32, 1, kSubThreads);
     else if (s.nv < kEight) BWD(0, 1, kNarrow);
     else if (s.nv == kEight && (int)block.x <= kNarrow) BWD(0, kEight, kNarrow);
@@ -722,6 +930,21 @@ int backward_t(const NormBackArgs& a, const RowShape& s, hipStream_t st, ProfSco
 #undef BWD
     DSP_HIP(hipGetLastError());
     return DSP_OK;
+}
+
+template <typename T, bool FOLD>
+int backward_fold(const NormBackArgs& a, const RowShape& s, const BackPlan& p, hipStream_t st, ProfScope& ps)
+{
+#define CLASS(SUMS) return p.biased ? backward_t<T, SUMS, true, FOLD>(a, s, st, ps) : backward_t<T, SUMS, false, FOLD>(a, s, st, ps)
+    if (p.sums == kPreOnly) CLASS(kPreOnly);
+    if (p.sums == kRms) CLASS(kRms);
+    CLASS(kLayer);
+#undef CLASS
+}
+template <typename T>
+int backward_any(const NormBackArgs& a, const RowShape& s, const BackPlan& p, hipStream_t st, ProfScope& ps)
+{
+    return p.fold ? backward_fold<T, true>(a, s, p, st, ps) : backward_fold<T, false>(a, s, p, st, ps);
 }
 
 }  // namespace
@@ -808,19 +1031,14 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh
     {
         const double n = (double)d->M * d->C;
         ProfScope ps("norm_residual_bwd", n * e * ((pre ? 2 : 0) + (d_dy ? 1 : 0) + (a.z ? 1 : 0) + (d_dx ? 1 : 0) + (d_dz ? 1 : 0)), 1);
-        const bool bf = d->dtype == DSP_BF16;
-        int rc;
-        if (p.full) rc = p.fold ? (bf ? backward_t<bf16_t, true, true>(a, s, st, ps) : backward_t<float, true, true>(a, s, st, ps))
-                                : (bf ? backward_t<bf16_t, true, false>(a, s, st, ps) : backward_t<float, true, false>(a, s, st, ps));
-        else rc = p.fold ? (bf ? backward_t<bf16_t, false, true>(a, s, st, ps) : backward_t<float, false, true>(a, s, st, ps))
-                         : (bf ? backward_t<bf16_t, false, false>(a, s, st, ps) : backward_t<float, false, false>(a, s, st, ps));
+        const int rc = d->dtype == DSP_BF16 ? backward_any<bf16_t>(a, s, p, st, ps) : backward_any<float>(a, s, p, st, ps);
         DSP_TRY(rc);
     }
     if (!sums) return DSP_OK;
     NormFinalArgs f;
     f.partial = a.partial; f.gate = d_gate; f.post_gain = a.post_gain; f.post_bias = a.post_bias; f.dgate = d_dgate;
     f.dpost_gain = d_dpost_gain; f.dpost_bias = d_dpost_bias; f.dpre_gain = d_dpre_gain; f.dpre_bias = d_dpre_bias;
-    f.gs = a.gs; f.C = d->C; f.parts = p.parts; f.groups = p.groups; f.parts_per_group = p.parts_per_group; f.full = p.full; f.fold = p.fold;
+    f.gs = a.gs; f.C = d->C; f.parts = p.parts; f.groups = p.groups; f.parts_per_group = p.parts_per_group; f.full = p.biased; f.fold = p.fold;
     f.act = d->gate_act; f.gate_f16 = d->gate_dtype == DSP_BF16; f.gate_any = d->gate_rows > 0; f.beta = d->beta;
     ProfScope ps("norm_residual_final", (double)p.bytes, 1);
     DSP_LAUNCH(ps, norm_residual_final_kernel, dim3(ceil_div(d->C, 64), 2), dim3(64 * kFinalWaves), 0, st, f);
