@@ -11,7 +11,7 @@ namespace dsp {
 namespace {
 
 constexpr int kMaxC = 16384;
-constexpr int kSubThreads = 256;  // workgroup of the kernels whose rows are shorter than a wave
+constexpr int kSubThreads = 512;  // workgroup of the kernels whose rows are shorter than a wave
 constexpr int kBackWaves = 8;     // waves a workgroup of the backward kernel fills with rows side by side
 constexpr int kParts = 512;       // most workgroups of the backward kernel = rows of partial sums
 
@@ -35,6 +35,7 @@ struct NormBackArgs {
     int M, C, post, pre, act, gate_f32, gate_rows, waves;
     int parts, groups, parts_per_group, rows_per_part;  // fold: rows_per_part = rows of the gate of a workgroup
     float alpha, beta;
+    bool whole;  // rows of whole 16-byte runs on 16-byte addresses (and, folded, a gate of the rows' type)
 };
 
 // Runs of 16 bytes on addresses of the element's size: rows may begin at any element (an odd C, a stride of the caller's).
@@ -72,12 +73,24 @@ struct RowIO<bf16_t> {
 template <typename T>
 using Raw = typename RowIO<T>::Raw;
 
-// VW elements from column c on, as they lie in memory; those behind the row are 0.
+// A run as it lies in memory, kept so: what was unpacked of it before is not held beside it.
 template <typename T>
-__device__ inline Raw<T> load_raw(const T* row, int c, int C)
+__device__ inline Raw<T> hold(Raw<T> r)
+{
+    uint32_t w[4];
+    __builtin_memcpy(w, &r, 16);
+    asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+    __builtin_memcpy(&r, w, 16);
+    return r;
+}
+
+// VW elements from column c on, as they lie in memory; those behind the row are 0.  (whole: there are none.  Every row shape has that
+// for all runs of a thread but its last.)
+template <typename T>
+__device__ inline Raw<T> load_raw(const T* row, int c, int C, bool whole = false)
 {
     constexpr int VW = RowIO<T>::VW;
-    if (c + VW <= C) return *(const Raw<T>*)(row + c);
+    if (whole || c + VW <= C) return *(const Raw<T>*)(row + c);
     float v[VW] = {};
     if (c < C) {
 #pragma unroll
@@ -85,11 +98,31 @@ __device__ inline Raw<T> load_raw(const T* row, int c, int C)
     }
     return RowIO<T>::pack(v);
 }
+// The same of rows of whole 16-byte runs on 16-byte addresses, through a descriptor of the row: what lies behind it, or all of it
+// where there is no such row, reads 0 and is not written.  Without a branch around any access the compiler can count them, and a wait
+// for the next row's runs does not wait for the stores issued behind them.
+typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+__device__ inline __amdgpu_buffer_rsrc_t row_rsrc(const void* p, int64_t byte, uint32_t bytes, bool there)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((char*)const_cast<void*>(p) + (there ? byte : 0), 0, there ? (int)bytes : 0, 0x00020000);
+}
 template <typename T>
-__device__ inline void store_run(T* row, int c, int C, const float (&v)[RowIO<T>::VW])
+__device__ inline Raw<T> load_rsrc(__amdgpu_buffer_rsrc_t r, int c)
+{
+    return __builtin_bit_cast(Raw<T>, __builtin_amdgcn_raw_buffer_load_b128(r, c * (int)sizeof(T), 0, 0));
+}
+template <typename T>
+__device__ inline void store_rsrc(__amdgpu_buffer_rsrc_t r, int c, const float (&v)[RowIO<T>::VW])
+{
+    constexpr int kNonTemporal = 2;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(U4, RowIO<T>::pack(v)), r, c * (int)sizeof(T), 0, kNonTemporal);
+}
+
+template <typename T>
+__device__ inline void store_run(T* row, int c, int C, const float (&v)[RowIO<T>::VW], bool whole = false)
 {
     constexpr int VW = RowIO<T>::VW;
-    if (c + VW <= C) {
+    if (whole || c + VW <= C) {
         __builtin_nontemporal_store(RowIO<T>::pack(v), (Raw<T>*)(row + c));
     } else if (c < C) {
 #pragma unroll
@@ -137,24 +170,38 @@ __device__ inline void load_gate(const void* gate, int gate_f32, int64_t at, int
 // exp(-g) from the hardware's power of two (within one unit of its last place) of a product that is rounded once: relative error
 // (|g| + 2) 2^-24.  Quotients from its reciprocal, within one unit too.
 __device__ inline float exp_of_minus(float g) { return __builtin_amdgcn_exp2f(g * -1.44269504f); }
-// tanh: (1 - e) / (1 + e) with e = exp(-2 |g|), below 1/4 its series up to g^9 (the next term is 1e-8 of it there).
+// The activation and its derivative, with e = exp(-|g|) (tanh: exp(-2 |g|)) and q = 1 / (1 + e): sigmoid = q or e q, sigmoid' = e q^2;
+// tanh = (1 - e) q, below 1/4 its series up to g^9 (the next term is 1e-8 of it there), tanh' = 4 e q^2.  No difference of nearly
+// equal numbers.
+__device__ inline void gate_both(int act, float g, float& a, float& slope)
+{
+    a = g;
+    slope = 1.f;
+    if (act == DSP_GATE_IDENTITY) return;
+    const float e = exp_of_minus(act == DSP_GATE_SIGMOID ? fabsf(g) : 2.f * fabsf(g)), q = __builtin_amdgcn_rcpf(1.f + e);
+    if (act == DSP_GATE_SIGMOID) {
+        a = g >= 0.f ? q : e * q;
+        slope = e * q * q;
+        return;
+    }
+    const float s = g * g, near = g + g * s * (-1.f / 3 + s * (2.f / 15 + s * (-17.f / 315 + s * (62.f / 2835))));
+    a = fabsf(g) < 0.25f ? near : copysignf((1.f - e) * q, g);
+    slope = 4.f * e * q * q;
+}
 __device__ inline float gate_act(int act, float g)
 {
-    if (act == DSP_GATE_IDENTITY) return g;
-    if (act == DSP_GATE_SIGMOID) return __builtin_amdgcn_rcpf(1.f + exp_of_minus(g));
-    const float e = exp_of_minus(2.f * fabsf(g)), far = (1.f - e) * __builtin_amdgcn_rcpf(1.f + e), s = g * g;
-    const float near = g + g * s * (-1.f / 3 + s * (2.f / 15 + s * (-17.f / 315 + s * (62.f / 2835))));
-    return fabsf(g) < 0.25f ? near : copysignf(far, g);
+    float a, slope;
+    gate_both(act, g, a, slope);
+    return a;
 }
 __device__ inline float gate_slope(int act, float g)
 {
-    // sigmoid' = e / (1 + e)^2 with e = exp(-|g|), tanh' = 4 sigmoid'(2 g): no difference of nearly equal numbers
-    if (act == DSP_GATE_IDENTITY) return 1.f;
-    const float e = exp_of_minus(fabsf(act == DSP_GATE_SIGMOID ? g : 2.f * g)), q = __builtin_amdgcn_rcpf(1.f + e);
-    return (act == DSP_GATE_SIGMOID ? 1.f : 4.f) * e * q * q;
+    float a, slope;
+    gate_both(act, g, a, slope);
+    return slope;
 }
 
-// How a workgroup's threads hold rows: TPR lanes a row and 256 / TPR rows, or (TPR = 0) `waves` waves a row and as many rows as the
+// How a workgroup's threads hold rows: TPR lanes a row and kSubThreads / TPR rows, or (TPR = 0) `waves` waves a row and as many rows as the
 // workgroup has waves for.
 template <int TPR>
 struct Place {
@@ -195,7 +242,7 @@ struct RowSum {
             STEP(0xB1, 0xf);                      // quad_perm 1,0,3,2
             STEP(0x4E, 0xf);                      // quad_perm 2,3,0,1
             STEP(0x141, 0xf);                     // row_half_mirror
-            if (LANES >= 32) STEP(0x140, 0xf);    // row_mirror
+            if (LANES >= 16) STEP(0x140, 0xf);    // row_mirror
             if (LANES == 64) {                    // (the last lane has the whole sum: a scalar)
                 STEP(0x142, 0xa);                 // row_bcast:15
                 STEP(0x143, 0xc);                 // row_bcast:31
@@ -242,10 +289,10 @@ __device__ inline void row_stats(int kind, Run run, const int (&c)[NV], int C, f
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         run(k, v);
-        if (kind != DSP_NORM_LAYER || c[k] >= C) {
+        if (kind != DSP_NORM_LAYER || (k + 1 == NV && c[k] >= C)) {
 #pragma unroll
             for (int e = 0; e < VW; ++e) s[0] += v[e] * v[e];
-        } else if (c[k] + VW <= C) {
+        } else if (k + 1 < NV || c[k] + VW <= C) {
 #pragma unroll
             for (int e = 0; e < VW; ++e) s[0] += (v[e] - mean) * (v[e] - mean);
         } else {  // the row ends inside the run
@@ -280,9 +327,9 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
         const int64_t gate = raw_gate ? gate_row(row) : 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C);
-            if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
-            if (raw_gate) rg[k] = load_raw<T>((const T*)a.gate + gate, c[k], a.C);
+            rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C, k + 1 < NV);
+            if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C, k + 1 < NV);
+            if (raw_gate) rg[k] = load_raw<T>((const T*)a.gate + gate, c[k], a.C, k + 1 < NV);
         }
     };
     int64_t base = (int64_t)blockIdx.x * at.slots;
@@ -339,7 +386,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
                     const float n = (z[k][e] * inv - shift) * gpost[k][e] + bpost[k][e];
                     y[k][e] = a.alpha * y[k][e] + act * n;
                 }
-                if (live) store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k]);
+                if (live) store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k], k + 1 < NV);
             }
         }
         if (a.pre == DSP_NORM_NONE) continue;
@@ -352,7 +399,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
         for (int k = 0; k < NV; ++k) {
 #pragma unroll
             for (int e = 0; e < VW; ++e) y[k][e] = (y[k][e] * inv - mean * inv) * gpre[k][e] + bpre[k][e];
-            if (live) store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k]);
+            if (live) store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k], k + 1 < NV);
         }
     }
 }
@@ -420,9 +467,9 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
         const int64_t gate = ROW_GATE ? (int64_t)((uint32_t)row / (uint32_t)a.gate_rows) * a.gs : 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
-            rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C);
-            if (raw_gate) rg[k] = load_raw<T>((const T*)a.gate + gate, c[k], a.C);
+            if (branch) rz[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C, k + 1 < NV);
+            rx[k] = load_raw<T>((const T*)a.x + row * a.xs, c[k], a.C, k + 1 < NV);
+            if (raw_gate) rg[k] = load_raw<T>((const T*)a.gate + gate, c[k], a.C, k + 1 < NV);
         }
         float y[NV][VW];
         float mean = 0.f, inv = 1.f;
@@ -438,6 +485,7 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float x[VW], z[VW], g[VW], w[VW], b[VW];
+                if (sizeof(T) == 2) rz[k] = hold<T>(rz[k]);
                 RowIO<T>::unpack(rz[k], z);
                 RowIO<T>::unpack(rx[k], x);
                 get(vpost, k, w);
@@ -451,7 +499,7 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
                     if (ROW_GATE) n *= gate_act(a.act, g[e]);
                     y[k][e] = a.alpha * x[e] + n;
                 }
-                store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k]);
+                store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k], k + 1 < NV);
             }
         } else {
 #pragma unroll
@@ -477,7 +525,7 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
                 y[k][e] = (y[k][e] * inv - shift) * w[e];
                 if (bpre) y[k][e] += b[e];
             }
-            store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k]);
+            store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k], k + 1 < NV);
         }
     }
 }
@@ -493,7 +541,7 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
 // A thread keeps its columns' sums in registers over all rows of its workgroup.  FOLD (a gate with more rows than there are
 // workgroups): a workgroup takes whole rows of the gate, writes their dgate at once and folds the rest into sums of its own.
 constexpr int kPreOnly = 0, kRms = 1, kLayer = 2;  // SUMS: no norm behind the branch, none of the norms a layer norm, others
-template <typename T, int TPR, int NV, int MAXT, int SUMS, bool BIAS, bool FOLD>
+template <typename T, int TPR, int NV, int MAXT, int SUMS, bool BIAS, bool FOLD, bool WHOLE>
 __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
 {
     constexpr int VW = RowIO<T>::VW, K = SUMS == kPreOnly ? 2 : SUMS == kRms ? 3 : 8, ACC = BIAS ? 4 : 2;
@@ -503,39 +551,73 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
     const Place<TPR> at(a.waves);
     RowSum<TPR, K> sum(red, a.waves, at.slot);
     const float inv_c = 1.f / (float)a.C;
+    const uint32_t row_bytes = (uint32_t)a.C * (uint32_t)sizeof(T);
     const bool pre = a.pre != DSP_NORM_NONE, post = POST && a.post != DSP_NORM_NONE, has_dy = a.dy != nullptr, has_z = a.z != nullptr;
     int c[NV];
-    float w[NV][VW], gpre[NV][VW], p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
+    float w[NV][VW], act[NV][VW], dact[NV][VW], gpost[NV][VW], bpost[NV][VW], gpre[NV][VW], p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         c[k] = (at.t + k * at.threads) * VW;
         load_vector(a.pre_gain, c[k], a.C, gpre[k], 1.f);
+        load_vector(a.post_gain, c[k], a.C, gpost[k], 1.f);
+        if (FOLD && BIAS) load_vector(a.post_bias, c[k], a.C, bpost[k], 0.f);
 #pragma unroll
         for (int e = 0; e < VW; ++e) p1[k][e] = p2[k][e] = s1[k][e] = s2[k][e] = f1[k][e] = f2[k][e] = 0.f;
     }
-    // w of a row of the gate
+    // A row of the gate: fetched as it lies (where its type is the rows'), and w of it
+    const bool raw_gate = a.gate_rows > 0 && (sizeof(T) == 4 || !a.gate_f32);
+    Raw<T> rg[NV];
+    auto fetch_gate = [&](int64_t group) {
+        if (WHOLE) {
+            const auto r = row_rsrc(a.gate, group * a.gs * (int)sizeof(T), row_bytes, raw_gate && group < a.groups);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) rg[k] = load_rsrc<T>(r, c[k]);
+            return;
+        }
+        if (!raw_gate) return;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) rg[k] = load_raw<T>((const T*)a.gate + min(group, (int64_t)a.groups - 1) * a.gs, c[k], a.C, k + 1 < NV);
+    };
     auto weights = [&](int64_t group) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float g[VW];
-            load_vector(a.post_gain, c[k], a.C, w[k], 1.f);
-            if (a.gate_rows) load_gate<T>(a.gate, a.gate_f32, group * a.gs, c[k], a.C, g);
+            if (raw_gate || (FOLD && WHOLE)) RowIO<T>::unpack(rg[k], g);
+            else if (a.gate_rows) load_gate<T>(a.gate, a.gate_f32, min(group, (int64_t)a.groups - 1) * a.gs, c[k], a.C, g);
 #pragma unroll
-            for (int e = 0; e < VW; ++e) w[k][e] *= a.gate_rows ? a.beta * gate_act(a.act, g[e]) : a.beta;
+            for (int e = 0; e < VW; ++e) {
+                act[k][e] = 1.f;
+                if (a.gate_rows) gate_both(a.act, g[e], act[k][e], dact[k][e]);
+                act[k][e] *= a.beta;
+                w[k][e] = gpost[k][e] * act[k][e];
+            }
         }
     };
     Raw<T> rdh[NV], ry_[NV], rz_[NV], rdy[NV];
     float my = 0.f, ry = 0.f, mz = 0.f, rz = 1.f;  // 1 / deviations and the means times them
     auto fetch = [&](int64_t row) {
+        const bool there = row < a.M;
         row = min(row, (int64_t)a.M - 1);
+        if (WHOLE) {
+            constexpr int e = sizeof(T);
+            const auto rh = row_rsrc(a.dh, row * a.hs * e, row_bytes, pre && there), r1 = row_rsrc(a.y, row * a.ys * e, row_bytes, pre && there);
+            const auto r2 = row_rsrc(a.z, row * a.zs * e, row_bytes, has_z && there), r3 = row_rsrc(a.dy, row * a.ys * e, row_bytes, has_dy && there);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (pre) {
-                rdh[k] = load_raw<T>((const T*)a.dh + row * a.hs, c[k], a.C);
-                ry_[k] = load_raw<T>((const T*)a.y + row * a.ys, c[k], a.C);
+            for (int k = 0; k < NV; ++k) {
+                rdh[k] = load_rsrc<T>(rh, c[k]);
+                ry_[k] = load_rsrc<T>(r1, c[k]);
+                rz_[k] = load_rsrc<T>(r2, c[k]);
+                rdy[k] = load_rsrc<T>(r3, c[k]);
             }
-            if (has_z) rz_[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C);
-            if (has_dy) rdy[k] = load_raw<T>((const T*)a.dy + row * a.ys, c[k], a.C);
+        }
+#pragma unroll
+        for (int k = 0; k < NV && !WHOLE; ++k) {
+            if (pre) {
+                rdh[k] = load_raw<T>((const T*)a.dh + row * a.hs, c[k], a.C, k + 1 < NV);
+                ry_[k] = load_raw<T>((const T*)a.y + row * a.ys, c[k], a.C, k + 1 < NV);
+            }
+            if (has_z) rz_[k] = load_raw<T>((const T*)a.z + row * a.zs, c[k], a.C, k + 1 < NV);
+            if (has_dy) rdy[k] = load_raw<T>((const T*)a.dy + row * a.ys, c[k], a.C, k + 1 < NV);
         }
         if (pre) {
             ry = a.pre_stats[a.M + row];
@@ -557,12 +639,12 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
         for (int k = 0; k < NV; ++k) {
 #pragma unroll
             for (int e = 0; e < VW; ++e) dh[k][e] = yh[k][e] = zh[k][e] = q[k][e] = 0.f;
-            if (pre) {
+            if (WHOLE || pre) {
                 RowIO<T>::unpack(rdh[k], dh[k]);
                 RowIO<T>::unpack(ry_[k], yh[k]);
             }
-            if (has_z) RowIO<T>::unpack(rz_[k], zh[k]);
-            if (has_dy) RowIO<T>::unpack(rdy[k], q[k]);
+            if (WHOLE || has_z) RowIO<T>::unpack(rz_[k], zh[k]);
+            if (WHOLE || has_dy) RowIO<T>::unpack(rdy[k], q[k]);
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
                 yh[k][e] = yh[k][e] * ry - my;
@@ -594,6 +676,8 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
             t1 = (s[o % K] - r_y * (m1 * s[(o + 1) % K] + (LAYER ? m0 * s[4 % K] : 0.f))) * inv_c;
             if (LAYER && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - r_y * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
         }
+        const int64_t at_x = WHOLE ? row * a.xs * (int64_t)sizeof(T) : 0, at_z = WHOLE ? row * a.zs * (int64_t)sizeof(T) : 0;
+        const auto rx = row_rsrc(a.dx, at_x, row_bytes, WHOLE && live && a.dx), rzo = row_rsrc(a.dz, at_z, row_bytes, WHOLE && live && a.dz);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float dz[VW];
@@ -611,41 +695,45 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
                 dz[e] = POST ? r_z * (w[k][e] * D - t0 - zh[k][e] * t1) : w[k][e] * D;
                 q[k][e] = a.alpha * D;
             }
-            if (live && a.dx) store_run<T>((T*)a.dx + row * a.xs, c[k], a.C, q[k]);
-            if (live && a.dz) store_run<T>((T*)a.dz + row * a.zs, c[k], a.C, dz);
+            if (WHOLE) {
+                store_rsrc<T>(rx, c[k], q[k]);
+                store_rsrc<T>(rzo, c[k], dz);
+                continue;
+            }
+            if (live && a.dx) store_run<T>((T*)a.dx + row * a.xs, c[k], a.C, q[k], k + 1 < NV);
+            if (live && a.dz) store_run<T>((T*)a.dz + row * a.zs, c[k], a.C, dz, k + 1 < NV);
         }
     };
 
     if (FOLD) {
         const int64_t g0 = (int64_t)blockIdx.x * a.rows_per_part, g1 = min(g0 + a.rows_per_part, (int64_t)a.groups);
         fetch((g0 + at.slot) * a.gate_rows);
+        fetch_gate(g0 + at.slot);
         for (int64_t gb = g0; gb < g1; gb += at.slots) {
             const int64_t group = gb + at.slot;
-            const bool mine = group < g1;
-            weights(mine ? group : g1 - 1);
+            const bool mine = group < g1, more = gb + at.slots < g1;
+            weights(group);
             for (int i = 0; i < a.gate_rows; ++i) {
                 const int64_t row = group * a.gate_rows + i;
                 const bool last = i + 1 == a.gate_rows;
-                one_row(row, mine && row < a.M, !last ? row + 1 : gb + at.slots < g1 ? (group + at.slots) * a.gate_rows : -1);
+                if (last && more) fetch_gate(group + at.slots);
+                one_row(row, mine && row < a.M, !last ? row + 1 : more ? (group + at.slots) * a.gate_rows : -1);
             }
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                float g[VW], gain[VW], bias[VW];
-                load_gate<T>(a.gate, a.gate_f32, (mine ? group : g1 - 1) * a.gs, c[k], a.C, g);
-                load_vector(a.post_gain, c[k], a.C, gain, 1.f);
-                load_vector(a.post_bias, c[k], a.C, bias, 0.f);
+                float d[VW];
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
-                    const float act = a.beta * gate_act(a.act, g[e]);
-                    const float d = a.beta * gate_slope(a.act, g[e]) * (gain[e] * s1[k][e] + (BIAS ? bias[e] * s2[k][e] : 0.f));
-                    f1[k][e] += act * s1[k][e];
-                    f2[k][e] += act * s2[k][e];
+                    d[e] = a.beta * dact[k][e] * (gpost[k][e] * s1[k][e] + (BIAS ? bpost[k][e] * s2[k][e] : 0.f));
+                    f1[k][e] += act[k][e] * s1[k][e];
+                    if (BIAS) f2[k][e] += act[k][e] * s2[k][e];
                     s1[k][e] = s2[k][e] = 0.f;
-                    g[e] = d;
                 }
-                if (mine && a.dgate) {
-                    if (sizeof(T) == 4 || !a.gate_f32) store_run<T>((T*)a.dgate + group * a.gs, c[k], a.C, g);
-                    else store_vector((float*)a.dgate + group * a.gs, c[k], a.C, g);
+                if (WHOLE) {
+                    store_rsrc<T>(row_rsrc(a.dgate, group * a.gs * (int64_t)sizeof(T), row_bytes, mine && a.dgate), c[k], d);
+                } else if (mine && a.dgate) {
+                    if (sizeof(T) == 4 || !a.gate_f32) store_run<T>((T*)a.dgate + group * a.gs, c[k], a.C, d, k + 1 < NV);
+                    else store_vector((float*)a.dgate + group * a.gs, c[k], a.C, d);
                 }
             }
         }
@@ -655,6 +743,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
         const int64_t r0 = group * rows + (int64_t)part * a.rows_per_part;
         const int64_t r1 = min(min(r0 + a.rows_per_part, (group + 1) * rows), (int64_t)a.M);
         if (r0 < r1) {
+            fetch_gate(group);
             fetch(r0 + at.slot);
             weights(group);
         }
@@ -829,6 +918,7 @@ RowShape row_shape(int dtype, int C)
 {
     const int vw = dtype == DSP_BF16 ? 8 : 4, runs = ceil_div(C, vw);
     if (runs <= 8) return {8, 1, 1};
+    if (runs <= 16) return {16, 1, 1};
     if (runs <= 32) return {32, 1, 1};
     // eight elements a thread while a workgroup of 16 waves holds the row, sixteen then
     const int nv = (dtype == DSP_BF16 ? 1 : runs <= 64 ? 1 : 2) * (C <= 8192 ? 1 : 2);
@@ -906,6 +996,7 @@ int forward_t(const NormArgs& a, const RowShape& s, hipStream_t st, ProfScope& p
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.M, slots), 256 * std::max(1, 2048 / (int)block.x)));
 #define FWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_fwd_kernel<T, TPR, NV, MAXT>), grid, block, 0, st, a)
     if (s.tpr == 8) FWD(8, 1, kSubThreads);
+    else if (s.tpr == 16) FWD(16, 1, kSubThreads);
     else if (s.tpr == 32) FWD(32, 1, kSubThreads);
     else if (s.nv == 1) FWD(0, 1, 1024);
     else if (s.nv == 2) FWD(0, 2, 1024);
@@ -919,14 +1010,17 @@ template <typename T, int SUMS, bool BIAS, bool FOLD>
 int backward_t(const NormBackArgs& a, const RowShape& s, hipStream_t st, ProfScope& ps)
 {
     const dim3 grid(a.parts), block(s.tpr ? kSubThreads : 64 * s.waves * std::max(1, kBackWaves / s.waves));
-#define BWD(TPR, NV, MAXT) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, TPR, NV, MAXT, SUMS, BIAS, FOLD>), grid, block, 0, st, a)
+#define BWD(TPR, NV, MAXT, WHOLE) DSP_LAUNCH(ps, (norm_residual_bwd_kernel<T, TPR, NV, MAXT, SUMS, BIAS, FOLD, WHOLE>), grid, block, 0, st, a)
     constexpr int kNarrow = 64 * kBackWaves, kEight = sizeof(T) == 4 ? 2 : 1;  // kEight: runs of eight elements
-    if (s.tpr == 8) BWD(8, 1, kSubThreads);
-    else if (s.tpr == 32) BWD(32, 1, kSubThreads);
-    else if (s.nv < kEight) BWD(0, 1, kNarrow);
-    else if (s.nv == kEight && (int)block.x <= kNarrow) BWD(0, kEight, kNarrow);
-    else if (s.nv == kEight) BWD(0, kEight, 1024);
-    else BWD(0, 2 * kEight, 1024);
+    if (s.tpr == 8) BWD(8, 1, kSubThreads, false);
+    else if (s.tpr == 16) BWD(16, 1, kSubThreads, false);
+    else if (s.tpr == 32) BWD(32, 1, kSubThreads, false);
+    else if (s.nv < kEight) BWD(0, 1, kNarrow, false);
+    else if (s.nv == kEight && (int)block.x <= kNarrow) {
+        if (a.whole) BWD(0, kEight, kNarrow, true);
+        else BWD(0, kEight, kNarrow, false);
+    } else if (s.nv == kEight) BWD(0, kEight, 1024, false);
+    else BWD(0, 2 * kEight, 1024, false);
 #undef BWD
     DSP_HIP(hipGetLastError());
     return DSP_OK;
@@ -1027,6 +1121,9 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh
     a.alpha = d->alpha; a.beta = d->beta;
     const RowShape s = row_shape(d->dtype, d->C);
     a.waves = s.waves;
+    auto runs = [&](const void* q, int64_t stride) { return (uintptr_t)q % 16 == 0 && stride * e % 16 == 0; };
+    a.whole = d->C * e % 16 == 0 && runs(a.dh, a.hs) && runs(a.dy, a.ys) && runs(a.y, a.ys) && runs(a.z, a.zs) && runs(a.dx, a.xs) &&
+              runs(a.dz, a.zs) && (!d->gate_rows || (d->gate_dtype == d->dtype ? runs(a.gate, a.gs) && runs(a.dgate, a.gs) : !p.fold));
     hipStream_t st = (hipStream_t)stream;
     {
         const double n = (double)d->M * d->C;
