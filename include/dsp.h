@@ -279,7 +279,8 @@ int dsp_adamw_destroy(dsp_adamw* o);
  *     m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
  *     x <- x - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay x)    (the last term where decay != 0)
  * (beta^t: the product over the steps taken, should beta change.)  d_norm, unless NULL, receives the norm, also without a clip.
- * With max_norm > 0 a step whose norm is no finite number changes nothing but d_norm and is not counted.
+ * With max_norm > 0 a step whose norm is no finite number changes nothing but d_norm and is not counted.  (So a block's update then
+ * uses up the gradient and leaves the parameters.)
  * Wants lr, weight_decay, max_norm >= 0, 0 <= beta < 1, eps >= 1e-15 and the object's device to be the current one.  Launches
  * one kernel, or two with the norm; the step number is kept on the device, so that a captured step counts on in every replay (its
  * hyperparameters stay those of the capture).  Steps of one object must be ordered by the caller, on whatever streams.

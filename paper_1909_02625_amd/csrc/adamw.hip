@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 #include <new>
 #include <vector>
 
@@ -522,7 +523,7 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
         DSP_REQUIRE((uintptr_t)t.d_param % 4 == 0 && (uintptr_t)t.d_grad % gs == 0 && (uintptr_t)t.d_copy % 2 == 0 &&
                         (uintptr_t)t.d_m % ss == 0 && (uintptr_t)t.d_v % ss == 0,
                     DSP_EINVAL, "dsp_adamw_init: a buffer of tensor %d is not aligned to its elements", (int)j);
-        DSP_REQUIRE(t.n < (1ll << 40), DSP_EINVAL, "dsp_adamw_init: tensor %d is too large", (int)j);
+        DSP_REQUIRE(t.n < (1ll << 37), DSP_EINVAL, "dsp_adamw_init: tensor %d is too large", (int)j);
         const size_t n = (size_t)t.n, blocks = (n + kStateBlock - 1) / kStateBlock, chunk = chunk_elems(state_bits);
         auto range = [&](const void* p, size_t bytes, bool written) {
             if (p) ranges.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written});
@@ -600,7 +601,7 @@ int dsp_adamw_init(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t s
     try {
         o = new dsp_adamw();
         rc = adamw_build(n_tensors, tensors, state_bits, seed, o);
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         set_error("dsp_adamw_init: out of host memory");
     }
     if (rc != DSP_OK) {

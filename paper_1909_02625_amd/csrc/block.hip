@@ -1246,7 +1246,7 @@ int dsp_block_set_adamw(dsp_block* b, int32_t state_bits, uint64_t seed)
         DSP_TRY(dsp_adamw_init((int32_t)t.size(), t.data(), state_bits, seed, &b->adamw));
         b->adamw_state = state;
         b->adamw_bytes = bytes;
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         set_error("dsp_block_set_adamw: out of host memory");
         return DSP_ENOMEM;
     }

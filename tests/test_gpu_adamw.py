@@ -145,6 +145,40 @@ def test_many_small_tensors_and_a_large_one(bits):
     m.check(1)
 
 
+def test_more_elements_than_32_bits_count():
+    """Elements on both sides of 2^32 of one tensor, and its last ones."""
+    n = (1 << 32) + 70001
+    x, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    me, ve = (torch.zeros(-(-n // 256), dtype=torch.uint8, device="cuda") for _ in range(2))
+    rng = np.random.default_rng(8)
+    places = [(0, 2560), ((1 << 31) - 512, 1024), ((1 << 32) - 1024, 2048), (n // 256 * 256 - 2048, n - n // 256 * 256 + 2048)]
+    host = []
+    for at, k in places:
+        a = torch.from_numpy(rng.standard_normal(k).astype(np.float32)).bfloat16()
+        g[at:at + k] = a.cuda()
+        host.append(a.float().numpy())
+    o = D.dsp_adamw_init([{"param": x, "grad": g, "m": m, "v": v, "m_exp": me, "v_exp": ve}], 8, 77)
+    norm = torch.zeros(1, device="cuda")
+    D.dsp_adamw_step(o, 1e-3, d_norm=norm)
+    torch.cuda.synchronize()
+    D.dsp_adamw_destroy(o)
+    total = P.clip_factor(host, 0)[0]
+    assert abs(float(norm) - total) <= 2 * U * total
+    for (at, k), a in zip(places, host):
+        low, high = P.random_halves(77, 1, 0, k, first=at)
+        m32, v32 = P.moments_fp32(a, np.zeros(k), np.zeros(k), 0.9, 0.999)
+        for code, exp, val, r, args in ((m, me, m32, low, (3, 7, 7, False)), (v, ve, v32, high, (2, 15, 14, True))):
+            c, e = P.encode(val, r, *args)
+            np.testing.assert_array_equal(code[at:at + k].cpu().numpy(), c)
+            np.testing.assert_array_equal(exp[at // 256:at // 256 + e.size].cpu().numpy(), e)
+        # the first step of AdamW is lr g / |g| (1 - eps / |g| ...): 20 roundings
+        ref = -1e-3 * a / (np.abs(a.astype(np.float64)) + 1e-8)
+        assert np.abs(x[at:at + k].cpu().numpy() - ref).max() <= 20 * U * 1e-3
+    at, k = places[1]
+    assert not x[at + k:at + k + 4096].any() and not m[at + k:at + k + 4096].any()
+
+
 def test_new_moments_of_8_bits():
     """From zero moments: every code stands for one of the two neighbours of its value, and none is favoured."""
     n = 1 << 20

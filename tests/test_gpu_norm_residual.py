@@ -169,6 +169,41 @@ def test_more_rows_of_the_gate_than_workgroups(M, C, rows, dtype):
     run(problem(M, C, dtype, 1, 2, (rows, dtype), 1, "both"), dtype)
 
 
+@pytest.mark.parametrize("C", [64, 1024])
+def test_rows_whose_offsets_pass_32_bits(C):
+    """Rows 20000 elements apart in tensors of 4.4e9: the first and the last ones against a call on those alone."""
+    M, stride, td = 220000, 20000, torch.bfloat16
+    wide = [torch.empty(M, stride, dtype=td, device="cuda")[:, :C] for _ in range(6)]   # x, z, y, h, then dx, dz
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for w in wide[:2]:
+        w.copy_(torch.randn(M, C, generator=gen, device="cuda"))
+    gate = torch.randn(M, C, generator=gen, device="cuda").to(td)
+    gain = torch.ones(C, device="cuda")
+    desc = lambda m, s: D.make_norm_residual_desc(m, C, D.DSP_BF16, 1, 2, 1.0, 0.5, EPS, 1, 1, None, s, s, s, s, C)  # noqa: E731
+    stats = [torch.empty(2, M, device="cuda") for _ in range(2)]
+    x, z, y, h, dx, dz = wide
+    D.dsp_norm_residual_forward(desc(M, stride), x, z, gate, gain, None, gain, None, y, h, *stats)
+    dgate = torch.empty_like(gate)
+    ws = torch.empty(D.dsp_norm_residual_workspace_bytes(desc(M, stride)), dtype=torch.uint8, device="cuda")
+    D.dsp_norm_residual_backward(desc(M, stride), h, x, y, z, gate, gain, None, gain, *stats, dx, dz, dgate, d_workspace=ws,
+                                 workspace_bytes=ws.numel())
+    torch.cuda.synchronize()
+    for rows in (slice(0, 50), slice(M - 50, M)):
+        small = [w[rows].contiguous() for w in (x, z, gate)]
+        out = [torch.empty(50, C, dtype=td, device="cuda") for _ in range(5)]
+        st = [torch.empty(2, 50, device="cuda") for _ in range(2)]
+        D.dsp_norm_residual_forward(desc(50, 0), *small, gain, None, gain, None, out[0], out[1], *st)
+        D.dsp_norm_residual_backward(desc(50, 0), out[1], small[0], out[0], small[1], small[2], gain, None, gain, *st, out[2], out[3], out[4],
+                                     d_workspace=ws, workspace_bytes=ws.numel())
+        torch.cuda.synchronize()
+        for big, alone in zip((y, h, dx, dz, dgate), out):
+            a, b = big[rows].float(), alone.float()
+            # another row shape adds a row's elements up in another order: 200 U of a sum, and then the other bf16 neighbour
+            assert (a - b).abs().max() <= 2.0 ** -7 * b.abs().max() and (a != b).float().mean() < 0.05
+    for w in wide[2:]:
+        assert torch.isfinite(w[::997]).all()
+
+
 def test_rows_far_from_zero_keep_their_variance():
     run(problem(64, 1000, "fp32", 2, 2, None, 0, "both", shift=100.0), "fp32")
 
