@@ -3,7 +3,9 @@
 //   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  x <- x - lr ((m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps) + wd x)
 //
 // Every element is touched once: parameters and states in and out, the gradient in, the bf16 copy out.  The tensors are cut
-// into chunks of 4096 elements at init; a workgroup finds all addresses of its chunk in one table entry.
+// into chunks at init; a workgroup finds all addresses of its chunk in one table entry.  Memory bounds it: 270 M parameters with
+// bf16 gradients and copies take 1.35 ms with states of 32 bits (5.6 TB/s, where a copy of 4 GiB reaches 4.9) and 0.81 ms with 8
+// (5.35 TB/s; vector instructions fill half of that time), the norm of their gradients 0.115 ms (4.7 TB/s).
 #include "common.h"
 
 #include <string.h>
@@ -22,7 +24,8 @@ constexpr int kThreads = 256;
 constexpr int kStateBlock = 256;                      // elements that share a power of two: one wave, four elements a lane
 constexpr int kRow = kThreads * 4;                    // elements of a workgroup's quads side by side: four of those blocks
 static_assert(kStateBlock == 64 * 4, "a wave's quad is a block of the 8-bit states");
-// Quads a thread has in flight.
+// Quads a thread has in flight, all loaded before the first is used.  (270 M parameters, us: 32 bits with 2, 4, 8 quads 1646, 1348, 1397;
+// 8 bits 1800, 970, 941; 1024 or 2048 workgroups that go through all chunks 1500 and 1045 to 1117.)
 constexpr int quads(int bits) { return bits == 8 ? 8 : 4; }
 constexpr int chunk_elems(int bits) { return kRow * quads(bits); }
 constexpr int kNormThreads = 1024;                    // workgroup of the gradient norm
@@ -70,6 +73,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32u __attribute__((aligned(1)));
 
 // What a step touches once: a model's parameters and states pass through the caches, nothing of them is there at the next step.
+// (270 M parameters: 1464 -> 1340 us, 8 bits 1017 -> 941; 11 M parameters, which the last cache holds in part: 105 -> 90.)
 template <typename V>
 __device__ inline V stream_load(const void* p) { return __builtin_nontemporal_load((const GLOBAL V*)p); }
 template <typename V>
@@ -316,7 +320,7 @@ __device__ inline double block_sum(double v, double (&red)[WAVES])
     return v;
 }
 
-// Partial sums of squares of all gradients.  Squares are exact in fp64 and every workgroup takes its chunks in order, as the
+// Partial sums of squares of all gradients, 16 bytes a load whatever their type.  Squares are exact in fp64 and every workgroup takes its chunks in order, as the
 // update kernel takes the partial sums: the same bits every time.
 template <int BITS>
 __global__ __launch_bounds__(kNormThreads) void adamw_norm_kernel(const AdamwChunk* __restrict__ chunks, int n_chunks,
