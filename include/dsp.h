@@ -588,8 +588,9 @@ int dsp_norm_residual_forward(const dsp_norm_residual_desc* desc, const void* d_
  * dgate = sum beta act'(gate) n D over the rows of each row of the gate, and the gradients of gains and biases; of these outputs
  * NULL ones are not formed.  d_y: y as the forward pass left it; d_z is needed for dgate and with a norm behind the branch.
  * d_dx may be d_dy, d_dz may be d_z (same strides).  d_workspace: dsp_norm_residual_workspace_bytes() bytes (whatever is asked
- * for: that many are enough), 16-byte aligned, contents unspecified before and after; NULL and 0 if no gradient of a
- * parameter is asked for.  Sums are taken in a fixed order: the same call gives the same bits.
+ * for: that many are enough), 16-byte aligned, contents unspecified before and after (calls that may run at the same time, replays
+ * of captured ones among them, need one each); NULL and 0 if no gradient of a parameter is asked for.  Sums are taken in a
+ * fixed order: the same call gives the same bits.
  */
 int dsp_norm_residual_workspace_bytes(const dsp_norm_residual_desc* desc, size_t* bytes);
 int dsp_norm_residual_backward(const dsp_norm_residual_desc* desc, const void* d_dh, const void* d_dy, const void* d_y,

@@ -4,8 +4,8 @@
 //
 // Every element is touched once: parameters and states in and out, the gradient in, the bf16 copy out.  The tensors are cut
 // into chunks at init; a workgroup finds all addresses of its chunk in one table entry.  Memory bounds it: 270 M parameters with
-// bf16 gradients and copies take 1.35 ms with states of 32 bits (5.6 TB/s, where a copy of 4 GiB reaches 4.9) and 0.81 ms with 8
-// (5.35 TB/s; vector instructions fill half of that time), the norm of their gradients 0.115 ms (4.7 TB/s).
+// bf16 gradients and copies take 1.34 ms with states of 32 bits (5.7 TB/s, where a copy of 4 GiB reaches 4.9) and 0.75 ms with 8
+// (5.75 TB/s; vector instructions fill half of that time), the norm of their gradients 0.115 ms (4.7 TB/s).
 #include "common.h"
 
 #include <string.h>
@@ -24,9 +24,10 @@ constexpr int kThreads = 256;
 constexpr int kStateBlock = 256;                      // elements that share a power of two: one wave, four elements a lane
 constexpr int kRow = kThreads * 4;                    // elements of a workgroup's quads side by side: four of those blocks
 static_assert(kStateBlock == 64 * 4, "a wave's quad is a block of the 8-bit states");
-// Quads a thread has in flight, all loaded before the first is used.  (270 M parameters, us: 32 bits with 2, 4, 8 quads 1646, 1348, 1397;
-// 8 bits 1800, 970, 941; 1024 or 2048 workgroups that go through all chunks 1500 and 1045 to 1117.)
-constexpr int quads(int bits) { return bits == 8 ? 8 : 4; }
+// Quads a thread has in flight, all loaded before the first is used.  (270 M parameters, us: 32 bits with 2, 3, 4, 5, 8 quads 1646, 1369,
+// 1341, 1390, 1397; 8 bits with the norm and 4, 5, 6, 7, 8 quads 940, 896, 867, 919, 907: six leave registers for four waves a SIMD.
+// 1024 or 2048 workgroups that go through all chunks are slower by 2 to 15 %.)
+constexpr int quads(int bits) { return bits == 8 ? 6 : 4; }
 constexpr int chunk_elems(int bits) { return kRow * quads(bits); }
 constexpr int kNormThreads = 1024;                    // workgroup of the gradient norm
 constexpr int kNormBlocks = 512;                      // most of its workgroups: two fill a compute unit
@@ -328,7 +329,7 @@ __global__ __launch_bounds__(kNormThreads) void adamw_norm_kernel(const AdamwChu
 {
     __shared__ double red[kNormThreads / 64];
     double s = 0.0;
-    constexpr int kRuns = chunk_elems(BITS) * 4 / (kNormThreads * 16);  // of 16 bytes a thread, at most
+    constexpr int kRuns = (chunk_elems(BITS) * 4 + kNormThreads * 16 - 1) / (kNormThreads * 16);  // of 16 bytes a thread, at most
     for (int k = blockIdx.x; k < n_chunks; k += gridDim.x * kNormRows) {
         u32x4 raw[kNormRows][kRuns];
         int left[kNormRows][kRuns];  // elements of the run in the chunk
@@ -541,7 +542,9 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
             range(t.d_m_exp, blocks, true);
             range(t.d_v_exp, blocks, true);
         }
-        for (size_t at = 0; at < n; at += chunk) {
+        constexpr size_t kWord = (size_t)1 << 32;  // (a chunk does not pass a multiple: the upper half of its elements' numbers is one)
+        for (size_t at = 0, len = 0; at < n; at += len) {
+            len = std::min(std::min(chunk, n - at), kWord - at % kWord);
             AdamwChunk c = {};
             c.x = t.d_param + at;
             c.g = (const char*)t.d_grad + gs * at;
@@ -552,7 +555,7 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
                 c.m_exp = t.d_m_exp + at / kStateBlock;
                 c.v_exp = t.d_v_exp + at / kStateBlock;
             }
-            c.n = (int32_t)std::min(chunk, n - at);
+            c.n = (int32_t)len;
             c.flags = (t.decay ? kDecay : 0) | (t.grad_dtype == DSP_BF16 ? kGradBf16 : 0);
             c.tensor = (uint32_t)j;
             c.first_lo = (uint32_t)at;

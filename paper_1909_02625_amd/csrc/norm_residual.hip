@@ -684,6 +684,15 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
             t1 = (s[o % K] - r_y * (m1 * s[(o + 1) % K] + (LAYER ? m0 * s[4 % K] : 0.f))) * inv_c;
             if (LAYER && a.post == DSP_NORM_LAYER) t0 = (s[5 % K] - r_y * (m1 * s[6 % K] + m0 * s[7 % K])) * inv_c;
         }
+        if (!WHOLE && TPR == 0) {  // the next row's runs are there before this one's stores: the wait for them is none for the stores
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                rdh[k] = hold<T>(rdh[k]);
+                ry_[k] = hold<T>(ry_[k]);
+                rz_[k] = hold<T>(rz_[k]);
+                rdy[k] = hold<T>(rdy[k]);
+            }
+        }
         const int64_t at_x = WHOLE ? row * a.xs * (int64_t)sizeof(T) : 0, at_z = WHOLE ? row * a.zs * (int64_t)sizeof(T) : 0;
         const auto rx = row_rsrc(a.dx, at_x, row_bytes, WHOLE && live && a.dx), rzo = row_rsrc(a.dz, at_z, row_bytes, WHOLE && live && a.dz);
 #pragma unroll

@@ -204,6 +204,16 @@ def test_rows_whose_offsets_pass_32_bits(C):
         assert torch.isfinite(w[::997]).all()
 
 
+@pytest.mark.parametrize("dtype,C", [("bf16", c) for c in (300, 1024, 1499, 2048, 2500, 2904, 3500, 4096)] +
+                         [("fp32", c) for c in (200, 500, 700, 1024, 1100, 1301, 1700, 2048)])
+def test_every_number_of_runs_a_lane(dtype, C):
+    """From 1024 rows on the forward pass takes a row a wave, one to eight runs a lane; the backward pass many rows a workgroup."""
+    M = 1030 + C % 7
+    run(problem(M, C, dtype, 2, 1, (1, dtype), 2, "both"), dtype)
+    run(problem(M, C, dtype, 1, 2, (M, "fp32"), 1, "gain"), dtype, pad=8)
+    run(problem(M, C, dtype, 0, 1, (300, dtype), 0, "none"), dtype, pad=1 if C % 2 else 0)
+
+
 def test_rows_far_from_zero_keep_their_variance():
     run(problem(64, 1000, "fp32", 2, 2, None, 0, "both", shift=100.0), "fp32")
 
