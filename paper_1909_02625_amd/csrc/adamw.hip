@@ -321,8 +321,8 @@ __device__ inline double block_sum(double v, double (&red)[WAVES])
     return v;
 }
 
-// Partial sums of squares of all gradients, 16 bytes a load whatever their type.  Squares are exact in fp64 and every workgroup takes its chunks in order, as the
-// update kernel takes the partial sums: the same bits every time.
+// Partial sums of squares of all gradients, 16 bytes a load whatever their type.  Squares are exact in fp64 and every workgroup takes
+// its chunks in order, as the update kernel takes the partial sums: the same bits every time.
 template <int BITS>
 __global__ __launch_bounds__(kNormThreads) void adamw_norm_kernel(const AdamwChunk* __restrict__ chunks, int n_chunks,
                                                                   double* __restrict__ partial)

@@ -562,7 +562,9 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
     const uint32_t row_bytes = (uint32_t)a.C * (uint32_t)sizeof(T);
     const bool pre = a.pre != DSP_NORM_NONE, post = POST && a.post != DSP_NORM_NONE, has_dy = a.dy != nullptr, has_z = a.z != nullptr;
     int c[NV];
-    float w[NV][VW], act[NV][VW], dact[NV][VW], gpost[NV][VW], bpost[NV][VW], gpre[NV][VW], p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
+    // act: beta act(gate), dact: act'(gate); f: the sums S over the rows of the gate that are done, times act (FOLD)
+    float w[NV][VW], act[NV][VW], dact[NV][VW], gpost[NV][VW], bpost[NV][VW], gpre[NV][VW];
+    float p1[NV][VW], p2[NV][VW], s1[NV][VW], s2[NV][VW], f1[NV][VW], f2[NV][VW];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         c[k] = (at.t + k * at.threads) * VW;

@@ -3,8 +3,9 @@
 U = 2^-24 is half a step of fp32, E half a step of the storage type relative to the value.  A row's sums run over at most 64
 elements a lane, 6 levels of a wave and 16 waves: 86 additions, so a sum is off by at most 90 U of its terms' magnitudes, a
 statistic by half of that and its own roundings; what an element takes from two statistics, a product of up to 8 factors and a
-rational activation (tanh, exp: 4 U each) is off by at most 256 U of the magnitudes of its terms.  Sums over rows add the rows of a
-workgroup, then at most 1024 / 16 parts a wave and 16 waves (or a row of the gate's parts, as many): n + 96 additions, n = rows of a workgroup."""
+rational activation (tanh, exp: 4 U each) is off by at most 256 U of the magnitudes of its terms.  Sums over rows add n rows a lane
+(n at most 4, the rows over 512 workgroups or those of a row of the gate), up to 64 rows side by side, then 512 / 16 parts a wave and 16
+waves: n + 116 additions."""
 import numpy as np
 import pytest
 import torch
@@ -126,8 +127,8 @@ def run(p, dtype, pad=0, off=0, stream=None):
     ref = P.backward(p, gy, p["dy"], p["dh"], st[1], st[0])
     for name, got in (("x", dx), ("z", dz)):
         within(got.get(), ref[name], E * np.abs(ref[name]) + 400 * U * ref[name + "~"] + 1e-40, "d" + name)
-    rows = -(-M // 1024) * 1.0 + (p["gate_rows"] if p["gate"] is not None and p["gate_rows"] < M else 0)
-    chain = (min(rows, M) + 96 + 400) * U
+    rows = 4 + -(-M // 512) + (p["gate_rows"] if p["gate"] is not None and p["gate_rows"] < M else 0)
+    chain = (min(rows, M) + 116 + 400) * U
     if gt:
         within(dgate.get(), ref["gate"], gt[2] * np.abs(ref["gate"]) + chain * ref["gate~"] + 1e-40, "dgate")
     assert (ws[nbytes:] == 77).all(), "written behind the workspace"
