@@ -1084,7 +1084,7 @@ int dsp_norm_residual_forward(const dsp_norm_residual_desc* d, const void* d_x, 
     NormArgs a;
     a.x = d_x; a.z = d_z; a.gate = d_gate;
     a.post_gain = post ? d_post_gain : nullptr; a.post_bias = post ? d_post_bias : nullptr;
-    a.pre_gain = d_pre_gain; a.pre_bias = d_pre_bias;
+    a.pre_gain = pre ? d_pre_gain : nullptr; a.pre_bias = pre ? d_pre_bias : nullptr;
     a.y = d_y; a.h = d_h; a.post_stats = d_post_stats; a.pre_stats = d_pre_stats;
     a.xs = stride_of(d->x_stride, d->C); a.zs = stride_of(d->z_stride, d->C); a.ys = stride_of(d->y_stride, d->C);
     a.hs = stride_of(d->h_stride, d->C); a.gs = stride_of(d->gate_stride, d->C);

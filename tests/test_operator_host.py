@@ -1,0 +1,71 @@
+"""Host code of AdamW and of the norm-gate-residual entry points on a runtime of host memory (host_launches.cpp), each test in a process of
+its own: nothing is computed, but what the library allocates and hands to its kernels can be seen."""
+import ctypes
+import os
+import subprocess
+import sys
+import types
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def runtime(tmp_path_factory):
+    """The stand-in under the name and symbol versions the library asks for."""
+    d = tmp_path_factory.mktemp("runtime")
+    lib, ver = str(d / "libamdhip64.so.7"), str(d / "versions")
+    with open(ver, "w") as f:
+        f.write("hip_4.2 { global: *; };\nhip_4.3 { global: hipGraph*; hipStreamBeginCapture; hipStreamEndCapture; } hip_4.2;\n")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-pthread", "-Wl,-soname,libamdhip64.so.7",
+                    "-Wl,--version-script," + ver, os.path.join(ROOT, "tests", "host_launches.cpp"), "-o", lib], check=True)
+    return lib
+
+
+CASES = {}
+
+
+def case(f):
+    """Makes `f(rt, D)` a test that runs in a process whose HIP runtime is the stand-in `rt`."""
+    CASES[f.__name__] = f
+    return f
+
+
+A = 1 << 20  # an address; nothing is read there
+
+
+@case
+def norm_forward_ignores_gains_of_a_norm_that_is_none(rt, D):
+    """The addresses of what is ignored do not reach a kernel, those of what is used do; rows of every kind of kernel."""
+    for dtype in (D.DSP_FP32, D.DSP_BF16):
+        for M, C in ((5, 40), (5, 700), (3, 9000), (5000, 1000)):
+            for post in (0, 1, 2):
+                for pre in (0, 1, 2):
+                    d = D.make_norm_residual_desc(M, C, dtype, post, pre)
+                    rt.host_launches_keep(128)  # (the pointers and strides that a launch's one argument begins with)
+                    D.dsp_norm_residual_forward(d, A, 2 * A, None, 3 * A, 4 * A, 5 * A, 6 * A, 7 * A, 8 * A if pre else None, stream=0)
+                    assert rt.host_launches_kept() == 1
+                    holds = [bool(rt.host_launches_holds(0, i * A)) for i in range(1, 8)]
+                    assert holds == [True, True, post > 0, post > 0, pre > 0, pre > 0, True], (dtype, M, C, post, pre, holds)
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_on_the_host(runtime, name):
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), runtime, name], capture_output=True, text=True, timeout=100, cwd=ROOT)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+def _main(path, name):
+    rt = ctypes.CDLL(path, mode=ctypes.RTLD_GLOBAL)  # before the library, which then takes it for the HIP runtime
+    rt.host_launches_holds.argtypes = [ctypes.c_int, ctypes.c_uint64]
+    rt.host_launches_keep.argtypes = [ctypes.c_size_t]
+    rt.host_launches_bytes_held.restype = rt.host_launches_synchronised.restype = ctypes.c_int64
+    sys.path.insert(0, ROOT)
+    sys.modules["torch"] = types.ModuleType("torch")  # the binding imports it for the sake of that runtime alone
+    import paper_1909_02625_amd as D
+    CASES[name](rt, D)
+
+
+if __name__ == "__main__":
+    _main(*sys.argv[1:])
