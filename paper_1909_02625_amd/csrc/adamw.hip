@@ -482,10 +482,13 @@ void adamw_free(dsp_adamw* o)
 int adamw_upload(dsp_adamw* o, const std::vector<AdamwChunk>& chunks)
 {
     DSP_HIP(hipGetDevice(&o->device));
-    DSP_REQUIRE(hipMalloc((void**)&o->clock, sizeof(AdamwClock)) == hipSuccess &&
-                    hipMalloc((void**)&o->partial, kNormBlocks * sizeof(double)) == hipSuccess &&
-                    hipMalloc((void**)&o->chunks, chunks.size() * sizeof(AdamwChunk)) == hipSuccess,
-                DSP_ENOMEM, "dsp_adamw_init: out of device memory");
+    if (hipMalloc((void**)&o->clock, sizeof(AdamwClock)) != hipSuccess ||
+        hipMalloc((void**)&o->partial, kNormBlocks * sizeof(double)) != hipSuccess ||
+        hipMalloc((void**)&o->chunks, chunks.size() * sizeof(AdamwChunk)) != hipSuccess) {
+        (void)hipGetLastError();  // (see DSP_HIP)
+        set_error("dsp_adamw_init: out of device memory");
+        return DSP_ENOMEM;
+    }
     AdamwClock clock = {};
     clock.p1 = clock.p2 = 1.0;
     DSP_HIP(hipMemcpy(o->clock, &clock, sizeof(clock), hipMemcpyHostToDevice));

@@ -211,6 +211,7 @@ static int dev_alloc(dsp_block* b, void** p, size_t bytes, size_t* counter)
     if (bytes == 0) bytes = 16;
     hipError_t e = hipMalloc(p, bytes);
     if (e != hipSuccess) {
+        (void)hipGetLastError();  // (see DSP_HIP)
         set_error("hipMalloc(%zu) failed: %s", bytes, hipGetErrorString(e));
         return DSP_ENOMEM;
     }

@@ -4596,6 +4596,7 @@ int wgrad_reduce_set_create(const WgradReduceItem* items, int n, WgradReduceSet*
     if (s->n_tasks > 0) {
         if (hipMalloc((void**)&s->d_tasks, tasks.size() * sizeof(ReduceTask)) != hipSuccess ||
             hipMemcpy(s->d_tasks, tasks.data(), tasks.size() * sizeof(ReduceTask), hipMemcpyHostToDevice) != hipSuccess) {
+            (void)hipGetLastError();  // (see DSP_HIP)
             set_error("wgrad_reduce_set_create: device table allocation failed");
             if (s->d_tasks) (void)hipFree(s->d_tasks);
             delete s;

@@ -307,7 +307,11 @@ int dsp_pipeline_destroy(dsp_pipeline* pl)
 static int pl_alloc(dsp_pipeline* pl, void** p, size_t bytes)
 {
     hipError_t e = hipMalloc(p, bytes ? bytes : 16);
-    DSP_REQUIRE(e == hipSuccess, DSP_ENOMEM, "dsp_pipeline_init: hipMalloc(%zu) failed: %s", bytes, hipGetErrorString(e));
+    if (e != hipSuccess) {
+        (void)hipGetLastError();  // (see DSP_HIP)
+        set_error("dsp_pipeline_init: hipMalloc(%zu) failed: %s", bytes, hipGetErrorString(e));
+        return DSP_ENOMEM;
+    }
     pl->allocs.push_back(*p);
     return DSP_OK;
 }

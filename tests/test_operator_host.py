@@ -50,6 +50,68 @@ def norm_forward_ignores_gains_of_a_norm_that_is_none(rt, D):
                     assert holds == [True, True, post > 0, post > 0, pre > 0, pre > 0, True], (dtype, M, C, post, pre, holds)
 
 
+@case
+def adamw_out_of_memory_leaves_nothing_behind(rt, D):
+    """Whichever allocation is refused: an error, no memory kept, and none of it reported by the next launch."""
+    buffers = [ctypes.c_void_p() for _ in range(4)]
+    for b in buffers:
+        rt.hipMalloc(ctypes.byref(b), ctypes.c_size_t(4000))
+    t = D.dsp_adamw_tensor(*[b.value for b in buffers[:2]], 0, *[b.value for b in buffers[2:]], 0, 0, 1000, D.DSP_FP32, 1)
+    out, held = ctypes.c_void_p(), rt.host_launches_bytes_held()
+    for n in range(3):
+        rt.host_launches_refuse_malloc(n)
+        assert D.lib().dsp_adamw_init(1, ctypes.byref(t), 32, 0, ctypes.byref(out)) == 3 and not out.value, n
+        assert rt.host_launches_bytes_held() == held
+        D.dsp_norm_residual_forward(D.make_norm_residual_desc(5, 40, D.DSP_FP32, 0, 1), A, None, d_h=A, stream=0)
+    assert D.lib().dsp_adamw_init(1, ctypes.byref(t), 32, 0, ctypes.byref(out)) == 0
+    D.dsp_adamw_step(out.value, 1e-3, max_norm=1.0, stream=0)
+    D.dsp_adamw_destroy(out.value)
+    assert rt.host_launches_bytes_held() == held
+
+
+def _blocks(D, n=1):
+    """Blocks of a small network, as for a pipeline without delays."""
+    import numpy as np
+    from workloads import flatten_params, get_config, make_params
+    cfg = get_config("tiny2")
+    rng, shape, blocks = np.random.default_rng(0), tuple(cfg["input"]), []
+    for k, layers in enumerate(cfg["blocks"][:n]):
+        desc, keep = D.make_block_desc(layers, shape, D.DSP_BF16, k, n, 0, p_prev=0, needs_input_grad=k > 0)
+        blocks.append(D.dsp_block_init(desc, flatten_params(layers, make_params(layers, rng))))
+        shape = D.dsp_block_output_shape(blocks[-1])[0]
+    return blocks
+
+
+def _until_it_has_memory(rt, D, call):
+    """`call` with its first, second, .. allocation refused until it needs no more; returns what it gives then."""
+    held = rt.host_launches_bytes_held()
+    for n in range(1000):
+        rt.host_launches_refuse_malloc(n)
+        try:
+            out = call()
+        except D.DSPError as e:
+            assert e.status == 3
+            assert rt.host_launches_bytes_held() == held, n
+            D.dsp_norm_residual_forward(D.make_norm_residual_desc(5, 40, D.DSP_FP32, 0, 1), A, None, d_h=A, stream=0)
+            continue
+        rt.host_launches_refuse_malloc(-1)
+        assert n > 0
+        return out
+
+
+@case
+def blocks_and_pipelines_out_of_memory_leave_nothing_behind(rt, D):
+    held = rt.host_launches_bytes_held()
+    (b,) = _until_it_has_memory(rt, D, lambda: _blocks(D))
+    D.dsp_block_destroy(b)
+    blocks = _blocks(D, 2)
+    pl = _until_it_has_memory(rt, D, lambda: D.dsp_pipeline_init(blocks, (0, 0), (0, 0), 0.1, 0.9, 0.0, 4))
+    D.dsp_pipeline_destroy(pl)
+    for b in blocks:
+        D.dsp_block_destroy(b)
+    assert rt.host_launches_bytes_held() == held
+
+
 @pytest.mark.parametrize("name", CASES)
 def test_on_the_host(runtime, name):
     r = subprocess.run([sys.executable, os.path.abspath(__file__), runtime, name], capture_output=True, text=True, timeout=100, cwd=ROOT)
