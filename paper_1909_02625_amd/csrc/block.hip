@@ -1208,50 +1208,62 @@ int dsp_param_update(dsp_block* b, float lr, float momentum, float weight_decay,
     return dsp_param_update_sum(b, lr, momentum, 0, weight_decay, stream);
 }
 
+// The moments and the update over them; what has been allocated stays in b->allocs should it fail.
+static int block_add_adamw(dsp_block* b, int32_t state_bits, uint64_t seed)
+{
+    constexpr size_t kBlock = 256;
+    const size_t es = state_bits == 8 ? 1 : 4;
+    std::vector<dsp_adamw_tensor> t;
+    std::vector<size_t> at;
+    size_t blocks = 0;
+    for (const ParamRun& r : b->runs) {  // (whole blocks of the 8-bit states for every run)
+        at.push_back(blocks);
+        blocks += (r.n + kBlock - 1) / kBlock;
+    }
+    const size_t moment = blocks * kBlock * es, bytes = 2 * moment + (state_bits == 8 ? 2 * blocks : 0);
+    char* state = nullptr;
+    DSP_TRY(dev_alloc(b, (void**)&state, bytes, &b->param_bytes));
+    DSP_HIP(hipMemset(state, 0, bytes));
+    for (size_t i = 0; i < b->runs.size(); ++i) {
+        const ParamRun& r = b->runs[i];
+        dsp_adamw_tensor a = {};
+        a.d_param = b->x + r.p0;
+        a.d_grad = b->g + r.p0;
+        a.d_m = state + at[i] * kBlock * es;
+        a.d_v = state + moment + at[i] * kBlock * es;
+        if (state_bits == 8) {
+            a.d_m_exp = (uint8_t*)state + 2 * moment + at[i];
+            a.d_v_exp = a.d_m_exp + blocks;
+        }
+        a.n = (int64_t)r.n;
+        a.grad_dtype = DSP_FP32;
+        a.decay = r.decay ? 1 : 0;
+        t.push_back(a);
+    }
+    DSP_HIP(hipDeviceSynchronize());
+    DSP_TRY(dsp_adamw_init((int32_t)t.size(), t.data(), state_bits, seed, &b->adamw));
+    b->adamw_state = state;
+    b->adamw_bytes = bytes;
+    return DSP_OK;
+}
+
 int dsp_block_set_adamw(dsp_block* b, int32_t state_bits, uint64_t seed)
 {
     DSP_REQUIRE(b && (state_bits == 32 || state_bits == 8), DSP_EINVAL, "dsp_block_set_adamw: bad argument (states of 32 or 8 bits)");
     DSP_REQUIRE(!b->adamw, DSP_ESTATE, "dsp_block_set_adamw: the block has its moments already");
     DSP_REQUIRE(b->nP > 0, DSP_EINVAL, "dsp_block_set_adamw: the block has no parameters");
-    constexpr size_t kBlock = 256;
-    const size_t es = state_bits == 8 ? 1 : 4;
+    const size_t n_allocs = b->allocs.size(), param_bytes = b->param_bytes;
+    int rc = DSP_ENOMEM;
     try {
-        std::vector<dsp_adamw_tensor> t;
-        std::vector<size_t> at;
-        size_t blocks = 0;
-        for (const ParamRun& r : b->runs) {  // (whole blocks of the 8-bit states for every run)
-            at.push_back(blocks);
-            blocks += (r.n + kBlock - 1) / kBlock;
-        }
-        const size_t moment = blocks * kBlock * es, bytes = 2 * moment + (state_bits == 8 ? 2 * blocks : 0);
-        char* state = nullptr;
-        DSP_TRY(dev_alloc(b, (void**)&state, bytes, &b->param_bytes));
-        DSP_HIP(hipMemset(state, 0, bytes));
-        for (size_t i = 0; i < b->runs.size(); ++i) {
-            const ParamRun& r = b->runs[i];
-            dsp_adamw_tensor a = {};
-            a.d_param = b->x + r.p0;
-            a.d_grad = b->g + r.p0;
-            a.d_m = state + at[i] * kBlock * es;
-            a.d_v = state + moment + at[i] * kBlock * es;
-            if (state_bits == 8) {
-                a.d_m_exp = (uint8_t*)state + 2 * moment + at[i];
-                a.d_v_exp = a.d_m_exp + blocks;
-            }
-            a.n = (int64_t)r.n;
-            a.grad_dtype = DSP_FP32;
-            a.decay = r.decay ? 1 : 0;
-            t.push_back(a);
-        }
-        DSP_HIP(hipDeviceSynchronize());
-        DSP_TRY(dsp_adamw_init((int32_t)t.size(), t.data(), state_bits, seed, &b->adamw));
-        b->adamw_state = state;
-        b->adamw_bytes = bytes;
+        rc = block_add_adamw(b, state_bits, seed);
     } catch (const std::exception&) {
         set_error("dsp_block_set_adamw: out of host memory");
-        return DSP_ENOMEM;
     }
-    return DSP_OK;
+    if (rc != DSP_OK) {  // the block is as it was, and the call can be repeated
+        for (; b->allocs.size() > n_allocs; b->allocs.pop_back()) (void)hipFree(b->allocs.back());
+        b->param_bytes = param_bytes;
+    }
+    return rc;
 }
 
 int dsp_param_update_adamw(dsp_block* b, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm,

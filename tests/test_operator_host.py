@@ -112,6 +112,21 @@ def blocks_and_pipelines_out_of_memory_leave_nothing_behind(rt, D):
     assert rt.host_launches_bytes_held() == held
 
 
+@case
+def a_block_that_gets_no_moments_is_left_as_it_was(rt, D):
+    """dsp_block_set_adamw without memory keeps none and can be repeated."""
+    (b,) = _blocks(D)
+    held, was = rt.host_launches_bytes_held(), D.dsp_block_query(b)
+    _until_it_has_memory(rt, D, lambda: D.dsp_block_set_adamw(b, 8, 1) if D.dsp_block_query(b) == was else pytest.fail("the block has changed"))
+    state = D.dsp_block_adamw_state_bytes(b)
+    assert rt.host_launches_bytes_held() - held < state + 8192  # (beside the moments: 512 partial sums, the table and the clock)
+    fresh = _blocks(D)[0]
+    D.dsp_block_set_adamw(fresh, 8, 1)
+    assert D.dsp_block_query(b) == D.dsp_block_query(fresh)
+    D.dsp_block_destroy(fresh)
+    D.dsp_block_destroy(b)
+
+
 @pytest.mark.parametrize("name", CASES)
 def test_on_the_host(runtime, name):
     r = subprocess.run([sys.executable, os.path.abspath(__file__), runtime, name], capture_output=True, text=True, timeout=100, cwd=ROOT)
