@@ -349,7 +349,7 @@ int dsp_pipeline_set_optimizer(dsp_pipeline* pl, float lr, float momentum, int32
 /*
  * The updates of all later ticks are dsp_param_update_adamw's with these arguments (every block must have had
  * dsp_block_set_adamw: DSP_ESTATE otherwise); dsp_pipeline_set_optimizer goes back to Eq. (3).  A pipeline with a gradient
- * probe attached may use it; the probe pipeline itself may not (its step size is 0).
+ * probe attached may use it; the probe pipeline itself may not while the other one exists (its step size is 0).
  */
 int dsp_pipeline_set_adamw(dsp_pipeline* pl, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm);
 

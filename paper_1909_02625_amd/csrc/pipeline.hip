@@ -20,6 +20,7 @@
 // per phase of the ring rotation, lcm(ring sizes) of them -- with the K block chains as parallel
 // branches, and later ticks of the same phase replay that graph with a single launch while the
 // blocks' host-side state is advanced without launching.
+#include <algorithm>
 #include <atomic>
 #include <chrono>
 #include <condition_variable>
@@ -158,7 +159,8 @@ struct dsp_pipeline {
     // blocks of the same architecture re-runs each mini-batch as ordinary backpropagation at the
     // parameters every block held when it ran the forward pass of that mini-batch.
     dsp_pipeline* probe = nullptr;
-    bool is_probe = false;
+    bool probe_gone = false;                // the caller has destroyed it (after this pipeline's last step)
+    std::vector<dsp_pipeline*> probe_of;    // the pipelines that this one is the probe of
     std::vector<float*> xsnap, gstash;      // per block: rings of parameter snapshots / DSP gradients, by mini-batch
     std::vector<int> xsnap_n, gstash_n;     // their entry counts
     int32_t* probe_labels = nullptr;        // labels of the last 1 + m_0 mini-batches
@@ -285,6 +287,11 @@ int dsp_schedule_waits(int32_t K, const int32_t* p, const int32_t* m, const int3
 int dsp_pipeline_destroy(dsp_pipeline* pl)
 {
     if (!pl) return DSP_OK;
+    if (pl->probe && !pl->probe_gone) {
+        std::vector<dsp_pipeline*>& of = pl->probe->probe_of;
+        of.erase(std::remove(of.begin(), of.end(), pl), of.end());
+    }
+    for (dsp_pipeline* other : pl->probe_of) other->probe_gone = true;
     stop_workers(pl);
     (void)hipDeviceSynchronize();
     drop_graphs(pl);
@@ -519,7 +526,7 @@ int dsp_pipeline_set_adamw(dsp_pipeline* pl, double lr, double beta1, double bet
     DSP_TRY(adamw_check_hyper(lr, beta1, beta2, eps, weight_decay, max_norm, "dsp_pipeline_set_adamw"));
     for (dsp_block* b : pl->blocks)
         DSP_REQUIRE(block_has_adamw(b), DSP_ESTATE, "dsp_pipeline_set_adamw: a block without dsp_block_set_adamw");
-    DSP_REQUIRE(!pl->is_probe, DSP_ESTATE, "dsp_pipeline_set_adamw: the pipeline is a gradient probe");
+    DSP_REQUIRE(pl->probe_of.empty(), DSP_ESTATE, "dsp_pipeline_set_adamw: the pipeline is a gradient probe");
     pl->adamw = true;
     pl->adamw_lr = lr;
     pl->beta1 = beta1;
@@ -564,8 +571,8 @@ int dsp_pipeline_attach_gradient_probe(dsp_pipeline* pl, dsp_pipeline* probe)
     DSP_TRY(pl_alloc(pl, (void**)&pl->probe_out, sizeof(double) * 2 * K));
     pl->probe_diff.assign(K, 0.0);
     pl->probe_ref.assign(K, 0.0);
+    probe->probe_of.push_back(pl);
     pl->probe = probe;
-    probe->is_probe = true;
     return DSP_OK;
 }
 

@@ -69,14 +69,14 @@ def adamw_out_of_memory_leaves_nothing_behind(rt, D):
     assert rt.host_launches_bytes_held() == held
 
 
-def _blocks(D, n=1):
-    """Blocks of a small network, as for a pipeline without delays."""
+def _blocks(D, n=1, p=0, m=(0, 0)):
+    """The first blocks of a small network, `p` ticks from one to the next, block k recomputing m[k] later."""
     import numpy as np
     from workloads import flatten_params, get_config, make_params
     cfg = get_config("tiny2")
     rng, shape, blocks = np.random.default_rng(0), tuple(cfg["input"]), []
     for k, layers in enumerate(cfg["blocks"][:n]):
-        desc, keep = D.make_block_desc(layers, shape, D.DSP_BF16, k, n, 0, p_prev=0, needs_input_grad=k > 0)
+        desc, keep = D.make_block_desc(layers, shape, D.DSP_BF16, k, n, m[k], p_prev=p if k else 0, needs_input_grad=k > 0)
         blocks.append(D.dsp_block_init(desc, flatten_params(layers, make_params(layers, rng))))
         shape = D.dsp_block_output_shape(blocks[-1])[0]
     return blocks
@@ -125,6 +125,34 @@ def a_block_that_gets_no_moments_is_left_as_it_was(rt, D):
     assert D.dsp_block_query(b) == D.dsp_block_query(fresh)
     D.dsp_block_destroy(fresh)
     D.dsp_block_destroy(b)
+
+
+@case
+def a_pipeline_is_a_probe_while_it_measures_another(rt, D):
+    """Either may go first; a probe of pipelines that are gone takes AdamW as any other."""
+    blocks, probes = _blocks(D, 2, 1, (2, 0)), _blocks(D, 2)
+    for b in probes:
+        D.dsp_block_set_adamw(b)
+    for probe_first in (False, True):
+        pr = D.dsp_pipeline_init(probes, (0, 0), (0, 0), 0.0, 0.0, 0.0, 4)
+        pls = [D.dsp_pipeline_init(blocks, (1, 0), (2, 0), 0.1, 0.9, 0.0, 4) for _ in range(2)]
+        for pl in pls:
+            D.dsp_pipeline_attach_gradient_probe(pl, pr)
+        if probe_first:
+            D.dsp_pipeline_destroy(pr)
+        for pl in pls:
+            if not probe_first:
+                with pytest.raises(D.DSPError) as e:
+                    D.dsp_pipeline_set_adamw(pr, 1e-3)
+                assert e.value.status == 2
+            else:
+                D.dsp_pipeline_gradient_difference(pl, 2)
+            D.dsp_pipeline_destroy(pl)
+        if not probe_first:
+            D.dsp_pipeline_set_adamw(pr, 1e-3)
+            D.dsp_pipeline_destroy(pr)
+    for b in blocks + probes:
+        D.dsp_block_destroy(b)
 
 
 @pytest.mark.parametrize("name", CASES)
