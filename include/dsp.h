@@ -262,6 +262,7 @@ typedef struct dsp_adamw_tensor {
 
 /*
  * Builds the update of n_tensors tensors (the array is not kept).  A new optimizer starts from states of zero bytes and step 0.
+ * Tensors are cut into chunks of 4096 elements (6144 with states of 8 bits); together they may have 2^24 - 1 of them.
  *
  * state_bits = 8: element i of a moment stands for its 8-bit float (OCP e4m3 for m, e5m2 for v) times 2^(exp[i / 256] - 127).
  * The step forms the new moments in 32 bits, updates the parameters with them and stores them rounded STOCHASTICALLY: up with

@@ -29,6 +29,7 @@ static_assert(kStateBlock == 64 * 4, "a wave's quad is a block of the 8-bit stat
 // 1024 or 2048 workgroups that go through all chunks are slower by 2 to 15 %.)
 constexpr int quads(int bits) { return bits == 8 ? 6 : 4; }
 constexpr int chunk_elems(int bits) { return kRow * quads(bits); }
+constexpr size_t kMostChunks = 0xffffffffu / kThreads;  // a grid holds fewer than 2^32 threads
 constexpr int kNormThreads = 1024;                    // workgroup of the gradient norm
 constexpr int kNormBlocks = 512;                      // most of its workgroups: two fill a compute unit
 constexpr int kNormRows = 4;                          // chunks it has in flight
@@ -546,6 +547,8 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
             range(t.d_v_exp, blocks, true);
         }
         constexpr size_t kWord = (size_t)1 << 32;  // (a chunk does not pass a multiple: the upper half of its elements' numbers is one)
+        DSP_REQUIRE(chunks.size() + n / kWord * ((kWord + chunk - 1) / chunk) + (n % kWord + chunk - 1) / chunk <= kMostChunks, DSP_EINVAL,
+                    "dsp_adamw_init: too many tensors or elements");
         for (size_t at = 0, len = 0; at < n; at += len) {
             len = std::min(std::min(chunk, n - at), kWord - at % kWord);
             AdamwChunk c = {};
@@ -570,7 +573,6 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
         o->update_bytes += (double)n * (8 + gs + (t.d_copy ? 2 : 0)) + (state_bits == 8 ? 4.0 * n + 4.0 * blocks : 16.0 * n);
     }
     if (chunks.empty()) chunks.push_back(AdamwChunk{});  // (nothing but a step to count)
-    DSP_REQUIRE(chunks.size() < (size_t)1 << 29, DSP_EINVAL, "dsp_adamw_init: too many elements");
     DSP_REQUIRE(!ranges_clash(ranges), DSP_EINVAL, "dsp_adamw_init: a buffer that is written overlaps another one (the same tensor twice?)");
     o->n_chunks = (int)chunks.size();
     return adamw_upload(o, chunks);

@@ -155,6 +155,34 @@ def a_pipeline_is_a_probe_while_it_measures_another(rt, D):
         D.dsp_block_destroy(b)
 
 
+@case
+def an_optimizer_belongs_to_its_device(rt, D):
+    """With another device current its calls are refused, and destroying it waits for its own."""
+    rt.hipSetDevice(1)
+    (b,) = _blocks(D)
+    D.dsp_block_set_adamw(b)
+    blob = D.dsp_block_get_adamw_state(b)
+    t = D.dsp_adamw_tensor(A, 2 * A, 0, 3 * A, 4 * A, 0, 0, 1000, D.DSP_FP32, 1)
+    o = ctypes.c_void_p()
+    assert D.lib().dsp_adamw_init(1, ctypes.byref(t), 32, 0, ctypes.byref(o)) == 0
+    D.dsp_adamw_set_steps(o.value, 5)
+    rt.hipSetDevice(0)
+    for call in (lambda: D.dsp_adamw_step(o.value, 1e-3, stream=0), lambda: D.dsp_adamw_get_steps(o.value), lambda: D.dsp_adamw_set_steps(o.value, 7),
+                 lambda: D.dsp_block_get_adamw_state(b), lambda: D.dsp_block_set_adamw_state(b, blob)):
+        with pytest.raises(D.DSPError) as e:
+            call()
+        assert e.value.status == 1 and "device 1" in str(e.value)
+    before = rt.host_launches_synchronised(1)
+    D.dsp_adamw_destroy(o.value)
+    assert rt.host_launches_synchronised(1) == before + 1
+    device = ctypes.c_int(-1)
+    rt.hipGetDevice(ctypes.byref(device))
+    assert device.value == 0
+    rt.hipSetDevice(1)
+    assert (D.dsp_block_get_adamw_state(b) == blob).all()
+    D.dsp_block_destroy(b)
+
+
 @pytest.mark.parametrize("name", CASES)
 def test_on_the_host(runtime, name):
     r = subprocess.run([sys.executable, os.path.abspath(__file__), runtime, name], capture_output=True, text=True, timeout=100, cwd=ROOT)

@@ -47,6 +47,20 @@ def test_adamw_refuses(bits):
     D.dsp_adamw_destroy(None)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_refuses_more_chunks_than_a_launch_has_workgroups(bits):
+    """2^24 workgroups of 256 threads are more than a grid may hold: 4096 or 6144 elements each, in one tensor or in many."""
+    B_ = 1 << 42
+    big = lambda n: tensor(d_param=B_, d_grad=2 * B_, d_m=3 * B_, d_v=4 * B_, d_m_exp=5 * B_, d_v_exp=6 * B_, n=n)  # noqa: E731
+    per = 4096 if bits == 32 else 6144
+    assert init([big((1 << 24) * per)], bits) == 1 and "too many" in D.dsp_last_error()
+    third = [big((1 << 24) * per // 3 + per) for _ in range(3)]
+    for i, t in enumerate(third):
+        for f in ("d_param", "d_grad", "d_m", "d_v", "d_m_exp", "d_v_exp"):
+            setattr(t, f, getattr(t, f) + i * (B_ // 4))
+    assert init(third, bits) == 1 and "too many" in D.dsp_last_error()
+
+
 def test_adamw_binding_wants_whole_tensors():
     import torch
     z = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt)  # noqa: E731
