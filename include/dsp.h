@@ -289,7 +289,7 @@ int dsp_adamw_destroy(dsp_adamw* o);
 int dsp_adamw_step(dsp_adamw* o, double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm,
                    float* d_norm, void* stream);
 /* Steps taken so far, and setting it when training is resumed (beta^steps then counts as their product).  Both synchronise
- * the device. */
+ * the object's device, which must be the current one. */
 int dsp_adamw_get_steps(dsp_adamw* o, int64_t* steps);
 int dsp_adamw_set_steps(dsp_adamw* o, int64_t steps, double beta1, double beta2);
 

@@ -582,6 +582,14 @@ int adamw_build(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t stat
 
 namespace dsp {
 
+int adamw_check_device(const dsp_adamw* o, const char* who)
+{
+    int device = -1;
+    DSP_HIP(hipGetDevice(&device));
+    DSP_REQUIRE(device == o->device, DSP_EINVAL, "%s: the optimizer belongs to device %d, the current one is %d", who, o->device, device);
+    return DSP_OK;
+}
+
 static_assert(offsetof(AdamwClock, done) == kAdamwClockBytes, "steps, p1, p2 lead the clock");
 
 int adamw_clock_read(dsp_adamw* o, void* h_dst)
@@ -627,7 +635,11 @@ int dsp_adamw_init(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t s
 int dsp_adamw_destroy(dsp_adamw* o)
 {
     if (!o) return DSP_OK;
+    int device = o->device;
+    (void)hipGetDevice(&device);
+    if (device != o->device) (void)hipSetDevice(o->device);
     (void)hipDeviceSynchronize();
+    if (device != o->device) (void)hipSetDevice(device);
     adamw_free(o);
     return DSP_OK;
 }
@@ -637,9 +649,7 @@ int dsp_adamw_step(dsp_adamw* o, double lr, double beta1, double beta2, double e
 {
     DSP_REQUIRE(o, DSP_EINVAL, "dsp_adamw_step: null object");
     DSP_TRY(adamw_check_hyper(lr, beta1, beta2, eps, weight_decay, max_norm, "dsp_adamw_step"));
-    int device = -1;
-    DSP_HIP(hipGetDevice(&device));
-    DSP_REQUIRE(device == o->device, DSP_EINVAL, "dsp_adamw_step: the object belongs to device %d, the current one is %d", o->device, device);
+    DSP_TRY(adamw_check_device(o, "dsp_adamw_step"));
     hipStream_t st = (hipStream_t)stream;
     const bool norm = max_norm > 0.0 || d_norm;
     const int norm_blocks = std::min(o->n_chunks, kNormBlocks);
@@ -676,6 +686,7 @@ int dsp_adamw_step(dsp_adamw* o, double lr, double beta1, double beta2, double e
 int dsp_adamw_get_steps(dsp_adamw* o, int64_t* steps)
 {
     DSP_REQUIRE(o && steps, DSP_EINVAL, "dsp_adamw_get_steps: bad argument");
+    DSP_TRY(adamw_check_device(o, "dsp_adamw_get_steps"));
     DSP_HIP(hipDeviceSynchronize());
     DSP_HIP(hipMemcpy(steps, &o->clock->steps, sizeof(int64_t), hipMemcpyDeviceToHost));
     return DSP_OK;
@@ -685,6 +696,7 @@ int dsp_adamw_set_steps(dsp_adamw* o, int64_t steps, double beta1, double beta2)
 {
     DSP_REQUIRE(o && steps >= 0 && beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0, DSP_EINVAL,
                 "dsp_adamw_set_steps: bad argument");
+    DSP_TRY(adamw_check_device(o, "dsp_adamw_set_steps"));
     DSP_HIP(hipDeviceSynchronize());
     AdamwClock c = {};
     c.steps = steps;

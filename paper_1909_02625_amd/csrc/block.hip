@@ -1296,6 +1296,7 @@ int dsp_block_get_adamw_state(dsp_block* b, void* h_dst, size_t bytes)
     DSP_REQUIRE(b && h_dst, DSP_EINVAL, "dsp_block_get_adamw_state: bad argument");
     DSP_REQUIRE(b->adamw, DSP_ESTATE, "dsp_block_get_adamw_state: dsp_block_set_adamw has not been called");
     DSP_REQUIRE(bytes == b->adamw_bytes + kAdamwClockBytes, DSP_EINVAL, "dsp_block_get_adamw_state: bad size");
+    DSP_TRY(adamw_check_device(b->adamw, "dsp_block_get_adamw_state"));
     DSP_HIP(hipDeviceSynchronize());
     DSP_HIP(hipMemcpy(h_dst, b->adamw_state, b->adamw_bytes, hipMemcpyDeviceToHost));
     return adamw_clock_read(b->adamw, (char*)h_dst + b->adamw_bytes);
@@ -1305,6 +1306,7 @@ int dsp_block_set_adamw_state(dsp_block* b, const void* h_src, size_t bytes)
     DSP_REQUIRE(b && h_src, DSP_EINVAL, "dsp_block_set_adamw_state: bad argument");
     DSP_REQUIRE(b->adamw, DSP_ESTATE, "dsp_block_set_adamw_state: dsp_block_set_adamw has not been called");
     DSP_REQUIRE(bytes == b->adamw_bytes + kAdamwClockBytes, DSP_EINVAL, "dsp_block_set_adamw_state: bad size");
+    DSP_TRY(adamw_check_device(b->adamw, "dsp_block_set_adamw_state"));
     DSP_HIP(hipDeviceSynchronize());
     DSP_TRY(adamw_clock_write(b->adamw, (const char*)h_src + b->adamw_bytes));
     DSP_HIP(hipMemcpy(b->adamw_state, h_src, b->adamw_bytes, hipMemcpyHostToDevice));

@@ -321,6 +321,7 @@ int launch_refresh_shadows(int dtype, const float* x, const UpdateTask* tasks, i
                            const int32_t* tap_tab, void* wf16, void* wt, size_t n, hipStream_t st);
 // ---- AdamW (adamw.hip) ----
 int adamw_check_hyper(double lr, double beta1, double beta2, double eps, double weight_decay, double max_norm, const char* who);
+int adamw_check_device(const dsp_adamw* o, const char* who);  // that it is the current one
 // What an optimizer counts on the device -- steps and the products of its betas -- as it is kept in a checkpoint.
 constexpr size_t kAdamwClockBytes = 24;
 int adamw_clock_read(dsp_adamw* o, void* h_dst);
