@@ -342,19 +342,23 @@ def dsp_pipeline_gradient_difference(pl, K):
 
 # ---- AdamW ---------------------------------------------------------------------------------------------
 def dsp_adamw_init(tensors, state_bits=32, seed=0):
-    """``tensors``: dicts of contiguous device tensors param, grad, m, v and, as they apply, copy, m_exp, v_exp; decay (default True).
-    They have to outlive the object."""
+    """``tensors``: dicts of contiguous device tensors param (float32), grad (float32 or bfloat16), m, v (float32; with states of 8 bits
+    uint8, or float8_e4m3fn and float8_e5m2) and, as they apply, copy (bfloat16), m_exp, v_exp (uint8 or float8_e8m0fnu); decay
+    (default True).  They have to outlive the object."""
     import torch
     arr = (dsp_adamw_tensor * max(1, len(tensors)))()
-    state = 1 if state_bits == 8 else 4
+    eight = state_bits == 8
+    types = {"param": (torch.float32,), "grad": (torch.float32, torch.bfloat16), "copy": (torch.bfloat16,),
+             "m": (torch.uint8, torch.float8_e4m3fn) if eight else (torch.float32,),
+             "v": (torch.uint8, torch.float8_e5m2) if eight else (torch.float32,),
+             "m_exp": (torch.uint8, torch.float8_e8m0fnu), "v_exp": (torch.uint8, torch.float8_e8m0fnu)}
     for a, t in zip(arr, tensors):
         n = t["param"].numel()
-        sizes = {"param": (4, n), "grad": (2 if t["grad"].dtype == torch.bfloat16 else 4, n), "copy": (2, n), "m": (state, n), "v": (state, n)}
-        for name in ("param", "grad", "copy", "m", "v", "m_exp", "v_exp"):
+        for name, dtypes in types.items():
             x = t.get(name)
-            size, count = sizes.get(name, (1, -(-n // 256)))
-            if x is not None and (x.element_size() != size or x.numel() != count or not x.is_contiguous()):
-                raise ValueError("dsp_adamw_init: %s: %d contiguous elements of %d bytes are wanted" % (name, count, size))
+            count = -(-n // 256) if name.endswith("_exp") else n
+            if x is not None and (x.dtype not in dtypes or x.numel() != count or not x.is_contiguous()):
+                raise ValueError("dsp_adamw_init: %s: %d contiguous elements of %s are wanted" % (name, count, " or ".join(map(str, dtypes))))
             setattr(a, "d_" + name, _ptr(x))
         a.n, a.decay = n, int(bool(t.get("decay", True)))
         a.grad_dtype = DSP_BF16 if t["grad"].dtype == torch.bfloat16 else DSP_FP32

@@ -73,6 +73,23 @@ def test_adamw_binding_wants_whole_tensors():
                            "v_exp": z(2, torch.uint8)}], 8)
 
 
+def test_adamw_binding_wants_the_types_that_the_kernels_read():
+    """Elements of the right size and another type: a float16 copy would receive bfloat16 bits, integer parameters those of floats."""
+    import torch
+    z = lambda n, dt=torch.float32: torch.zeros(n, dtype=dt)  # noqa: E731
+    good = {"param": z(300), "grad": z(300), "m": z(300), "v": z(300)}
+    for over in ({"copy": z(300, torch.float16)}, {"copy": z(300, torch.int16)}, {"param": z(300, torch.int32)}, {"grad": z(300, torch.int32)},
+                 {"grad": z(300, torch.float16)}, {"m": z(300, torch.int32)}, {"v": z(300, torch.int32)}):
+        with pytest.raises(ValueError):
+            D.dsp_adamw_init([{**good, **over}])
+    byte = lambda n: z(n, torch.uint8)  # noqa: E731
+    good = {"param": z(300), "grad": z(300), "m": byte(300), "v": byte(300), "m_exp": byte(2), "v_exp": byte(2)}
+    for over in ({"m": z(300, torch.float8_e5m2)}, {"v": z(300, torch.float8_e4m3fn)}, {"m": z(300, torch.int8)}, {"v": z(300, torch.bool)},
+                 {"m": z(300, torch.float8_e4m3fnuz)}, {"m_exp": z(2, torch.int8)}, {"v_exp": z(2, torch.bool)}):
+        with pytest.raises(ValueError):
+            D.dsp_adamw_init([{**good, **over}], 8)
+
+
 def desc(**over):
     d = D.make_norm_residual_desc(16, 64, D.DSP_FP32, 1, 2, gate_rows=4)
     for k, v in over.items():
