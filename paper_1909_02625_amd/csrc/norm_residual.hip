@@ -10,6 +10,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <initializer_list>
 
 namespace dsp {
 namespace {
@@ -928,6 +929,13 @@ int check_desc(const dsp_norm_residual_desc* d, const char* who)
 }
 
 bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+// Of vectors and statistics; what belongs to a norm that is NONE is not looked at.
+bool floats(bool used, std::initializer_list<const float*> ps)
+{
+    for (const float* p : ps)
+        if (used && !aligned_to(p, sizeof(float))) return false;
+    return true;
+}
 
 // Threads and runs a thread that hold a row of C elements.
 struct RowShape {
@@ -1080,7 +1088,9 @@ int dsp_norm_residual_forward(const dsp_norm_residual_desc* d, const void* d_x, 
                      "dsp_norm_residual_forward: without a branch there is the norm in front of the next block alone (d_y NULL, alpha 1)");
     const size_t e = dtype_size(d->dtype);
     DSP_REQUIRE(aligned_to(d_x, e) && aligned_to(d_z, e) && aligned_to(d_y, e) && aligned_to(d_h, e) &&
-                    aligned_to(d_gate, dtype_size(d->gate_dtype)), DSP_EINVAL, "dsp_norm_residual_forward: misaligned buffer");
+                    aligned_to(d_gate, dtype_size(d->gate_dtype)) && floats(post, {d_post_gain, d_post_bias, d_post_stats}) &&
+                    floats(pre, {d_pre_gain, d_pre_bias, d_pre_stats}),
+                DSP_EINVAL, "dsp_norm_residual_forward: misaligned buffer");
     NormArgs a;
     a.x = d_x; a.z = d_z; a.gate = d_gate;
     a.post_gain = post ? d_post_gain : nullptr; a.post_bias = post ? d_post_bias : nullptr;
@@ -1122,7 +1132,9 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh
                 "dsp_norm_residual_backward: gradient of a norm that is not there");
     const size_t e = dtype_size(d->dtype);
     DSP_REQUIRE(aligned_to(d_dh, e) && aligned_to(d_dy, e) && aligned_to(d_y, e) && aligned_to(d_z, e) && aligned_to(d_dx, e) &&
-                    aligned_to(d_dz, e) && aligned_to(d_gate, dtype_size(d->gate_dtype)) && aligned_to(d_dgate, dtype_size(d->gate_dtype)),
+                    aligned_to(d_dz, e) && aligned_to(d_gate, dtype_size(d->gate_dtype)) && aligned_to(d_dgate, dtype_size(d->gate_dtype)) &&
+                    floats(post, {d_post_gain, d_post_bias, d_post_stats, d_dpost_gain, d_dpost_bias}) &&
+                    floats(pre, {d_pre_gain, d_pre_stats, d_dpre_gain, d_dpre_bias}),
                 DSP_EINVAL, "dsp_norm_residual_backward: misaligned buffer");
     const BackPlan p = back_plan(d, d_dpre_bias || d_dpost_bias || (d_dgate && d_post_bias && post));
     const bool sums = d_dpre_gain || d_dpre_bias || d_dpost_gain || d_dpost_bias || (d_dgate && !p.fold);

@@ -140,6 +140,14 @@ def test_norm_residual_refuses():
     assert D.lib().dsp_norm_residual_workspace_bytes(desc(), None) == 1
 
 
+def test_norm_residual_wants_aligned_vectors_and_statistics():
+    """Floats on addresses of floats, as the header says of every buffer."""
+    for name in ("g1", "b1", "g2", "b2", "s1", "s2"):
+        assert fwd(desc(), **{name: A + 2}) == 1 and "misaligned" in D.dsp_last_error(), name
+    for name in ("g1", "b1", "g2", "s1", "s2", "dg1", "db1", "dg2", "db2"):
+        assert bwd(desc(), **{name: 20 * A + 1}) == 1 and "misaligned" in D.dsp_last_error(), name
+
+
 def test_workspace_stays_small():
     for M, C in ((1, 1), (1 << 20, 16384), (1 << 30, 64), (1024, 4096)):
         for rows in (0, 1, 3, 1000, M):
