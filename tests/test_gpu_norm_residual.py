@@ -448,3 +448,14 @@ def test_a_residual_stack_trains():
                 ref[k] = torch.from_numpy(dev[k].cpu().numpy()).double().requires_grad_()
     finally:
         D.dsp_adamw_destroy(opt)
+
+
+@pytest.mark.parametrize("dtype,M,C", [("bf16", 1100, c) for c in (4104, 5001, 8192, 8200)] + [("bf16", 600, 12288)] +
+                         [("fp32", 1100, c) for c in (2049, 3000, 4104, 5001)] + [("fp32", 600, c) for c in (8192, 8200, 12288)])
+def test_many_rows_of_several_waves(dtype, M, C):
+    """Rows longer than a wave's, more of them than workgroups: a workgroup goes on to its second and third row, and the column sums
+    have many parts."""
+    wide = {"fp32": 12288, "bf16": 12288}[dtype] == C
+    gates = [None, (M, "fp32"), (1, dtype), (300, dtype), (3, dtype)]
+    for i, (post, pre) in enumerate(((2, 2), (1, 1)) if not wide else ((2, 2),)):
+        run(problem(M, C, dtype, post, pre, gates[(C + 3 * i + (dtype == "fp32")) % 5], (C + i) % 3, ("both", "gain")[i]), dtype, pad=8 * i, off=0)
