@@ -276,7 +276,7 @@ struct RowSum {
 };
 
 // Mean (layer norm; else 0) and 1 / deviation of a row; run(k, v) gives run k of the thread, 0 behind the row.  Centred before it is
-// squared: a row far from zero keeps its variance.
+// squared, as every element is before it is scaled: a row far from zero keeps its variance, and one of equal elements is 0.
 template <int TPR, int NV, int VW, typename Run>
 __device__ inline void row_stats(int kind, Run run, const int (&c)[NV], int C, float inv_c, float eps, RowSum<TPR, 1>& sum, float& mean,
                                  float& inv)
@@ -385,14 +385,13 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
                 }
             }
             const int64_t gate = row_gate && !raw_gate ? gate_row(live ? row : a.M - 1) : 0;
-            const float shift = mean * inv;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 if (row_gate && !raw_gate) load_gate<T>(a.gate, a.gate_f32, gate, c[k], a.C, g[k]);
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
                     const float act = row_gate ? w[k][e] * gate_act(a.act, g[k][e]) : w[k][e];
-                    const float n = (z[k][e] * inv - shift) * gpost[k][e] + bpost[k][e];
+                    const float n = (z[k][e] - mean) * inv * gpost[k][e] + bpost[k][e];
                     y[k][e] = a.alpha * y[k][e] + act * n;
                 }
                 if (live) store_run<T>((T*)a.y + row * a.ys, c[k], a.C, y[k], k + 1 < NV);
@@ -407,7 +406,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
 #pragma unroll
-            for (int e = 0; e < VW; ++e) y[k][e] = (y[k][e] * inv - mean * inv) * gpre[k][e] + bpre[k][e];
+            for (int e = 0; e < VW; ++e) y[k][e] = (y[k][e] - mean) * inv * gpre[k][e] + bpre[k][e];
             if (live) store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k], k + 1 < NV);
         }
     }
@@ -490,7 +489,6 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
                     a.post_stats[a.M + row] = inv;
                 }
             }
-            const float shift = mean * inv;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 float x[VW], z[VW], g[VW], w[VW], b[VW];
@@ -503,7 +501,7 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
                 else if (ROW_GATE) load_gate<T>(a.gate, a.gate_f32, gate, c[k], a.C, g);
 #pragma unroll
                 for (int e = 0; e < VW; ++e) {
-                    float n = (z[e] * inv - shift) * w[e];
+                    float n = (z[e] - mean) * inv * w[e];
                     if (bpost) n += b[e];
                     if (ROW_GATE) n *= gate_act(a.act, g[e]);
                     y[k][e] = a.alpha * x[e] + n;
@@ -523,7 +521,6 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
             a.pre_stats[row] = mean;
             a.pre_stats[a.M + row] = inv;
         }
-        const float shift = mean * inv;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float w[VW], b[VW];
@@ -531,7 +528,7 @@ __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(No
             if (bpre) get(vbpre, k, b);
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
-                y[k][e] = (y[k][e] * inv - shift) * w[e];
+                y[k][e] = (y[k][e] - mean) * inv * w[e];
                 if (bpre) y[k][e] += b[e];
             }
             store_run<T>((T*)a.h + row * a.hs, c[k], a.C, y[k], k + 1 < NV);
@@ -605,7 +602,7 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
         }
     };
     Raw<T> rdh[NV], ry_[NV], rz_[NV], rdy[NV];
-    float my = 0.f, ry = 0.f, mz = 0.f, rz = 1.f;  // 1 / deviations and the means times them
+    float my = 0.f, ry = 0.f, mz = 0.f, rz = 1.f;  // means and 1 / deviations
     auto fetch = [&](int64_t row) {
         const bool there = row < a.M;
         row = min(row, (int64_t)a.M - 1);
@@ -632,11 +629,11 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
         }
         if (pre) {
             ry = a.pre_stats[a.M + row];
-            my = a.pre_stats[row] * ry;
+            my = a.pre_stats[row];
         }
         if (post) {
             rz = a.post_stats[a.M + row];
-            mz = a.post_stats[row] * rz;
+            mz = a.post_stats[row];
         }
     };
     // the fetched row; `next`, unless negative, is fetched while its sums are taken
@@ -658,8 +655,8 @@ __global__ __launch_bounds__(MAXT) void norm_residual_bwd_kernel(NormBackArgs a)
             if (WHOLE || has_dy) RowIO<T>::unpack(rdy[k], q[k]);
 #pragma unroll
             for (int e = 0; e < VW; ++e) {
-                yh[k][e] = yh[k][e] * ry - my;
-                if (POST) zh[k][e] = zh[k][e] * rz - mz;
+                yh[k][e] = (yh[k][e] - my) * ry;
+                if (POST) zh[k][e] = (zh[k][e] - mz) * rz;
                 const float b = dh[k][e] * gpre[k][e];
                 q[k][e] += ry * b;
                 s[0] += b * yh[k][e];

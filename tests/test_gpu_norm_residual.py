@@ -459,3 +459,35 @@ def test_many_rows_of_several_waves(dtype, M, C):
     gates = [None, (M, "fp32"), (1, dtype), (300, dtype), (3, dtype)]
     for i, (post, pre) in enumerate(((2, 2), (1, 1)) if not wide else ((2, 2),)):
         run(problem(M, C, dtype, post, pre, gates[(C + 3 * i + (dtype == "fp32")) % 5], (C + i) % 3, ("both", "gain")[i]), dtype, pad=8 * i, off=0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,C", [(5, 32), (5, 256), (300, 256), (5, 1024), (1100, 1024), (1100, 2048), (5, 4096), (3, 8192), (3, 16384)])
+def test_constant_rows_are_exactly_zero_once_centred(M, C, dtype):
+    """Row sums of whole numbers below 2^24 and the quotient by a power of two are exact, so is the mean, and u - mean is 0: N(u) is the
+    bias, and nothing of the row reaches the gradients of gain and gate."""
+    code, td, E = TYPES[dtype]
+    rows = np.broadcast_to((8.0 * (125 - 5 * (np.arange(M) % 7)))[:, None], (M, C))
+    rng = np.random.default_rng(C)
+    bias, g = vec(rng.standard_normal(C)), Rows(rng.standard_normal((M, C)), td)
+    u, h, dx, zero = Rows(rows, td), Rows(np.ones((M, C)), td), Rows(np.ones((M, C)), td), Rows(np.zeros((M, C)), td)
+    gain, stats = vec(1 + rng.standard_normal(C)), torch.zeros(2 * M, device="cuda")
+    ws = torch.empty(1024 * 16 * C, dtype=torch.uint8, device="cuda")
+    dg = torch.ones(C, device="cuda")
+    d = D.make_norm_residual_desc(M, C, code, pre=D.DSP_NORM_LAYER, eps=EPS)  # in front of the next block
+    D.dsp_norm_residual_forward(d, u.view, d_pre_gain=gain, d_pre_bias=bias, d_h=h.view, d_pre_stats=stats)
+    assert np.array_equal(h.get(), np.broadcast_to(rounded(bias.cpu().numpy(), td), (M, C)))
+    assert np.array_equal(stats[:M].cpu().numpy(), rows[:, 0])
+    D.dsp_norm_residual_backward(d, g.view, None, u.view, None, None, None, None, gain, None, stats, dx.view, None, d_dpre_gain=dg, d_workspace=ws,
+                                 workspace_bytes=ws.numel())
+    assert not dg.any()
+    for gate_rows in (0, 1, M):  # behind the branch
+        gate = Rows(np.ones((-(-M // max(gate_rows, 1)), C)), td) if gate_rows else None
+        dgate = Rows(np.ones(gate.shape), td) if gate else None
+        d = D.make_norm_residual_desc(M, C, code, post=D.DSP_NORM_LAYER, beta=-1.25, eps=EPS, gate_rows=gate_rows, gate_act=1)
+        y = Rows(np.ones((M, C)), td)
+        D.dsp_norm_residual_forward(d, zero.view, u.view, gate.view if gate else None, gain, d_y=y.view, d_post_stats=stats)
+        assert not y.get().any()
+        D.dsp_norm_residual_backward(d, None, g.view, None, u.view, gate.view if gate else None, gain, None, None, stats, None, None, dx.view,
+                                     dgate.view if gate else None, dg.fill_(1.0), d_workspace=ws, workspace_bytes=ws.numel())
+        assert not dg.any() and not (gate and dgate.get().any())
