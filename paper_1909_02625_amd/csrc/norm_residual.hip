@@ -176,10 +176,18 @@ __device__ inline void load_gate(const void* gate, int gate_f32, int64_t at, int
     else load_vector((const float*)gate + at, c, C, v, 0.f);
 }
 
-// exp(-g) from the hardware's power of two (within one unit of its last place) of a product that is rounded once: relative error
-// (|g| + 2) 2^-24.  Quotients from its reciprocal, within one unit too.
-__device__ inline float exp_of_minus(float g) { return __builtin_amdgcn_exp2f(g * -1.44269504f); }
-// The activation and its derivative, with e = exp(-|g|) (tanh: exp(-2 |g|)) and q = 1 / (1 + e): sigmoid = q or e q, sigmoid' = e q^2;
+// exp(-a) for a >= 0 (or NaN) from the hardware's power of two, within one unit of its last place.  The exponent's product is rounded,
+// which alone would cost a 2^-24 of the result: what hi ln(2), with ln(2) in two parts, lacks of -a is a factor 1 + off.  Relative error
+// 3 * 2^-24; 0 below 2^-126.  (Where a is infinite off is no number, and the bound makes it one; p is NaN only where a is.)
+__device__ inline float exp_of_minus(float a)
+{
+    constexpr float kLn2 = 0.693147182f, kRest = -1.90465421e-9f;  // ln(2) = kLn2 + kRest
+    const float hi = a * -1.44269504f, p = __builtin_amdgcn_exp2f(hi);
+    const float off = fminf(fmaf(hi, -kRest, fmaf(hi, -kLn2, -a)), 1.f);
+    return fmaf(p, off, p);
+}
+// The activation and its derivative, with e = exp(-|g|) (tanh: exp(-2 |g|)) and q = 1 / (1 + e) from the hardware's reciprocal, within one
+// unit too: sigmoid = q or e q, sigmoid' = e q^2;
 // tanh = (1 - e) q, below 1/4 its series up to g^9 (the next term is 1e-8 of it there), tanh' = 4 e q^2.  No difference of nearly
 // equal numbers.
 __device__ inline void gate_both(int act, float g, float& a, float& slope)

@@ -491,3 +491,46 @@ def test_constant_rows_are_exactly_zero_once_centred(M, C, dtype):
         D.dsp_norm_residual_backward(d, None, g.view, None, u.view, gate.view if gate else None, gain, None, None, stats, None, None, dx.view,
                                      dgate.view if gate else None, dg.fill_(1.0), d_workspace=ws, workspace_bytes=ws.numel())
         assert not dg.any() and not (gate and dgate.get().any())
+
+
+@pytest.mark.parametrize("M,C", [(7, 40), (7, 700), (1100, 700), (3, 5000)])
+@pytest.mark.parametrize("act", [1, 2], ids=["sigmoid", "tanh"])
+def test_gates_far_from_zero(act, M, C):
+    """The activation and its derivative relative to themselves, down to where they leave the floats, at infinities and at NaN.
+
+    exp(-a): the product with log2(e) is held in two parts, the hardware's power of two is off by 2 U and the correction rounds once: 3 U.
+    Its quotients with 1 + e (U, the reciprocal 2 U): sigmoid at most 3 + 1 + 2 + 1 U; tanh (1 - e) / (1 + e) from 1/4 on, where
+    2 e / (1 - e^2) < 2: 6 + 1 + 1 + 2 + 1 U; both derivatives 3 + 2 (1 + 2) + 2 U.  An exp(-a) below 2^-126 may
+    be 0 (the hardware's results are normal numbers or 0), and tanh' = 4 exp(-2 |g|) q^2 loses up to 4 times that."""
+    rng = np.random.default_rng(act * 1000 + C)
+    g = np.exp(rng.uniform(np.log(1e-4), np.log(100.0), (M, C))) * rng.choice([-1.0, 1.0], (M, C))
+    special = [np.inf, -np.inf, np.nan, 0.0, -0.0, 1e30, -1e30, 3e38, 0.25, -0.25, 43.5, -87.0, 87.4, -88.0, 1e-30]
+    g[0, :15], g[M - 1, C - 15:] = special, special
+    g = rounded(g, torch.float32)
+    with np.errstate(all="ignore"):
+        a, s = P.act(act, g), P.slope(act, g)
+        s = np.where(np.isinf(g), 0.0, s)
+    tiny = 2.0 ** -126 * (4 if act == 2 else 1)
+    one, out = Rows(np.ones((M, C)), torch.float32), [Rows(np.zeros((M, C)), torch.float32) for _ in range(3)]
+    x, (y, dz, dgate) = Rows(np.zeros((M, C)), torch.float32), out
+
+    def check(got, ref, n, what):
+        assert np.array_equal(np.isnan(got), np.isnan(ref)), what
+        off = np.abs(got - ref) / (n * U * np.abs(ref) + tiny)
+        assert not (off > 1).any(), (what, float(np.nanmax(off)), g.flat[np.nanargmax(off)])
+    d = D.make_norm_residual_desc(M, C, D.DSP_FP32, gate_rows=1, gate_act=act)
+    gate = Rows(g, torch.float32)
+    D.dsp_norm_residual_forward(d, x.view, one.view, gate.view, d_y=y.view)
+    check(y.get(), a, 12, "activation")
+    D.dsp_norm_residual_backward(d, None, one.view, None, one.view, gate.view, None, None, None, None, None, None, dz.view, dgate.view)
+    check(dz.get(), a, 12, "dz")
+    check(dgate.get(), s, 12, "derivative")
+    # one row of the gate for all: its derivative from the column sums
+    d = D.make_norm_residual_desc(1, C, D.DSP_FP32, gate_rows=1, gate_act=act)
+    ws = torch.empty(D.dsp_norm_residual_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    line = [Rows(v, torch.float32) for v in (np.zeros((1, C)), np.ones((1, C)), g[:1], np.zeros((1, C)), np.zeros((1, C)))]
+    D.dsp_norm_residual_forward(d, line[0].view, line[1].view, line[2].view, d_y=line[3].view)
+    D.dsp_norm_residual_backward(d, None, line[1].view, None, line[1].view, line[2].view, None, None, None, None, None, None, None, line[4].view,
+                                 d_workspace=ws, workspace_bytes=ws.numel())
+    check(line[3].get(), a[:1], 12, "activation of a vector")
+    check(line[4].get(), s[:1], 12, "derivative of a vector")
