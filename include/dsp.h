@@ -270,6 +270,7 @@ typedef struct dsp_adamw_tensor {
  * the tensor in the array and element alone.  (To nearest, v would stand still: one step moves it by 1 - beta2, far less than
  * half a step of any 8-bit float.)  A v > 0 is never stored as 0.  A value that is no finite number is stored as the format's
  * NaN and leaves the other 255 of its block alone.
+ * The step's root and quotient are then the hardware's, each within one unit of its last place (with 32 bits: rounded correctly).
  */
 int dsp_adamw_init(int32_t n_tensors, const dsp_adamw_tensor* tensors, int32_t state_bits, uint64_t seed, dsp_adamw** out);
 int dsp_adamw_destroy(dsp_adamw* o);

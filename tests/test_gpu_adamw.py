@@ -431,3 +431,18 @@ def test_pipeline_update_resumes_and_replays(bits):
     for k in range(K):  # the moments of AdamW wait; the parameters have moved on
         np.testing.assert_array_equal(a[1 + K + k], c[1 + K + k])
         assert not np.array_equal(a[1 + k], c[1 + k])
+
+
+def test_the_first_step_is_exactly_the_step_size():
+    """Without memory (betas of 0) m / sqrt(v) = g / |g|.  For gradients of 12 bits the square, its root and the quotient are exact, and
+    eps is less than half a step of the root."""
+    n = 1 << 16
+    rng = np.random.default_rng(0)
+    g = (rng.integers(1, 4096, n) * 2.0 ** rng.integers(-20, 10, n) * rng.choice([-1, 1], n)).astype(np.float32)
+    z = lambda: torch.zeros(n, device="cuda")  # noqa: E731
+    d = {"param": z(), "grad": torch.from_numpy(g).cuda(), "m": z(), "v": z()}
+    o = D.dsp_adamw_init([d])
+    D.dsp_adamw_step(o, 1.0, 0.0, 0.0, 1e-15)
+    x = d["param"].cpu().numpy()
+    D.dsp_adamw_destroy(o)
+    np.testing.assert_array_equal(x, -np.sign(g))
