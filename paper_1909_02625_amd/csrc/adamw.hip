@@ -251,7 +251,7 @@ __device__ inline void decode_quad(Quad& q)
 // The moments of a wave's quads, one block of the 8-bit states, as codes.
 //
 // The block's power of two puts its largest m into [2^7, 2^8) and its largest v into [2^14, 2^15): half of the formats' range is
-// left, so that rounding up never leaves it.  A float's leading bits, its exponent moved to the format's, are the code; random
+// left, so that rounding up never leaves it; only 2^128, which no float holds when it is read again, becomes the code below.  A float's leading bits, its exponent moved to the format's, are the code; random
 // bits added below them round up with the probability of what they drop.  `at`: the first element's number, of its key's tensor.
 __device__ inline void encode_quad(Quad& q, uint32_t key, uint32_t at)
 {
@@ -265,7 +265,7 @@ __device__ inline void encode_quad(Quad& q, uint32_t key, uint32_t at)
     }
     am = wave_max(am);
     av = wave_max(av);
-    const bool odd = am >= 0xff000000u || av >= 0x7f800000u;  // (the whole wave) something is no finite number
+    const bool odd = am >= 0xfe000000u || av >= 0x7f000000u;  // (the whole wave) something is no finite number, or from 2^127 on
     if (odd) {  // the exponents of what is
         am = av = 0u;
 #pragma unroll
@@ -289,8 +289,9 @@ __device__ inline void encode_quad(Quad& q, uint32_t key, uint32_t at)
     if (odd) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (um[e] >= 0xff000000u) km[e] |= 0x7f0000u;
-            if (uv[e] >= 0x7f800000u) kv[e] = 0x7f0000u;
+            const uint32_t sign = km[e] & 0x800000u;
+            km[e] = sign | (um[e] >= 0xff000000u ? 0x7f0000u : min(km[e] & 0x7fffffu, q.me == 247 ? 0x77ffffu : 0x7fffffu));
+            kv[e] = uv[e] >= 0x7f800000u ? 0x7f0000u : min(kv[e], q.ve == 240 ? 0x77ffffu : 0x7fffffu);
         }
     }
     auto bytes2 = [](const uint32_t (&k)[4]) -> uint32_t {

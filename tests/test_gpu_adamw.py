@@ -446,3 +446,23 @@ def test_the_first_step_is_exactly_the_step_size():
     x = d["param"].cpu().numpy()
     D.dsp_adamw_destroy(o)
     np.testing.assert_array_equal(x, -np.sign(g))
+
+
+def test_8_bits_keep_the_largest_floats_finite():
+    """Values in the last eighth below 2^128 are not rounded up to it: no float would hold that."""
+    n = 4096
+    g = np.full(n, 1.8e19, np.float32)  # squared 3.24e38, 1.9 * 2^127
+    g[::3] = 1.0
+    z = lambda k, dt: torch.zeros(k, dtype=dt, device="cuda")  # noqa: E731
+    d = {"param": z(n, torch.float32), "grad": torch.from_numpy(g).cuda(), "m": z(n, torch.uint8), "v": z(n, torch.uint8),
+         "m_exp": z(n // 256, torch.uint8), "v_exp": z(n // 256, torch.uint8)}
+    o = D.dsp_adamw_init([d], 8, 3)
+    for t in range(3):
+        D.dsp_adamw_step(o, 1e-3, 0.0, 0.0)
+        v = P.decode(d["v"].cpu().numpy(), d["v_exp"].cpu().numpy(), 2, 15)
+        assert (v < 2.0 ** 128).all() and (v[g > 1] >= 1.75 * 2.0 ** 127).all(), t
+        x = d["param"].cpu().numpy().astype(np.float64)
+        assert np.isfinite(x).all()
+        # every step is lr g / |g|, off by the hardware's root and reciprocal and a few roundings; x adds U of itself
+        assert np.abs(x[g > 1] + (t + 1) * 1e-3).max() <= (t + 1) * 12 * U * 1e-3
+    D.dsp_adamw_destroy(o)
