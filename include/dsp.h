@@ -559,7 +559,7 @@ int dsp_softmax_ce(const float* d_z, const int32_t* d_labels, float* d_loss, flo
  * positions of a sequence one row each (conditioning), gate_rows = 1 a gate of every element; gate_rows = 0: no gate.  Everything
  * is computed in float; h is normed before y is rounded to its type.
  * d_z = NULL is the first norm of a stack, h = N_pre(x): post = NONE, no gate, alpha = 1, d_y = NULL (the backward pass takes x
- * in the place of y).
+ * in the place of y, with y_stride).
  * Strides are the elements from one row to the next (0: C); a gradient has the stride of its tensor (dx: x, dz: z, dy: y,
  * dh: h, dgate: gate).  Buffers are aligned to their elements and no more.
  */

@@ -1096,6 +1096,8 @@ int dsp_norm_residual_forward(const dsp_norm_residual_desc* d, const void* d_x, 
                     aligned_to(d_gate, dtype_size(d->gate_dtype)) && floats(post, {d_post_gain, d_post_bias, d_post_stats}) &&
                     floats(pre, {d_pre_gain, d_pre_bias, d_pre_stats}),
                 DSP_EINVAL, "dsp_norm_residual_forward: misaligned buffer");
+    DSP_REQUIRE(d_y != d_x || stride_of(d->y_stride, d->C) == stride_of(d->x_stride, d->C), DSP_EINVAL,
+                "dsp_norm_residual_forward: y in the place of x wants its stride");
     NormArgs a;
     a.x = d_x; a.z = d_z; a.gate = d_gate;
     a.post_gain = post ? d_post_gain : nullptr; a.post_bias = post ? d_post_bias : nullptr;
@@ -1141,6 +1143,8 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* d, const void* d_dh
                     floats(post, {d_post_gain, d_post_bias, d_post_stats, d_dpost_gain, d_dpost_bias}) &&
                     floats(pre, {d_pre_gain, d_pre_stats, d_dpre_gain, d_dpre_bias}),
                 DSP_EINVAL, "dsp_norm_residual_backward: misaligned buffer");
+    DSP_REQUIRE(!d_dx || d_dx != d_dy || stride_of(d->x_stride, d->C) == stride_of(d->y_stride, d->C), DSP_EINVAL,
+                "dsp_norm_residual_backward: dx in the place of dy wants its stride");
     const BackPlan p = back_plan(d, d_dpre_bias || d_dpost_bias || (d_dgate && d_post_bias && post));
     const bool sums = d_dpre_gain || d_dpre_bias || d_dpost_gain || d_dpost_bias || (d_dgate && !p.fold);
     DSP_REQUIRE(!sums || (d_workspace && workspace_bytes >= p.bytes && ((uintptr_t)d_workspace % 16) == 0), DSP_EINVAL,

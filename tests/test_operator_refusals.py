@@ -148,6 +148,13 @@ def test_norm_residual_wants_aligned_vectors_and_statistics():
         assert bwd(desc(), **{name: 20 * A + 1}) == 1 and "misaligned" in D.dsp_last_error(), name
 
 
+def test_norm_residual_in_place_wants_the_same_stride():
+    """With another stride a row's result would fall on rows that others have still to read."""
+    for strides in (dict(x_stride=80), dict(y_stride=80), dict(x_stride=72, y_stride=80)):
+        assert fwd(desc(**strides), y=FWD["x"]) == 1 and "stride" in D.dsp_last_error(), strides
+        assert bwd(desc(**strides), dx=BWD["dy"]) == 1 and "stride" in D.dsp_last_error(), strides
+
+
 def test_workspace_stays_small():
     for M, C in ((1, 1), (1 << 20, 16384), (1 << 30, 64), (1024, 4096)):
         for rows in (0, 1, 3, 1000, M):
