@@ -4,8 +4,8 @@
 //
 // Every element is touched once: parameters and states in and out, the gradient in, the bf16 copy out.  The tensors are cut
 // into chunks at init; a workgroup finds all addresses of its chunk in one table entry.  Memory bounds it: 270 M parameters with
-// bf16 gradients and copies take 1.34 ms with states of 32 bits (5.7 TB/s, where a copy of 4 GiB reaches 4.9) and 0.75 ms with 8
-// (5.75 TB/s; vector instructions fill half of that time), the norm of their gradients 0.115 ms (4.7 TB/s).
+// bf16 gradients and copies take 1.35 ms with states of 32 bits (5.6 TB/s, where a copy of 4 GiB reaches 4.9) and 0.75 ms with 8
+// (5.75 TB/s; vector instructions fill half of that time), the norm of their gradients 0.12 ms (4.5 TB/s).
 #include "common.h"
 
 #include <string.h>

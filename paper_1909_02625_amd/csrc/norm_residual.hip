@@ -424,8 +424,11 @@ __global__ __launch_bounds__(MAXT) void norm_residual_fwd_kernel(NormArgs a)
 // biases lie in LDS, four floats of neighbouring lanes side by side: beta act(gate) gain_post, the same times bias_post, gain_pre,
 // bias_pre (of the gate only where one row of it serves all).
 //
-// From 1024 rows on (us a call, this against rows of several waves; both at a call's cost below): 1024 x 2560 bf16 8.7 / 13.4,
-// 1024 x 4096 10.5 / 12.7, 512 x 4096 9.2 / 8.5; 8192 x 1152 18.8 / 28.3, 8192 x 2560 30.4 / 51.4, 8192 x 4096 52.3 / 54.0.
+// From 1024 rows on (us a call, this / rows of several waves; 5.5 to 6.5 is what a call costs): bf16 1024 x 640 6.4 / 6.4, x 2560 6.5 /
+// 13.0, x 4096 8.6 / 12.3, 4096 x 1152 9.5 / 15.9, x 4096 22.6 / 29.4, fp32 1024 x 2048 7.2 / 7.9, 2048 x 1024 6.5 / 8.1.  Below, 768 x 2560
+// (6.5 / 9.0) and 768 x 4096 (8.5 / 10.1) would gain, 512 x 4096 (8.3 / 7.1), 256 x 4096 (7.6 / 6.4) and fp32 768 x 2048 (7.1 / 6.1) would
+// lose, and what is narrower costs a call either way.  With a row of the gate for a row or a sequence seven and eight bf16 runs a lane
+// no longer fit the registers, and this kernel is the slower one: 6000 x 3584 53 / 49, 6000 x 4096 72 / 54, 8192 x 4096 85 / 65.
 constexpr int kWaveThreads = 512, kWaveRows = 1024;
 template <typename T, int NV, bool ROW_GATE>
 __global__ __launch_bounds__(kWaveThreads) void norm_residual_fwd_wave_kernel(NormArgs a)
@@ -958,7 +961,13 @@ RowShape row_shape(int dtype, int C)
     return {0, ceil_div(runs, 64 * nv), nv};
 }
 
-// How the backward kernel's workgroups share the rows.
+// How the backward kernel's workgroups share the rows: four rows a slot before there is another workgroup, two for a compute unit at most.
+// (us with four, two and one: 8192 x 4096 92.1, 93.5, 94.2; 1024 x 4096 17.9, 19.2, 19.3; 512 x 4096 15.4, 14.2, 16.6; 2048 x 1024 14.7, 13.1,
+// 14.4; 512 x 1024 14.7, 13.0, 11.3; 2048 x 128 16.9, 15.1, 14.5: fewer parts to sum up for the large calls, a chain of rows for the small.)
+//
+// A gate of more rows than that many workgroups is folded, a row of it to a slot.  Where fewer of them than slots fall on a workgroup the
+// others wait: 32768 x 128 with 64 rows to one of the gate takes 95 us (41 with 512 workgroups), 16384 x 48 with 200 rows 465, and with 256,
+// which is not folded, 22.  Wide rows have one slot: 32768 x 4096 with 63 rows 490 us, with 65 355.
 struct BackPlan {
     int sums;
     bool biased, fold;
