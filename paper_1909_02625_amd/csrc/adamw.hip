@@ -251,8 +251,9 @@ __device__ inline void decode_quad(Quad& q)
 // The moments of a wave's quads, one block of the 8-bit states, as codes.
 //
 // The block's power of two puts its largest m into [2^7, 2^8) and its largest v into [2^14, 2^15): half of the formats' range is
-// left, so that rounding up never leaves it; only 2^128, which no float holds when it is read again, becomes the code below.  A float's leading bits, its exponent moved to the format's, are the code; random
-// bits added below them round up with the probability of what they drop.  `at`: the first element's number, of its key's tensor.
+// left, so that rounding up never leaves it; only 2^128, which no float holds when it is read again, becomes the code below.  A float's
+// leading bits, its exponent moved to the format's, are the code; random bits added below them round up with the probability of what
+// they drop.  `at`: the first element's number, of its key's tensor.
 __device__ inline void encode_quad(Quad& q, uint32_t key, uint32_t at)
 {
     uint32_t um[4], uv[4], am = 0u, av = 0u;
