@@ -602,6 +602,105 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* desc, const void* d
                                void* d_workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The product in a residual block's branch and what follows it, over M rows:
+ *     p = x W^T + bias,  y = act(p) + residual
+ * x: M rows of cin elements, W[cout][cin] without gaps, y, residual, pre: M rows of cout elements, all in `dtype`; bias: float.  act:
+ * identity, relu, gelu (p times the normal distribution function of p) or silu (p / (1 + exp(-p))).  Sums, bias, activation and residual are taken
+ * in float and rounded once.  (dsp_linear_forward is the float product of a classifier's head, without any of this.)
+ * Strides are the elements from one row to the next (x_stride: x and dx, 0: cin; y_stride: y, residual, pre and dy, 0: cout).  Buffers are
+ * aligned to their elements and no more; rows of whole 16-byte runs on 16-byte addresses are read and written fastest.
+ */
+typedef enum dsp_act_kind { DSP_ACT_IDENTITY = 0, DSP_ACT_RELU = 1, DSP_ACT_GELU = 2, DSP_ACT_SILU = 3 } dsp_act_kind;
+typedef struct dsp_dense_desc {
+    int64_t M;
+    int32_t cin, cout;
+    int32_t dtype; /* dsp_dtype of x, W, residual, y, pre and of the gradients but the bias's */
+    int32_t act;   /* dsp_act_kind */
+    int64_t x_stride, y_stride;
+} dsp_dense_desc;
+
+/*
+ * d_bias, d_residual: NULL = none.  d_pre: p as stored, for the backward pass of an activation; NULL: not kept.  d_y may be d_residual.
+ * d_workspace: dsp_dense_workspace_bytes(desc, 0) bytes (0 for most shapes: then NULL will do), 16-byte aligned, contents unspecified before
+ * and after; calls that may run at the same time, replays of captured ones among them, need one each.
+ */
+int dsp_dense_workspace_bytes(const dsp_dense_desc* desc, int32_t backward, size_t* bytes);
+int dsp_dense_forward(const dsp_dense_desc* desc, const void* d_x, const void* d_w, const float* d_bias, const void* d_residual, void* d_y,
+                      void* d_pre, void* d_workspace, size_t workspace_bytes, void* stream);
+/*
+ * Given dy: g = dy act'(pre) (pre as the forward pass stored it; not read with DSP_ACT_IDENTITY), dx = g W, dW = g^T x, dbias = the column sums of g;
+ * NULL ones are not formed.  The residual's gradient is dy itself.  The products read g in `dtype` (one more rounding); the column sums
+ * are of g in float.  d_workspace: dsp_dense_workspace_bytes(desc, 1) bytes, otherwise as above.  Sums are taken in a fixed order: the same
+ * call gives the same bits.
+ */
+int dsp_dense_backward(const dsp_dense_desc* desc, const void* d_dy, const void* d_x, const void* d_w, const void* d_pre, void* d_dx, void* d_dw,
+                       float* d_dbias, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A gated linear recurrence over the positions of sequences, for each of C channels:
+ *     a_t = 1 / (1 + exp(-f_t)) or exp(f_t),   u_t = x_t or (1 - a_t) x_t,   h_t = a_t h_(t-1) + u_t
+ * Rows are positions, of C elements in `dtype`; states are float.  The sequences lie one behind the other: with d_offsets (int32, on the
+ * device, sequences + 1 of them) sequence s has rows offsets[s] .. offsets[s + 1] - 1, none to `steps` of them (a longer one is read as its first
+ * `steps` rows; rows outside 0 .. rows - 1 are never touched); with NULL every one has `steps`.  Rows of no sequence stay as they
+ * were.  d_state_in: [sequences][C], h in front of each first row, NULL = 0; d_state_out: h behind each last row (of a sequence without rows: what
+ * went in), NULL: not kept; they may be the same buffer.  One step of serving is steps = 1 with both.
+ * Strides are the elements from one row to the next (0: C); a gradient has the stride of its tensor (dx: x, df: f, dh: h).  Buffers are
+ * aligned to their elements and no more.  d_h may not be d_x or d_f.
+ */
+typedef enum dsp_decay_kind { DSP_DECAY_SIGMOID = 0, DSP_DECAY_EXP = 1 } dsp_decay_kind;
+typedef struct dsp_recurrence_desc {
+    int64_t rows;      /* that x, f and h have */
+    int32_t sequences, steps;
+    int32_t C;
+    int32_t dtype;     /* dsp_dtype of x, f, h and their gradients */
+    int32_t decay;     /* dsp_decay_kind */
+    int32_t coupled;   /* 1: u = (1 - a) x */
+    int64_t x_stride, f_stride, h_stride;
+} dsp_recurrence_desc;
+
+/* d_workspace: dsp_recurrence_workspace_bytes() bytes for either call (0 for most shapes: then NULL will do), 16-byte aligned, contents unspecified
+ * before and after; calls that may run at the same time, replays of captured ones among them, need one each. */
+int dsp_recurrence_workspace_bytes(const dsp_recurrence_desc* desc, size_t* bytes);
+int dsp_recurrence_forward(const dsp_recurrence_desc* desc, const void* d_x, const void* d_f, const int32_t* d_offsets, const float* d_state_in,
+                           void* d_h, float* d_state_out, void* d_workspace, size_t workspace_bytes, void* stream);
+/*
+ * Given dh and the gradient of state_out (NULL = 0), h as the forward pass stored it and the same x, f, offsets and state_in: the gradients
+ * of x, f and state_in; NULL ones are not formed.  d_dx may be d_x or d_dh, d_df may be d_f (same strides), d_dstate_in may be d_dstate_out.
+ */
+int dsp_recurrence_backward(const dsp_recurrence_desc* desc, const void* d_dh, const float* d_dstate_out, const void* d_x, const void* d_f,
+                            const void* d_h, const int32_t* d_offsets, const float* d_state_in, void* d_dx, void* d_df, float* d_dstate_in,
+                            void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * What a policy is trained by, from `rows` rows of `vocab` logits in `dtype` and one token (label) of each:
+ *     p = softmax(z / temperature),  lp = log p[label],  rho = exp(lp - old),  H = -sum p log p
+ *     policy = max(-A rho, -A min(max(rho, 1 - clip_low), 1 + clip_high)),  kl = exp(ref - lp) - (ref - lp) - 1
+ *     L = sum over the rows of weight (policy + kl_coef kl - entropy_coef H)
+ * dsp_token_logprob gives lp and H (the old and the reference model's, say; the clip range and the coefficients are not looked at).
+ * dsp_policy_loss gives L and, reading every logit once, its gradient.  A row with a negative label (a prompt, padding) has no part in L: its
+ * lp, terms and gradient are 0, and so are those of a row whose logits are all -infinity.  A logit of -infinity has probability 0.  A label of
+ * vocab or more indexes nothing: its row's results are NaN, as are those of a row that holds NaN or +infinity.
+ */
+typedef struct dsp_policy_loss_desc {
+    int32_t rows, vocab;
+    int32_t dtype; /* dsp_dtype of the logits and their gradient */
+    float clip_low, clip_high, kl_coef, entropy_coef, temperature;
+    int64_t logits_stride, grad_stride; /* elements from one row to the next, 0: vocab */
+} dsp_policy_loss_desc;
+
+/* d_labels: int32[rows]; d_logp, d_entropy: float[rows], NULL: not formed. */
+int dsp_token_logprob(const dsp_policy_loss_desc* desc, const void* d_logits, const int32_t* d_labels, float* d_logp, float* d_entropy, void* stream);
+/*
+ * Floats of one row each: d_old_logp (NULL: the policy's own, rho = 1), d_ref_logp (NULL with kl_coef = 0: kl is then 0), d_advantage, d_weight
+ * (NULL: 1 / rows).  Out: d_loss, 5 floats: L and the weighted sums of policy, kl, H and of the rows that the clip holds; d_logp: lp, NULL: not
+ * kept; d_terms: float[4][rows], policy, kl, H and 1 where the clip holds; d_dlogits: dL/dz, NULL: not formed; may be d_logits
+ * (with the same stride).  Sums are taken in a fixed order: the same call gives the same bits.
+ */
+int dsp_policy_loss(const dsp_policy_loss_desc* desc, const void* d_logits, const int32_t* d_labels, const float* d_old_logp,
+                    const float* d_ref_logp, const float* d_advantage, const float* d_weight, float* d_loss, float* d_logp, float* d_terms,
+                    void* d_dlogits, void* stream);
+
+/*
  * Test support: copies what layer `layer` of the block left in the buffers the backward sweep reads (the
  * recompute of the latest dsp_block_recompute_backward / dsp_block_step, or the latest forward when m_k = 0)
  * to the host after a device synchronisation: the layer's output in the block's storage type (NHWC; float

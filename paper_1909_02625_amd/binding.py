@@ -19,6 +19,10 @@ __all__ = [
     "dsp_block_set_adamw_state", "dsp_pipeline_set_adamw",
     "dsp_norm_residual_desc", "make_norm_residual_desc", "dsp_norm_residual_forward", "dsp_norm_residual_workspace_bytes",
     "dsp_norm_residual_backward",
+    "DSP_ACT_IDENTITY", "DSP_ACT_RELU", "DSP_ACT_GELU", "DSP_ACT_SILU", "DSP_DECAY_SIGMOID", "DSP_DECAY_EXP",
+    "dsp_dense_desc", "make_dense_desc", "dsp_dense_workspace_bytes", "dsp_dense_forward", "dsp_dense_backward",
+    "dsp_recurrence_desc", "make_recurrence_desc", "dsp_recurrence_workspace_bytes", "dsp_recurrence_forward", "dsp_recurrence_backward",
+    "dsp_policy_loss_desc", "make_policy_loss_desc", "dsp_token_logprob", "dsp_policy_loss",
     "dsp_schedule_validate", "dsp_schedule_index", "dsp_schedule_queue_elems", "dsp_schedule_waits",
     "dsp_block_init", "dsp_block_destroy", "dsp_block_forward", "dsp_block_recompute_backward",
     "dsp_param_update", "dsp_param_update_sum", "dsp_pipeline_set_optimizer", "dsp_block_input_slot",
@@ -44,6 +48,8 @@ __all__ = [
 DSP_FP32, DSP_BF16 = 0, 1
 DSP_NORM_NONE, DSP_NORM_RMS, DSP_NORM_LAYER = 0, 1, 2
 DSP_GATE_IDENTITY, DSP_GATE_SIGMOID, DSP_GATE_TANH = 0, 1, 2
+DSP_ACT_IDENTITY, DSP_ACT_RELU, DSP_ACT_GELU, DSP_ACT_SILU = 0, 1, 2, 3
+DSP_DECAY_SIGMOID, DSP_DECAY_EXP = 0, 1
 _OPS = {"conv": 0, "bn": 1, "maxpool": 2, "gap": 3, "linear": 4, "softmax_ce": 5, "add": 6}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -77,6 +83,22 @@ class dsp_norm_residual_desc(C.Structure):
     _fields_ = [("M", C.c_int64)] + [(n, C.c_int32) for n in ("C", "dtype", "post", "pre", "gate_act", "gate_dtype")] + \
                [("gate_rows", C.c_int64)] + [(n, C.c_float) for n in ("alpha", "beta", "eps")] + \
                [(n, C.c_int64) for n in ("x_stride", "z_stride", "y_stride", "h_stride", "gate_stride")]
+
+
+class dsp_dense_desc(C.Structure):
+    _fields_ = [("M", C.c_int64)] + [(n, C.c_int32) for n in ("cin", "cout", "dtype", "act")] + \
+               [(n, C.c_int64) for n in ("x_stride", "y_stride")]
+
+
+class dsp_recurrence_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64)] + [(n, C.c_int32) for n in ("sequences", "steps", "C", "dtype", "decay", "coupled")] + \
+               [(n, C.c_int64) for n in ("x_stride", "f_stride", "h_stride")]
+
+
+class dsp_policy_loss_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "vocab", "dtype")] + \
+               [(n, C.c_float) for n in ("clip_low", "clip_high", "kl_coef", "entropy_coef", "temperature")] + \
+               [(n, C.c_int64) for n in ("logits_stride", "grad_stride")]
 
 
 def lib_path():
@@ -188,6 +210,14 @@ _SIGNATURES = {
     "dsp_norm_residual_forward": [C.POINTER(dsp_norm_residual_desc)] + [_vp] * 12,
     "dsp_norm_residual_workspace_bytes": [C.POINTER(dsp_norm_residual_desc), C.POINTER(_sz)],
     "dsp_norm_residual_backward": [C.POINTER(dsp_norm_residual_desc)] + [_vp] * 18 + [_sz, _vp],
+    "dsp_dense_workspace_bytes": [C.POINTER(dsp_dense_desc), _i32, C.POINTER(_sz)],
+    "dsp_dense_forward": [C.POINTER(dsp_dense_desc)] + [_vp] * 7 + [_sz, _vp],
+    "dsp_dense_backward": [C.POINTER(dsp_dense_desc)] + [_vp] * 8 + [_sz, _vp],
+    "dsp_recurrence_workspace_bytes": [C.POINTER(dsp_recurrence_desc), C.POINTER(_sz)],
+    "dsp_recurrence_forward": [C.POINTER(dsp_recurrence_desc)] + [_vp] * 7 + [_sz, _vp],
+    "dsp_recurrence_backward": [C.POINTER(dsp_recurrence_desc)] + [_vp] * 11 + [_sz, _vp],
+    "dsp_token_logprob": [C.POINTER(dsp_policy_loss_desc)] + [_vp] * 5,
+    "dsp_policy_loss": [C.POINTER(dsp_policy_loss_desc)] + [_vp] * 11,
     "dsp_block_get_activation": [_vp, _i32, _vp, _sz],
     "dsp_block_get_pool_argmax": [_vp, _i32, _vp, _sz],
     "dsp_conv_backward_weight_static_bytes": [C.POINTER(_sz)],
@@ -740,6 +770,66 @@ def dsp_norm_residual_backward(desc, d_dh, d_dy, d_y, d_z, d_gate, d_post_gain, 
                                            _ptr(d_pre_stats), _ptr(d_dx), _ptr(d_dz), _ptr(d_dgate), _ptr(d_dpost_gain),
                                            _ptr(d_dpost_bias), _ptr(d_dpre_gain), _ptr(d_dpre_bias), _ptr(d_workspace),
                                            workspace_bytes, _stream(stream)), "dsp_norm_residual_backward")
+
+
+# ---- products, recurrence and policy loss of residual blocks ------------------------------------------
+def make_dense_desc(M, cin, cout, dtype, act=0, x_stride=0, y_stride=0):
+    return dsp_dense_desc(M, cin, cout, dtype, act, x_stride, y_stride)
+
+
+def dsp_dense_workspace_bytes(desc, backward=False):
+    out = C.c_size_t()
+    check(lib().dsp_dense_workspace_bytes(C.byref(desc), int(backward), C.byref(out)), "dsp_dense_workspace_bytes")
+    return out.value
+
+
+def dsp_dense_forward(desc, d_x, d_w, d_bias, d_residual, d_y, d_pre=None, d_workspace=None, workspace_bytes=0, stream=None):
+    check(lib().dsp_dense_forward(C.byref(desc), _ptr(d_x), _ptr(d_w), _ptr(d_bias), _ptr(d_residual), _ptr(d_y), _ptr(d_pre),
+                                  _ptr(d_workspace), workspace_bytes, _stream(stream)), "dsp_dense_forward")
+
+
+def dsp_dense_backward(desc, d_dy, d_x, d_w, d_pre, d_dx, d_dw, d_dbias, d_workspace, workspace_bytes, stream=None):
+    check(lib().dsp_dense_backward(C.byref(desc), _ptr(d_dy), _ptr(d_x), _ptr(d_w), _ptr(d_pre), _ptr(d_dx), _ptr(d_dw), _ptr(d_dbias),
+                                   _ptr(d_workspace), workspace_bytes, _stream(stream)), "dsp_dense_backward")
+
+
+def make_recurrence_desc(sequences, steps, rows, C_, dtype, decay=0, coupled=True, x_stride=0, f_stride=0, h_stride=0):
+    return dsp_recurrence_desc(rows, sequences, steps, C_, dtype, decay, int(bool(coupled)), x_stride, f_stride, h_stride)
+
+
+def dsp_recurrence_workspace_bytes(desc):
+    out = C.c_size_t()
+    check(lib().dsp_recurrence_workspace_bytes(C.byref(desc), C.byref(out)), "dsp_recurrence_workspace_bytes")
+    return out.value
+
+
+def dsp_recurrence_forward(desc, d_x, d_f, d_offsets, d_state_in, d_h, d_state_out=None, d_workspace=None, workspace_bytes=0, stream=None):
+    check(lib().dsp_recurrence_forward(C.byref(desc), _ptr(d_x), _ptr(d_f), _ptr(d_offsets), _ptr(d_state_in), _ptr(d_h), _ptr(d_state_out),
+                                       _ptr(d_workspace), workspace_bytes, _stream(stream)), "dsp_recurrence_forward")
+
+
+def dsp_recurrence_backward(desc, d_dh, d_dstate_out, d_x, d_f, d_h, d_offsets, d_state_in, d_dx, d_df, d_dstate_in=None, d_workspace=None,
+                            workspace_bytes=0, stream=None):
+    check(lib().dsp_recurrence_backward(C.byref(desc), _ptr(d_dh), _ptr(d_dstate_out), _ptr(d_x), _ptr(d_f), _ptr(d_h), _ptr(d_offsets),
+                                        _ptr(d_state_in), _ptr(d_dx), _ptr(d_df), _ptr(d_dstate_in), _ptr(d_workspace), workspace_bytes,
+                                        _stream(stream)), "dsp_recurrence_backward")
+
+
+def make_policy_loss_desc(rows, vocab, dtype, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0, temperature=1.0, logits_stride=0,
+                          grad_stride=0):
+    return dsp_policy_loss_desc(rows, vocab, dtype, clip_low, clip_high, kl_coef, entropy_coef, temperature, logits_stride, grad_stride)
+
+
+def dsp_token_logprob(desc, d_logits, d_labels, d_logp, d_entropy=None, stream=None):
+    check(lib().dsp_token_logprob(C.byref(desc), _ptr(d_logits), _ptr(d_labels), _ptr(d_logp), _ptr(d_entropy), _stream(stream)),
+          "dsp_token_logprob")
+
+
+def dsp_policy_loss(desc, d_logits, d_labels, d_old_logp, d_ref_logp, d_advantage, d_weight, d_loss, d_logp, d_terms, d_dlogits=None,
+                    stream=None):
+    check(lib().dsp_policy_loss(C.byref(desc), _ptr(d_logits), _ptr(d_labels), _ptr(d_old_logp), _ptr(d_ref_logp), _ptr(d_advantage),
+                                _ptr(d_weight), _ptr(d_loss), _ptr(d_logp), _ptr(d_terms), _ptr(d_dlogits), _stream(stream)),
+          "dsp_policy_loss")
 
 
 def dsp_block_get_activation(b, layer, nbytes):

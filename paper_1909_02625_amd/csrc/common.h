@@ -406,6 +406,16 @@ struct VecIO<bf16_t, 1> {
     __device__ static inline void store(bf16_t* p, const float (&v)[1]) { *p = float_to_bf16(v[0]); }
 };
 
+// exp(-a) for a >= 0 (or NaN) from the hardware's power of two, within one unit of its last place.  The exponent's product is rounded,
+// which alone would cost a 2^-24 of the result: what hi ln(2), with ln(2) in two parts, lacks of -a is a factor 1 + off.  Relative error
+// 3 * 2^-24; 0 below 2^-126.  (Where a is infinite off is no number, and the bound makes it one; p is NaN only where a is.)
+__device__ inline float exp_of_minus(float a)
+{
+    constexpr float kLn2 = 0.693147182f, kRest = -1.90465421e-9f;  // ln(2) = kLn2 + kRest
+    const float hi = a * -1.44269504f, p = __builtin_amdgcn_exp2f(hi);
+    const float off = fminf(fmaf(hi, -kRest, fmaf(hi, -kLn2, -a)), 1.f);
+    return fmaf(p, off, p);
+}
 
 // n / d for n < 2^31 with precomputed mul = floor(2^32 * (2^sh - d) / d) + 1, sh = ceil(log2 d).
 __device__ inline uint32_t fast_div(uint32_t n, uint32_t mul, uint32_t sh) { return (__umulhi(n, mul) + n) >> sh; }

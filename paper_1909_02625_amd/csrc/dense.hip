@@ -1,0 +1,566 @@
+// The product in a residual block's branch with what follows it, and its gradients:
+//
+//   p = x W^T + b,  y = act(p) + residual;   g = dy act'(p),  dx = g W,  dW = g^T x,  db = column sums of g
+//
+// All three products are one contraction C[m][n] = sum_k A(m, k) B(n, k), whose operands lie with k or with their row as the
+// fast index.  Both go into LDS as they lie in memory.
+#include "common.h"
+
+#include <algorithm>
+
+namespace dsp {
+namespace {
+
+typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef float F16 __attribute__((ext_vector_type(16)));
+typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+typedef short S4 __attribute__((ext_vector_type(4)));
+
+// ---- activations ---------------------------------------------------------------------------------
+// Phi(x) = erfc(-x / sqrt 2) / 2 for x <= 0 as t P(t) exp(-x^2 / 2), t = 1 / (1 + 0.4 |x| / sqrt 2): P is a polynomial fitted to
+// erfc(z) exp(z^2) / (2 t) with the least largest relative error over z >= 0, 1.3e-7; in floats, with the exponential, 12 * 2^-24.
+// exp(-x^2 / 2) is given: the derivative of gelu wants it too.
+__device__ inline float normal_below(float ax, float e)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.282842712f, ax, 1.f));
+    float p = 0.0251324802f;
+    p = fmaf(p, t, -0.0914566156f);
+    p = fmaf(p, t, 0.0845527159f);
+    p = fmaf(p, t, -0.00281273362f);
+    p = fmaf(p, t, 0.0707202607f);
+    p = fmaf(p, t, 0.0842696947f);
+    p = fmaf(p, t, 0.103921543f);
+    p = fmaf(p, t, 0.112834786f);
+    p = fmaf(p, t, 0.112837931f);
+    return p * t * e;
+}
+// exp(-x^2 / 2): what rounding the square loses is a factor.
+__device__ inline float bell(float x)
+{
+    const float h = x * x, low = fmaf(x, x, -h), e = exp_of_minus(0.5f * h);
+    return fmaf(e * -0.5f, low, e);
+}
+// What lies so far below 0 that no float is left of the activation is brought to where the formulas have no infinity in them.
+__device__ inline float act_of(int act, float x)
+{
+    if (act == DSP_ACT_RELU) return x < 0.f ? 0.f : x;
+    if (act == DSP_ACT_GELU) {
+        x = x < -16.f ? -16.f : x;
+        const float q = normal_below(fabsf(x), bell(fminf(fabsf(x), 16.f)));
+        return x * (x > 0.f ? 1.f - q : q);
+    }
+    if (act == DSP_ACT_SILU) {
+        x = x < -128.f ? -128.f : x;
+        const float e = exp_of_minus(fabsf(x)), q = __builtin_amdgcn_rcpf(1.f + e);
+        return x * (x >= 0.f ? q : e * q);
+    }
+    return x;
+}
+__device__ inline float act_slope(int act, float x)
+{
+    if (act == DSP_ACT_RELU) return x > 0.f ? 1.f : 0.f;
+    if (act == DSP_ACT_GELU) {
+        x = fabsf(x) > 16.f ? copysignf(16.f, x) : x;
+        const float e = bell(x), q = normal_below(fabsf(x), e);
+        return fmaf(x * 0.398942280f, e, x > 0.f ? 1.f - q : q);
+    }
+    if (act == DSP_ACT_SILU) {
+        x = fabsf(x) > 128.f ? copysignf(128.f, x) : x;
+        const float e = exp_of_minus(fabsf(x)), q = __builtin_amdgcn_rcpf(1.f + e), a = x >= 0.f ? q : e * q, rest = x >= 0.f ? e * q : q;
+        return a * fmaf(x, rest, 1.f);
+    }
+    return 1.f;
+}
+
+// ---- what is done with a run of eight results -------------------------------------------------------
+struct OutArgs {
+    void* out;
+    const float* bias;
+    const void* residual;
+    void* pre;
+    int64_t stride;  // of out, residual and pre
+    int M, N, act;
+    bool whole;      // runs of eight: whole ones, all on 16-byte addresses
+};
+
+template <typename T>
+__device__ inline void load8(const T* p, float (&v)[8])
+{
+    constexpr int VW = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 8; h += VW) {
+        float t[VW];
+        VecIO<T, VW>::load(p + h, t);
+#pragma unroll
+        for (int i = 0; i < VW; ++i) v[h + i] = t[i];
+    }
+}
+template <typename T>
+__device__ inline void store8(T* p, const float (&v)[8])
+{
+    constexpr int VW = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 8; h += VW) {
+        float t[VW];
+#pragma unroll
+        for (int i = 0; i < VW; ++i) t[i] = v[h + i];
+        VecIO<T, VW>::store(p + h, t);
+    }
+}
+
+// Results m, n .. n + 7 (those within N).  Rounded once: bias, activation and residual are taken in float.
+template <typename T>
+__device__ inline void finish_run(const OutArgs& o, int64_t m, int n, float (&v)[8])
+{
+    if (m >= o.M || n >= o.N) return;
+    const int64_t at = m * o.stride + n;
+    if (o.whole) {
+        if (o.bias) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += o.bias[n + i];
+        }
+        if (o.pre) store8<T>((T*)o.pre + at, v);
+        if (o.act != DSP_ACT_IDENTITY) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = act_of(o.act, v[i]);
+        }
+        if (o.residual) {
+            float r[8];
+            load8<T>((const T*)o.residual + at, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += r[i];
+        }
+        store8<T>((T*)o.out + at, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (n + i >= o.N) break;
+        float u = v[i];
+        if (o.bias) u += o.bias[n + i];
+        if (o.pre) ((T*)o.pre)[at + i] = from_float<T>(u);
+        u = act_of(o.act, u);
+        if (o.residual) u += to_float<T>(((const T*)o.residual)[at + i]);
+        ((T*)o.out)[at + i] = from_float<T>(u);
+    }
+}
+
+// ---- the contraction --------------------------------------------------------------------------------
+struct GemmArgs {
+    const void *a, *b;  // A(m, k), B(n, k): element (m, k) at m stride + k, or, k outside, at k stride + m
+    int64_t as, bs;
+    int M, N, K;
+    int tiles_m, tiles_n;
+    OutArgs o;
+};
+
+template <typename T>
+struct Mma32;
+// 32 x 32 results of a wave; a lane's operands: 16 bytes of consecutive k of row lane % 32, those of lanes 32 .. 63 behind
+// those of lanes 0 .. 31.  (fp32: one k of each half at a time; any order of k will do, so long as both operands have it.)
+template <>
+struct Mma32<bf16_t> {
+    __device__ static inline void run(U4 a, U4 b, F16& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(B8, a), __builtin_bit_cast(B8, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma32<float> {
+    __device__ static inline void run(U4 a, U4 b, F16& c)
+    {
+        const F4 fa = __builtin_bit_cast(F4, a), fb = __builtin_bit_cast(F4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[i], c, 0, 0, 0);
+    }
+};
+
+// A tile of R rows and KB bytes of k of one operand in LDS.  K inside: R rows of KB bytes; chunk c (16 bytes) of row r lies at place
+// c ^ swz(r), so that the 16 rows that 16 lanes read at the same k fall on all 64 banks.  K outside: one row of R elements for each k, of
+// which a row's chunks change places so that the rows read together do not meet in a bank.
+template <typename T, bool MAJOR, int R, int KB>
+struct OperandTile {
+    static constexpr int E = 16 / (int)sizeof(T), BK = KB / (int)sizeof(T), CHUNKS = R * KB / 16;
+    static constexpr bool K_OUTSIDE = MAJOR;
+    static constexpr int ROWB = MAJOR ? R * (int)sizeof(T) : KB, CPR = ROWB / 16;
+    static_assert(KB == 128 || KB == 64, "bytes of k in a row");
+    static_assert(!MAJOR || ROWB >= 256, "rows of four banks' turns");
+    __device__ static inline int swz(int row)
+    {
+        if (!MAJOR) return KB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+        return sizeof(T) == 2 ? (row & 3) << 2 : ((row >> 2) & 1) << 3;
+    }
+    // chunk i of the tile: row and chunk within it, and where it lies
+    __device__ static inline int row_of(int i) { return i / CPR; }
+    __device__ static inline int place(int row, int chunk) { return row * ROWB + ((chunk ^ swz(row)) << 4); }
+
+    // Operand of MFMA block `blk` (32 rows) at k step ks (32 bytes of k a row).
+    __device__ static inline U4 fragment(const char* tile, int blk, int ks, int lane)
+    {
+        if constexpr (!MAJOR) {
+            return *(const U4*)(tile + place(blk * 32 + (lane & 31), 2 * ks + (lane >> 5)));
+        } else if constexpr (sizeof(T) == 2) {
+            // 16 lanes address four k of 16 rows, four rows each, and come away with four k of one row
+            const int j = lane & 15, k = 16 * ks + 8 * (lane >> 5) + (j >> 2), chunk = blk * 4 + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1);
+            const char* p = tile + place(k, chunk) + (j & 1) * 8;
+            const U2 lo = tr16(p), hi = tr16(p + 4 * ROWB);  // (rows four apart change places alike)
+            return U4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            const int k = 8 * ks + 4 * (lane >> 5), m = blk * 32 + (lane & 31);
+            U4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *(const uint32_t*)(tile + place(k + i, m >> 2) + (m & 3) * 4);
+            return v;
+        }
+    }
+    __device__ static inline U2 tr16(const char* p)
+    {
+        return __builtin_bit_cast(U2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4*)(p)));
+    }
+};
+
+// Up to E consecutive elements from p on, any alignment; zeros behind them.
+template <typename T>
+__device__ inline U4 load_chunk(const T* p, int count)
+{
+    constexpr int E = 16 / sizeof(T);
+    U4 v = {};
+    if (count >= E) {
+        __builtin_memcpy(&v, p, 16);
+    } else if (count > 0) {
+        T t[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) t[i] = i < count ? p[i] : T{};
+        __builtin_memcpy(&v, t, 16);
+    }
+    return v;
+}
+
+template <typename T_, bool AM_, bool BM_MAJOR, int BM_, int BN_, int WM_, int WN_, int KB_>
+struct StagedTile {
+    typedef T_ T;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_;
+    static constexpr int THREADS = 64 * WM * WN, TM = BM / (32 * WM), TN = BN / (32 * WN), NKS = KB / 32;
+    typedef OperandTile<T, AM_, BM, KB> A;
+    typedef OperandTile<T, BM_MAJOR, BN, KB> B;
+    static constexpr int STAGE = (BM + BN) * KB, OUT_ROW = TN * 32 + 4, OUT = WM * WN * 32 * OUT_ROW * 4;
+    static constexpr int LDS = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+};
+
+// The place of block b of nb among the tiles: the blocks of one XCD (every eighth) take neighbours.
+__device__ inline unsigned xcd_order(unsigned b, unsigned nb)
+{
+    const unsigned q = nb / 8, r = nb % 8, xcd = b % 8;
+    return xcd * q + (xcd < r ? xcd : r) + b / 8;
+}
+
+// The accumulators hold the transposed tile: a lane has, for row lane % 32 of a block, runs of four consecutive columns.  Through LDS,
+// 32 rows of a wave at a time, they become runs of eight, whole lines of a row.
+template <typename TL, int TM, int TN>
+__device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const OutArgs& o, int64_t m0, int n0, int wave, int lane)
+{
+    constexpr int ROW = TL::OUT_ROW, LPR = TN * 4, RPP = 64 / LPR;
+    float* const mine = (float*)smem + wave * 32 * ROW;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(F4*)(mine + (lane & 31) * ROW + j * 32 + 8 * q + 4 * (lane >> 5)) =
+                    F4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < 32; r += RPP) {
+            const int row = r + lane / LPR, col = lane % LPR * 8;
+            const F4 u = *(const F4*)(mine + row * ROW + col), w = *(const F4*)(mine + row * ROW + col + 4);
+            float v[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+            finish_run<typename TL::T>(o, m0 + i * 32 + row, n0 + col, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <typename TL>
+__global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
+{
+    typedef typename TL::T T;
+    typedef typename TL::A A;
+    typedef typename TL::B B;
+    __shared__ __attribute__((aligned(16))) char smem[TL::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / TL::WN, wn = wave % TL::WN;
+    const unsigned tile = xcd_order(blockIdx.x, gridDim.x);
+    const int64_t m0 = (int64_t)(tile / g.tiles_n) * TL::BM;
+    const int n0 = (int)(tile % g.tiles_n) * TL::BN;
+    constexpr int PA = A::CHUNKS / TL::THREADS, PB = B::CHUNKS / TL::THREADS;
+    static_assert(PA * TL::THREADS == A::CHUNKS && PB * TL::THREADS == B::CHUNKS, "whole chunks for every thread");
+    U4 ra[PA], rb[PB];
+    auto load = [&](auto op, const T* p, int64_t stride, int64_t r0, int rows, int k0, auto& reg, auto count) {
+        typedef decltype(op) O;
+        constexpr bool MAJOR = O::K_OUTSIDE;
+#pragma unroll
+        for (int i = 0; i < decltype(count)::value; ++i) {
+            const int idx = tid + i * TL::THREADS, row = O::row_of(idx), c = idx % O::CPR * O::E;
+            const int64_t r = r0 + (MAJOR ? c : row);
+            const int k = k0 + (MAJOR ? row : c);
+            int left = r < rows && k < g.K ? (int)(MAJOR ? (rows - r < O::E ? rows - r : O::E) : (g.K - k < O::E ? g.K - k : O::E)) : 0;
+            reg[i] = load_chunk<T>(left ? p + (MAJOR ? k * stride + r : r * stride + k) : p, left);
+        }
+    };
+    auto keep = [&](auto op, char* to, auto& reg, auto count) {
+        typedef decltype(op) O;
+#pragma unroll
+        for (int i = 0; i < decltype(count)::value; ++i) {
+            const int idx = tid + i * TL::THREADS;
+            *(U4*)(to + O::place(O::row_of(idx), idx % O::CPR)) = reg[i];
+        }
+    };
+    auto load_both = [&](int k0) {
+        load(A{}, (const T*)g.a, g.as, m0, g.M, k0, ra, std::integral_constant<int, PA>{});
+        load(B{}, (const T*)g.b, g.bs, n0, g.N, k0, rb, std::integral_constant<int, PB>{});
+    };
+    auto keep_both = [&](int stage) {
+        keep(A{}, smem + stage * TL::STAGE, ra, std::integral_constant<int, PA>{});
+        keep(B{}, smem + stage * TL::STAGE + TL::BM * TL::KB, rb, std::integral_constant<int, PB>{});
+    };
+    F16 acc[TL::TM][TL::TN];
+#pragma unroll
+    for (int i = 0; i < TL::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TL::TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    const int nk = (g.K + A::BK - 1) / A::BK;
+    load_both(0);
+    keep_both(0);
+    __syncthreads();
+    for (int kt = 0; kt < nk; ++kt) {
+        if (kt + 1 < nk) load_both((kt + 1) * A::BK);
+        const char* s = smem + (kt & 1) * TL::STAGE;
+#pragma unroll
+        for (int ks = 0; ks < TL::NKS; ++ks) {
+            U4 fa[TL::TM], fb[TL::TN];
+#pragma unroll
+            for (int i = 0; i < TL::TM; ++i) fa[i] = A::fragment(s, wm * TL::TM + i, ks, lane);
+#pragma unroll
+            for (int j = 0; j < TL::TN; ++j) fb[j] = B::fragment(s + TL::BM * TL::KB, wn * TL::TN + j, ks, lane);
+#pragma unroll
+            for (int i = 0; i < TL::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TL::TN; ++j) Mma32<T>::run(fb[j], fa[i], acc[i][j]);
+        }
+        if (kt + 1 < nk) keep_both((kt + 1) & 1);
+        __syncthreads();
+    }
+    finish_tile<TL>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
+}
+
+// ---- the gradient in front of the activation, and its column sums ------------------------------------
+struct GradArgs {
+    const void *dy, *pre;
+    void* g;         // nullptr: the activation is the identity, or nobody reads g
+    float* partial;  // [parts][N], or nullptr
+    int64_t ys, gs;
+    int M, N, act, rows_per_part;
+};
+constexpr int kGradThreads = 256, kGradCols = 64;
+
+// A workgroup has 64 columns, 8 lanes a row, 32 rows at a time, and a part of the rows.  g is rounded to the storage type because
+// the matrix instructions read that; the column sums are of the values before.
+template <typename T>
+__global__ __launch_bounds__(kGradThreads) void dense_grad_kernel(GradArgs a)
+{
+    __shared__ float sums[32][kGradCols + 4];
+    const int c = threadIdx.x % 8 * 8, r = threadIdx.x / 8, n = blockIdx.x * kGradCols + c;
+    const int64_t first = (int64_t)blockIdx.y * a.rows_per_part, last = first + a.rows_per_part < a.M ? first + a.rows_per_part : a.M;
+    float s[8] = {};
+    for (int64_t m = first + r; m < last; m += 32)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (n + i >= a.N) continue;
+            float v = to_float<T>(((const T*)a.dy)[m * a.ys + n + i]);
+            if (a.pre) v *= act_slope(a.act, to_float<T>(((const T*)a.pre)[m * a.ys + n + i]));
+            if (a.g) ((T*)a.g)[m * a.gs + n + i] = from_float<T>(v);
+            s[i] += v;
+        }
+    if (!a.partial) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[r][c + i] = s[i];
+    __syncthreads();
+    const int col = threadIdx.x;
+    if (col < kGradCols && blockIdx.x * kGradCols + col < a.N) {
+        float t = 0.f;
+        for (int q = 0; q < 32; ++q) t += sums[q][col];
+        a.partial[(int64_t)blockIdx.y * a.N + blockIdx.x * kGradCols + col] = t;
+    }
+}
+
+__global__ __launch_bounds__(256) void dense_bias_kernel(const float* partial, float* dbias, int parts, int N)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= N) return;
+    float s = 0.f;
+    for (int p = 0; p < parts; ++p) s += partial[(int64_t)p * N + n];
+    dbias[n] = s;
+}
+
+// ---- host --------------------------------------------------------------------------------------------
+constexpr int kMaxWidth = 1 << 24;
+
+int64_t stride_of(int64_t s, int32_t n) { return s ? s : n; }
+
+int check_desc(const dsp_dense_desc* d, const char* who)
+{
+    DSP_REQUIRE(d, DSP_EINVAL, "%s: null descriptor", who);
+    DSP_REQUIRE(d->dtype == DSP_FP32 || d->dtype == DSP_BF16, DSP_EINVAL, "%s: bad type", who);
+    DSP_REQUIRE(d->act == DSP_ACT_IDENTITY || d->act == DSP_ACT_RELU || d->act == DSP_ACT_GELU || d->act == DSP_ACT_SILU, DSP_EINVAL,
+                "%s: bad activation", who);
+    DSP_REQUIRE(d->M > 0 && d->M < (1ll << 31) && d->cin > 0 && d->cin <= kMaxWidth && d->cout > 0 && d->cout <= kMaxWidth, DSP_EINVAL,
+                "%s: bad shape", who);
+    DSP_REQUIRE((d->x_stride == 0 || (d->x_stride >= d->cin && d->x_stride < (1ll << 31))) &&
+                    (d->y_stride == 0 || (d->y_stride >= d->cout && d->y_stride < (1ll << 31))),
+                DSP_EINVAL, "%s: a row stride is shorter than the row", who);
+    // (a grid holds fewer than 2^32 threads: tiles of 64 x 64 results by 256 threads, and strips of the column sums)
+    const double tiles = ((double)d->M / 64 + 1) * ((double)std::max(d->cin, d->cout) / 64 + 1) +
+                         ((double)d->cin / 64 + 1) * ((double)d->cout / 64 + 1);
+    DSP_REQUIRE(tiles < (double)(1 << 23), DSP_EINVAL, "%s: too many tiles", who);
+    return DSP_OK;
+}
+
+bool on(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+
+// The rows of the column sums' parts: as many workgroups as four for a compute unit.
+struct BackPlan {
+    int parts, rows_per_part;
+    int64_t gs;
+    size_t g_bytes, bytes;
+};
+size_t rounded16(size_t n) { return (n + 15) / 16 * 16; }
+BackPlan back_plan(const dsp_dense_desc* d)
+{
+    BackPlan p;
+    const int strips = ceil_div(d->cout, kGradCols);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(1024 / strips, ceil_div(d->M, 32)));
+    p.rows_per_part = (int)((d->M + want - 1) / want);
+    p.parts = ceil_div(d->M, p.rows_per_part);
+    p.gs = (d->cout + 7) / 8 * 8;
+    p.g_bytes = d->act == DSP_ACT_IDENTITY ? 0 : rounded16((size_t)d->M * p.gs * dtype_size(d->dtype));
+    p.bytes = p.g_bytes + rounded16((size_t)p.parts * d->cout * 4);
+    return p;
+}
+
+template <typename T, bool AM, bool BMJ>
+int launch_staged(GemmArgs& g, hipStream_t st, ProfScope& ps)
+{
+    typedef StagedTile<T, AM, BMJ, 128, 128, 2, 2, 64> TL;
+    g.tiles_m = ceil_div(g.M, TL::BM);
+    g.tiles_n = ceil_div(g.N, TL::BN);
+    DSP_LAUNCH(ps, dense_staged_kernel<TL>, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(TL::THREADS), 0, st, g);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+template <bool AM, bool BMJ>
+int contract(int dtype, const char* name, GemmArgs& g, hipStream_t st)
+{
+    const size_t e = dtype_size(dtype);
+    g.o.M = g.M;
+    g.o.N = g.N;
+    g.o.whole = g.N % 8 == 0 && g.o.stride * e % 16 == 0 && on(g.o.out, 16) && on(g.o.residual, 16) && on(g.o.pre, 16);
+    ProfScope ps(name, 2.0 * g.M * g.N * g.K, 0);
+    return dtype == DSP_BF16 ? launch_staged<bf16_t, AM, BMJ>(g, st, ps) : launch_staged<float, AM, BMJ>(g, st, ps);
+}
+
+}  // namespace
+}  // namespace dsp
+
+using namespace dsp;
+
+extern "C" {
+
+int dsp_dense_workspace_bytes(const dsp_dense_desc* d, int32_t backward, size_t* bytes)
+{
+    DSP_REQUIRE(bytes, DSP_EINVAL, "dsp_dense_workspace_bytes: null argument");
+    DSP_TRY(check_desc(d, "dsp_dense_workspace_bytes"));
+    *bytes = backward ? back_plan(d).bytes : 0;
+    return DSP_OK;
+}
+
+int dsp_dense_forward(const dsp_dense_desc* d, const void* d_x, const void* d_w, const float* d_bias, const void* d_residual, void* d_y,
+                      void* d_pre, void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    DSP_TRY(check_desc(d, "dsp_dense_forward"));
+    DSP_REQUIRE(d_x && d_w && d_y, DSP_EINVAL, "dsp_dense_forward: null buffer");
+    const size_t e = dtype_size(d->dtype);
+    DSP_REQUIRE(on(d_x, e) && on(d_w, e) && on(d_bias, 4) && on(d_residual, e) && on(d_y, e) && on(d_pre, e), DSP_EINVAL,
+                "dsp_dense_forward: misaligned buffer");
+    DSP_REQUIRE(d_y != d_x && d_y != d_w && d_pre != d_x && d_pre != d_w && d_pre != d_y && (!d_pre || d_pre != d_residual), DSP_EINVAL,
+                "dsp_dense_forward: y and pre want buffers of their own (y may be the residual)");
+    (void)d_workspace;
+    (void)workspace_bytes;
+    GemmArgs g{};
+    g.a = d_x; g.b = d_w; g.as = stride_of(d->x_stride, d->cin); g.bs = d->cin;
+    g.M = (int)d->M; g.N = d->cout; g.K = d->cin;
+    g.o.out = d_y; g.o.bias = d_bias; g.o.residual = d_residual; g.o.pre = d_pre; g.o.act = d->act;
+    g.o.stride = stride_of(d->y_stride, d->cout);
+    return contract<false, false>(d->dtype, "dense_fwd", g, (hipStream_t)stream);
+}
+
+int dsp_dense_backward(const dsp_dense_desc* d, const void* d_dy, const void* d_x, const void* d_w, const void* d_pre, void* d_dx, void* d_dw,
+                       float* d_dbias, void* d_workspace, size_t workspace_bytes, void* stream)
+{
+    DSP_TRY(check_desc(d, "dsp_dense_backward"));
+    const bool act = d->act != DSP_ACT_IDENTITY;
+    DSP_REQUIRE(d_dy && (d_dx || d_dw || d_dbias) && (!d_dx || d_w) && (!d_dw || d_x) && (!act || d_pre), DSP_EINVAL,
+                "dsp_dense_backward: null buffer");
+    const size_t e = dtype_size(d->dtype);
+    DSP_REQUIRE(on(d_dy, e) && on(d_x, e) && on(d_w, e) && on(d_pre, e) && on(d_dx, e) && on(d_dw, e) && on(d_dbias, 4), DSP_EINVAL,
+                "dsp_dense_backward: misaligned buffer");
+    DSP_REQUIRE((!d_dx || (d_dx != d_dy && d_dx != d_x && d_dx != d_w && d_dx != d_pre && d_dx != d_dw)) &&
+                    (!d_dw || (d_dw != d_dy && d_dw != d_x && d_dw != d_w && d_dw != d_pre)),
+                DSP_EINVAL, "dsp_dense_backward: dx and dw want buffers of their own");
+    const BackPlan p = back_plan(d);
+    DSP_REQUIRE(d_workspace && workspace_bytes >= p.bytes && on(d_workspace, 16), DSP_EINVAL,
+                "dsp_dense_backward: workspace too small or not 16-byte aligned (%zu < %zu)", workspace_bytes, p.bytes);
+    hipStream_t st = (hipStream_t)stream;
+    const int64_t ys = stride_of(d->y_stride, d->cout), xs = stride_of(d->x_stride, d->cin);
+    const bool g_read = act && (d_dx || d_dw);
+    const void* grad = act ? d_workspace : d_dy;
+    const int64_t gs = act ? p.gs : ys;
+    if (g_read || d_dbias) {
+        GradArgs a;
+        a.dy = d_dy; a.pre = act ? d_pre : nullptr; a.g = g_read ? d_workspace : nullptr;
+        a.partial = d_dbias ? (float*)((char*)d_workspace + p.g_bytes) : nullptr;
+        a.ys = ys; a.gs = p.gs; a.M = (int)d->M; a.N = d->cout; a.act = d->act; a.rows_per_part = p.rows_per_part;
+        const dim3 grid(ceil_div(d->cout, kGradCols), p.parts);
+        ProfScope ps("dense_grad", (double)d->M * d->cout * e * (1 + act + g_read), 1);
+        if (d->dtype == DSP_BF16) DSP_LAUNCH(ps, dense_grad_kernel<bf16_t>, grid, dim3(kGradThreads), 0, st, a);
+        else DSP_LAUNCH(ps, dense_grad_kernel<float>, grid, dim3(kGradThreads), 0, st, a);
+        DSP_HIP(hipGetLastError());
+        if (d_dbias) {
+            ProfScope pb("dense_bias", 4.0 * p.parts * d->cout, 1);
+            DSP_LAUNCH(pb, dense_bias_kernel, dim3(ceil_div(d->cout, 256)), dim3(256), 0, st, a.partial, d_dbias, p.parts, d->cout);
+            DSP_HIP(hipGetLastError());
+        }
+    }
+    if (d_dx) {
+        GemmArgs g{};
+        g.a = grad; g.as = gs; g.b = d_w; g.bs = d->cin;
+        g.M = (int)d->M; g.N = d->cin; g.K = d->cout;
+        g.o.out = d_dx; g.o.stride = xs;
+        DSP_TRY((contract<false, true>(d->dtype, "dense_dx", g, st)));
+    }
+    if (d_dw) {
+        GemmArgs g{};
+        g.a = grad; g.as = gs; g.b = d_x; g.bs = xs;
+        g.M = d->cout; g.N = d->cin; g.K = (int)d->M;
+        g.o.out = d_dw; g.o.stride = d->cin;
+        DSP_TRY((contract<true, true>(d->dtype, "dense_dw", g, st)));
+    }
+    return DSP_OK;
+}
+
+}  // extern "C"
