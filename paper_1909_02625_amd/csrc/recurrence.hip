@@ -36,9 +36,6 @@ __device__ inline void gate_of(int decay, float f, float& a, float& b)
     const float s = f * (1.f + f * (1.f / 2 + f * (1.f / 6 + f * (1.f / 24 + f * (1.f / 120 + f * (1.f / 720 + f * (1.f / 5040)))))));
     b = fabsf(f) < 0.35f ? -s : 1.f - a;
 }
-// a h, from whichever of a and 1 - a has more digits of it.
-__device__ inline float decayed(float a, float b, float h) { return fabsf(b) < 0.5f ? fmaf(-b, h, h) : a * h; }
-
 // The rows of a sequence: whatever the offsets hold, rows that there are and no more than `steps` of them.
 __device__ inline int64_t rows_of(const ScanArgs& p, int s, int& length)
 {
@@ -52,76 +49,339 @@ __device__ inline int64_t rows_of(const ScanArgs& p, int s, int& length)
     return first;
 }
 
-constexpr int kWalkThreads = 64;
+// The decay of a step or of many: what h is multiplied by is a + c, where c is the part of 1 - (1 - a) that a has no digits for.  h (a + c) + u are two
+// operations; only where a is the larger of the two does c hold anything.
+__device__ inline float rest_of(float a, float b) { return b < 0.5f ? (1.f - a) - b : 0.f; }
+__device__ inline float step_of(float a, float c, float h, float u) { return fmaf(a, h, fmaf(c, h, u)); }
 
-// A lane walks through a sequence for VW channels.
-template <typename T, int VW>
+// ---- four bytes of a row: a lane's channels -----------------------------------------------------------
+template <typename T>
+struct Lane4;
+template <>
+struct Lane4<float> {
+    static constexpr int VW = 1;
+    static constexpr uint32_t kInfinity = 0x7f800000u;
+    __device__ static inline void unpack(uint32_t r, float (&v)[1]) { v[0] = __uint_as_float(r); }
+    __device__ static inline uint32_t pack(const float (&v)[1]) { return __float_as_uint(v[0]); }
+    __device__ static inline uint32_t load(const float* p, bool) { return __float_as_uint(*p); }
+    __device__ static inline void store(float* p, uint32_t r, bool) { *p = __uint_as_float(r); }
+};
+template <>
+struct Lane4<bf16_t> {
+    static constexpr int VW = 2;
+    static constexpr uint32_t kInfinity = 0x7f807f80u;
+    __device__ static inline void unpack(uint32_t r, float (&v)[2])
+    {
+        v[0] = __uint_as_float(r << 16);
+        v[1] = __uint_as_float(r & 0xffff0000u);
+    }
+    __device__ static inline uint32_t pack(const float (&v)[2]) { return pack_bf16x2(v[0], v[1]); }
+    // (any alignment; the last channel of an odd number is alone)
+    __device__ static inline uint32_t load(const bf16_t* p, bool both)
+    {
+        uint32_t r = p->bits;
+        if (both) __builtin_memcpy(&r, p, 4);
+        return r;
+    }
+    __device__ static inline void store(bf16_t* p, uint32_t r, bool both)
+    {
+        if (both) __builtin_memcpy(p, &r, 4);
+        else p->bits = (uint16_t)r;
+    }
+};
+
+// ---- many short sequences, or one step: a lane walks through a sequence --------------------------------
+constexpr int kWalkThreads = 256, kWalkAhead = 8;
+
+template <typename T>
 __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_kernel(ScanArgs p)
 {
+    typedef Lane4<T> L;
+    constexpr int VW = L::VW;
     const int c = (blockIdx.x * kWalkThreads + threadIdx.x) * VW, s = blockIdx.y;
     if (c >= p.C) return;
+    const bool both = c + VW <= p.C;
     int n;
     const int64_t first = rows_of(p, s, n);
     float h[VW] = {};
     const int64_t at = (int64_t)s * p.C + c;
     if (p.state)
 #pragma unroll
-        for (int v = 0; v < VW; ++v) h[v] = p.state[at + v];
-    for (int t = 0; t < n; ++t) {
-        const int64_t row = first + t;
-        float x[VW], f[VW];
-        VecIO<T, VW>::load((const T*)p.x + row * p.xs + c, x);
-        VecIO<T, VW>::load((const T*)p.f + row * p.fs + c, f);
+        for (int v = 0; v < VW; ++v) h[v] = v == 0 || both ? p.state[at + v] : 0.f;
+    const T* x = (const T*)p.x + first * p.xs + c;
+    const T* f = (const T*)p.f + first * p.fs + c;
+    T* out = (T*)p.out + first * p.hs + c;
+    auto one = [&](uint32_t rx, uint32_t rf) {
+        float xv[VW], fv[VW];
+        L::unpack(rx, xv);
+        L::unpack(rf, fv);
 #pragma unroll
         for (int v = 0; v < VW; ++v) {
             float a, b;
-            gate_of(p.decay, f[v], a, b);
-            h[v] = decayed(a, b, h[v]) + (p.coupled ? b * x[v] : x[v]);
+            gate_of(p.decay, fv[v], a, b);
+            h[v] = step_of(a, rest_of(a, b), h[v], p.coupled ? b * xv[v] : xv[v]);
         }
-        VecIO<T, VW>::store((T*)p.out + row * p.hs + c, h);
+        return L::pack(h);
+    };
+    int t = 0;
+    for (; t + kWalkAhead <= n; t += kWalkAhead) {
+        uint32_t rx[kWalkAhead], rf[kWalkAhead];
+#pragma unroll
+        for (int i = 0; i < kWalkAhead; ++i) {
+            rx[i] = L::load(x + (t + i) * p.xs, both);
+            rf[i] = L::load(f + (t + i) * p.fs, both);
+        }
+#pragma unroll
+        for (int i = 0; i < kWalkAhead; ++i) L::store(out + (t + i) * p.hs, one(rx[i], rf[i]), both);
     }
+    for (; t < n; ++t) L::store(out + t * p.hs, one(L::load(x + t * p.xs, both), L::load(f + t * p.fs, both)), both);
     if (p.left)
 #pragma unroll
-        for (int v = 0; v < VW; ++v) p.left[at + v] = h[v];
+        for (int v = 0; v < VW; ++v)
+            if (v == 0 || both) p.left[at + v] = h[v];
 }
 
-template <typename T, int VW>
+template <typename T>
 __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_back_kernel(ScanArgs p)
 {
+    typedef Lane4<T> L;
+    constexpr int VW = L::VW, AHEAD = kWalkAhead / 2;
     const int c = (blockIdx.x * kWalkThreads + threadIdx.x) * VW, s = blockIdx.y;
     if (c >= p.C) return;
+    const bool both = c + VW <= p.C;
     int n;
     const int64_t first = rows_of(p, s, n);
-    float r[VW] = {}, h[VW] = {};
+    float r[VW] = {}, before[VW] = {};
     const int64_t at = (int64_t)s * p.C + c;
-    if (p.dlast)
 #pragma unroll
-        for (int v = 0; v < VW; ++v) r[v] = p.dlast[at + v];
-    for (int t = n - 1; t >= 0; --t) {
-        const int64_t row = first + t;
-        float x[VW], f[VW], d[VW], dx[VW], df[VW];
-        VecIO<T, VW>::load((const T*)p.x + row * p.xs + c, x);
-        VecIO<T, VW>::load((const T*)p.f + row * p.fs + c, f);
-        VecIO<T, VW>::load((const T*)p.dh + row * p.hs + c, d);
-        if (t > 0) VecIO<T, VW>::load((const T*)p.h + (row - 1) * p.hs + c, h);
-        else
-#pragma unroll
-            for (int v = 0; v < VW; ++v) h[v] = p.state ? p.state[at + v] : 0.f;
+    for (int v = 0; v < VW; ++v)
+        if (v == 0 || both) {
+            if (p.dlast) r[v] = p.dlast[at + v];
+            if (p.state) before[v] = p.state[at + v];
+        }
+    const T* x = (const T*)p.x + first * p.xs + c;
+    const T* f = (const T*)p.f + first * p.fs + c;
+    const T* h = (const T*)p.h + first * p.hs + c;
+    const T* dh = (const T*)p.dh + first * p.hs + c;
+    T* dx = p.dx ? (T*)p.dx + first * p.xs + c : nullptr;
+    T* df = p.df ? (T*)p.df + first * p.fs + c : nullptr;
+    auto one = [&](int t, uint32_t rx, uint32_t rf, uint32_t rh, uint32_t rd) {
+        float xv[VW], fv[VW], hv[VW], dv[VW];
+        L::unpack(rx, xv);
+        L::unpack(rf, fv);
+        L::unpack(rh, hv);
+        L::unpack(rd, dv);
 #pragma unroll
         for (int v = 0; v < VW; ++v) {
             float a, b;
-            gate_of(p.decay, f[v], a, b);
-            const float g = d[v] + r[v];
-            r[v] = decayed(a, b, g);
-            dx[v] = p.coupled ? b * g : g;
-            df[v] = (p.decay == DSP_DECAY_SIGMOID ? a * b : a) * g * (p.coupled ? h[v] - x[v] : h[v]);
+            gate_of(p.decay, fv[v], a, b);
+            const float g = dv[v] + r[v], hp = t ? hv[v] : before[v];
+            r[v] = step_of(a, rest_of(a, b), g, 0.f);
+            fv[v] = (p.decay == DSP_DECAY_SIGMOID ? a * b : a) * g * (p.coupled ? hp - xv[v] : hp);
+            xv[v] = p.coupled ? b * g : g;
         }
-        if (p.dx) VecIO<T, VW>::store((T*)p.dx + row * p.xs + c, dx);
-        if (p.df) VecIO<T, VW>::store((T*)p.df + row * p.fs + c, df);
+        if (dx) L::store(dx + t * p.xs, L::pack(xv), both);
+        if (df) L::store(df + t * p.fs, L::pack(fv), both);
+    };
+    int t = n - 1;
+    for (; t >= AHEAD; t -= AHEAD) {
+        uint32_t rx[AHEAD], rf[AHEAD], rh[AHEAD], rd[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            rx[i] = L::load(x + (t - i) * p.xs, both);
+            rf[i] = L::load(f + (t - i) * p.fs, both);
+            rd[i] = L::load(dh + (t - i) * p.hs, both);
+            rh[i] = L::load(h + (t - i - 1) * p.hs, both);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) one(t - i, rx[i], rf[i], rh[i], rd[i]);
     }
+    for (; t >= 0; --t)
+        one(t, L::load(x + t * p.xs, both), L::load(f + t * p.fs, both), t ? L::load(h + (t - 1) * p.hs, both) : 0u, L::load(dh + t * p.hs, both));
     if (p.left)
 #pragma unroll
-        for (int v = 0; v < VW; ++v) p.left[at + v] = r[v];
+        for (int v = 0; v < VW; ++v)
+            if (v == 0 || both) p.left[at + v] = r[v];
+}
+
+// ---- long sequences: a workgroup scans a strip of channels tile by tile ---------------------------------
+//
+// A tile is kTileRows rows of 128 bytes.  A lane has the four bytes of kLaneRows consecutive rows, half a wave a row's 128 bytes: a slot.  (1) Every
+// slot finds what its rows do to a state, h -> A h + H, from h = 0; (2) the first wave goes through the slots with the state and leaves in
+// LDS what each one starts from; (3) every slot goes through its rows once more, which it still has in registers.  Backward the same from
+// the last row on, with r = a g in the place of h.  Rows behind the end are steps that change nothing (a = 1, u = 0).
+//
+// A sequence with too few strips to fill the card is cut into parts, whose A and H a first kernel finds (it reads the inputs of the scan once
+// more: what comes back is all compute units).
+constexpr int kLaneRows = 8, kWaves = 8, kSlots = 2 * kWaves, kTileRows = kSlots * kLaneRows, kScanThreads = 64 * kWaves;
+
+struct PartArgs {
+    float* sums;      // [sequences][parts - 1][3][C]: a, c, H of each part but the last
+    float* state;     // [sequences][C]: the state that goes in (the call may overwrite it)
+    int parts, part_rows;
+};
+
+// LDS of a workgroup: what the slots do, and what they start from.
+template <int W>
+struct Slots {
+    float a[kSlots][W], c[kSlots][W], h[kSlots][W], in[kSlots][W];
+};
+
+__device__ inline void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (loads on their way to registers go on)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// MODE 0: the scan; 1: what each part does, for the kernel behind.
+template <typename T, bool BACK, int DECAY, bool COUPLED, int MODE>
+__global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
+{
+    typedef Lane4<T> L;
+    constexpr int VW = L::VW, W = 32 * VW, TT = kLaneRows;
+    constexpr uint32_t kNone = DECAY == DSP_DECAY_SIGMOID ? L::kInfinity : 0u;  // the f of a = 1
+    __shared__ Slots<W> lds;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = wave * 2 + lane / 32;
+    const int s = blockIdx.y, part = blockIdx.z, c = blockIdx.x * W + lane % 32 * VW;
+    const bool in = c < p.C, both = c + VW <= p.C;
+    int whole;
+    const int64_t first = rows_of(p, s, whole);
+    // the rows of this part, in the order of the scan: k = 0 .. n - 1 is row k, or backward row whole - 1 - k
+    const int begin = part * q.part_rows, n = whole - begin < q.part_rows ? whole - begin : q.part_rows;
+    const T* const x = (const T*)p.x + first * p.xs + c;
+    const T* const f = (const T*)p.f + first * p.fs + c;
+    const T* const h = (const T*)p.h + first * p.hs + c;
+    const T* const d = (const T*)p.dh + first * p.hs + c;
+
+    struct Raw {
+        uint32_t x[TT], f[TT], d[TT], h[TT];
+    };
+    auto load = [&](int t0, Raw& r) {
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+            const int k = t0 + slot * TT + i;
+            r.x[i] = r.d[i] = r.h[i] = 0u;
+            r.f[i] = kNone;
+            if (!in || k >= n) continue;
+            const int64_t row = BACK ? whole - 1 - (begin + k) : begin + k;
+            r.f[i] = L::load(f + row * p.fs, both);
+            if (BACK) r.d[i] = L::load(d + row * p.hs, both);
+            if (!BACK || (COUPLED && MODE == 0)) r.x[i] = L::load(x + row * p.xs, both);
+            if (BACK && MODE == 0 && row > 0) r.h[i] = L::load(h + (row - 1) * p.hs, both);
+        }
+    };
+
+    // the state that the first wave carries: lane l's channel l of the strip
+    const int cc = blockIdx.x * W + lane;
+    const bool mine = wave == 0 && lane < W && cc < p.C;
+    float carry = 0.f, pa = 1.f, pc = 0.f;
+    if (MODE == 0 && mine) {
+        const float* from = q.parts > 1 ? q.state : BACK ? p.dlast : p.state;
+        if (from) carry = from[(int64_t)s * p.C + cc];
+        const float* sums = q.sums + (int64_t)s * (q.parts - 1) * 3 * p.C + cc;
+        for (int j = 0; j < part; ++j, sums += 3 * p.C) carry = step_of(sums[0], sums[p.C], carry, sums[2 * p.C]);
+    }
+    if (MODE == 1 && mine && part == 0) {
+        const float* from = BACK ? p.dlast : p.state;
+        q.state[(int64_t)s * p.C + cc] = from ? from[(int64_t)s * p.C + cc] : 0.f;
+    }
+    float before[VW] = {};  // the state in front of the first row, which h_(t-1) is there
+    if (BACK && MODE == 0 && p.state) {
+#pragma unroll
+        for (int v = 0; v < VW; ++v)
+            if (c + v < p.C) before[v] = p.state[(int64_t)s * p.C + c + v];
+    }
+
+    Raw next;
+    if (n > 0) load(0, next);
+    for (int t0 = 0; t0 < n; t0 += kTileRows) {
+        const Raw r = next;
+        if (t0 + kTileRows < n) load(t0 + kTileRows, next);
+        float a[TT][VW], rest[TT][VW], u[TT][VW], A[VW], B[VW], H[VW];
+#pragma unroll
+        for (int v = 0; v < VW; ++v) A[v] = 1.f, B[v] = H[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+            float fv[VW], xv[VW];
+            L::unpack(r.f[i], fv);
+            L::unpack(BACK ? r.d[i] : r.x[i], xv);
+#pragma unroll
+            for (int v = 0; v < VW; ++v) {
+                float b;
+                gate_of(DECAY, fv[v], a[i][v], b);
+                rest[i][v] = rest_of(a[i][v], b);
+                u[i][v] = BACK || !COUPLED ? xv[v] : b * xv[v];
+                B[v] = fmaf(A[v], b, B[v]);
+                A[v] *= a[i][v];
+                H[v] = BACK ? step_of(a[i][v], rest[i][v], H[v] + u[i][v], 0.f) : step_of(a[i][v], rest[i][v], H[v], u[i][v]);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < VW; ++v) {
+            const int w = lane % 32 * VW + v;
+            lds.a[slot][w] = A[v];
+            lds.c[slot][w] = rest_of(A[v], B[v]);
+            lds.h[slot][w] = H[v];
+        }
+        lds_barrier();
+        if (wave == 0 && lane < W) {
+#pragma unroll 4
+            for (int j = 0; j < kSlots; ++j) {
+                const float ja = lds.a[j][lane], jc = lds.c[j][lane], jh = lds.h[j][lane];
+                lds.in[j][lane] = carry;
+                carry = step_of(ja, jc, carry, jh);
+                if (MODE == 1) {  // (pa + pc) (ja + jc), to twice the digits of either
+                    const float m = pa * ja;
+                    pc = fmaf(pa, ja, -m) + fmaf(pa, jc, pc * ja);
+                    pa = m;
+                }
+            }
+        }
+        lds_barrier();
+        if (MODE == 1) continue;
+        float st[VW];
+#pragma unroll
+        for (int v = 0; v < VW; ++v) st[v] = lds.in[slot][lane % 32 * VW + v];
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+            const int k = t0 + slot * TT + i;
+            const int64_t row = BACK ? whole - 1 - (begin + k) : begin + k;
+            float o[VW], o2[VW], xv[VW], hv[VW];
+            if (BACK) {
+                L::unpack(r.x[i], xv);
+                L::unpack(r.h[i], hv);
+            }
+#pragma unroll
+            for (int v = 0; v < VW; ++v) {
+                if (!BACK) {
+                    st[v] = step_of(a[i][v], rest[i][v], st[v], u[i][v]);
+                    o[v] = st[v];
+                } else {
+                    const float g = u[i][v] + st[v], b = (1.f - a[i][v]) - rest[i][v], hp = row == 0 ? before[v] : hv[v];
+                    st[v] = step_of(a[i][v], rest[i][v], g, 0.f);
+                    o[v] = COUPLED ? b * g : g;
+                    o2[v] = (DECAY == DSP_DECAY_SIGMOID ? a[i][v] * b : a[i][v]) * g * (COUPLED ? hp - xv[v] : hp);
+                }
+            }
+            if (!in || k >= n) continue;
+            if (!BACK) {
+                L::store((T*)p.out + (first + row) * p.hs + c, L::pack(o), both);
+            } else {
+                if (p.dx) L::store((T*)p.dx + (first + row) * p.xs + c, L::pack(o), both);
+                if (p.df) L::store((T*)p.df + (first + row) * p.fs + c, L::pack(o2), both);
+            }
+        }
+    }
+    if (!mine) return;
+    if (MODE == 1) {
+        float* to = q.sums + ((int64_t)s * (q.parts - 1) + part) * 3 * p.C + cc;
+        to[0] = pa;
+        to[p.C] = pc;
+        to[2 * p.C] = carry;
+    } else if (part == q.parts - 1 && p.left) {
+        p.left[(int64_t)s * p.C + cc] = carry;
+    }
 }
 
 // ---- host --------------------------------------------------------------------------------------------
@@ -134,7 +394,7 @@ int check_desc(const dsp_recurrence_desc* d, const char* who)
     DSP_REQUIRE((d->dtype == DSP_FP32 || d->dtype == DSP_BF16) && (d->decay == DSP_DECAY_SIGMOID || d->decay == DSP_DECAY_EXP) &&
                     (d->coupled == 0 || d->coupled == 1),
                 DSP_EINVAL, "%s: bad type, decay or coupling", who);
-    DSP_REQUIRE(d->sequences > 0 && d->sequences <= 65535 && d->steps > 0 && d->rows >= 0 && d->rows < (1ll << 31) && d->C > 0 && d->C <= (1 << 20),
+    DSP_REQUIRE(d->sequences > 0 && d->sequences <= 65535 && d->steps > 0 && d->steps <= (1 << 30) && d->rows >= 0 && d->rows < (1ll << 31) && d->C > 0 && d->C <= (1 << 20),
                 DSP_EINVAL, "%s: bad shape", who);
     const int64_t strides[3] = {d->x_stride, d->f_stride, d->h_stride};
     for (int64_t s : strides)
@@ -150,14 +410,68 @@ ScanArgs args_of(const dsp_recurrence_desc* d)
     return a;
 }
 
-template <typename T>
-int walk(const ScanArgs& a, bool back, hipStream_t st, ProfScope& ps)
+// Who does it, and how a sequence is cut.
+struct Plan {
+    bool walk;
+    int parts, part_rows;
+    size_t sums, bytes;
+};
+Plan plan_of(const dsp_recurrence_desc* d)
 {
-    const dim3 grid(ceil_div(a.C, kWalkThreads), a.sequences);
-    if (back) DSP_LAUNCH(ps, (recurrence_walk_back_kernel<T, 1>), grid, dim3(kWalkThreads), 0, st, a);
-    else DSP_LAUNCH(ps, (recurrence_walk_kernel<T, 1>), grid, dim3(kWalkThreads), 0, st, a);
+    Plan p{};
+    const int vw = d->dtype == DSP_BF16 ? 2 : 1, strips = ceil_div(d->C, 32 * vw);
+    p.parts = 1;
+    p.part_rows = d->steps;
+    p.walk = d->steps <= 32 || (int64_t)d->sequences * strips >= 8192;
+    if (p.walk) return p;
+    const int64_t groups = (int64_t)strips * d->sequences;
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->steps, 4 * kTileRows), groups >= 192 ? 1 : 256 / groups));
+    p.part_rows = ceil_div(ceil_div(d->steps, want), kTileRows) * kTileRows;
+    p.parts = ceil_div(d->steps, p.part_rows);
+    if (p.parts > 1) {
+        p.sums = (size_t)d->sequences * (p.parts - 1) * 3 * d->C * sizeof(float);
+        p.bytes = (p.sums + (size_t)d->sequences * d->C * sizeof(float) + 15) / 16 * 16;
+    }
+    return p;
+}
+
+template <typename T, bool BACK, int DECAY, bool COUPLED>
+int scan(const ScanArgs& a, const PartArgs& q, hipStream_t st, const char* name, double bytes)
+{
+    const dim3 grid(ceil_div(a.C, 32 * Lane4<T>::VW), a.sequences, q.parts);
+    if (q.parts > 1) {
+        ProfScope ps("recurrence_parts", bytes * 2 / (BACK ? 6 : 3), 1);
+        DSP_LAUNCH(ps, (recurrence_scan_kernel<T, BACK, DECAY, COUPLED, 1>), dim3(grid.x, grid.y, grid.z - 1), dim3(kScanThreads), 0, st, a, q);
+        DSP_HIP(hipGetLastError());
+    }
+    ProfScope ps(name, bytes, 1);
+    DSP_LAUNCH(ps, (recurrence_scan_kernel<T, BACK, DECAY, COUPLED, 0>), grid, dim3(kScanThreads), 0, st, a, q);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
+}
+
+template <typename T, bool BACK>
+int run(const dsp_recurrence_desc* d, const ScanArgs& a, void* workspace, hipStream_t st)
+{
+    const Plan p = plan_of(d);
+    const char* name = BACK ? "recurrence_bwd" : "recurrence_fwd";
+    const double bytes = (BACK ? 6.0 : 3.0) * sizeof(T) * d->rows * d->C;
+    if (p.walk) {
+        ProfScope ps(name, bytes, 1);
+        const dim3 grid(ceil_div(a.C, kWalkThreads * Lane4<T>::VW), a.sequences);
+        if (BACK) DSP_LAUNCH(ps, recurrence_walk_back_kernel<T>, grid, dim3(kWalkThreads), 0, st, a);
+        else DSP_LAUNCH(ps, recurrence_walk_kernel<T>, grid, dim3(kWalkThreads), 0, st, a);
+        DSP_HIP(hipGetLastError());
+        return DSP_OK;
+    }
+    PartArgs q;
+    q.sums = (float*)workspace;
+    q.state = (float*)((char*)workspace + p.sums);
+    q.parts = p.parts;
+    q.part_rows = p.part_rows;
+    if (d->decay == DSP_DECAY_SIGMOID)
+        return d->coupled ? scan<T, BACK, DSP_DECAY_SIGMOID, true>(a, q, st, name, bytes) : scan<T, BACK, DSP_DECAY_SIGMOID, false>(a, q, st, name, bytes);
+    return d->coupled ? scan<T, BACK, DSP_DECAY_EXP, true>(a, q, st, name, bytes) : scan<T, BACK, DSP_DECAY_EXP, false>(a, q, st, name, bytes);
 }
 
 }  // namespace
@@ -171,7 +485,7 @@ int dsp_recurrence_workspace_bytes(const dsp_recurrence_desc* d, size_t* bytes)
 {
     DSP_REQUIRE(bytes, DSP_EINVAL, "dsp_recurrence_workspace_bytes: null argument");
     DSP_TRY(check_desc(d, "dsp_recurrence_workspace_bytes"));
-    *bytes = 0;
+    *bytes = plan_of(d).bytes;
     return DSP_OK;
 }
 
@@ -185,12 +499,12 @@ int dsp_recurrence_forward(const dsp_recurrence_desc* d, const void* d_x, const 
     DSP_REQUIRE(on(d_x, e) && on(d_f, e) && on(d_h, e) && on(d_offsets, 4) && on(d_state_in, 4) && on(d_state_out, 4), DSP_EINVAL,
                 "dsp_recurrence_forward: misaligned buffer");
     DSP_REQUIRE(d_h != d_x && d_h != d_f, DSP_EINVAL, "dsp_recurrence_forward: h wants a buffer of its own");
-    (void)d_workspace;
-    (void)workspace_bytes;
+    const size_t want = plan_of(d).bytes;
+    DSP_REQUIRE(!want || (d_workspace && workspace_bytes >= want && on(d_workspace, 16)), DSP_EINVAL,
+                "dsp_recurrence_forward: workspace too small or not 16-byte aligned (%zu < %zu)", workspace_bytes, want);
     ScanArgs a = args_of(d);
     a.x = d_x; a.f = d_f; a.offsets = d_offsets; a.state = d_state_in; a.out = d_h; a.left = d_state_out;
-    ProfScope ps("recurrence_fwd", 3.0 * e * d->rows * d->C, 1);
-    return d->dtype == DSP_BF16 ? walk<bf16_t>(a, false, (hipStream_t)stream, ps) : walk<float>(a, false, (hipStream_t)stream, ps);
+    return d->dtype == DSP_BF16 ? run<bf16_t, false>(d, a, d_workspace, (hipStream_t)stream) : run<float, false>(d, a, d_workspace, (hipStream_t)stream);
 }
 
 int dsp_recurrence_backward(const dsp_recurrence_desc* d, const void* d_dh, const float* d_dstate_out, const void* d_x, const void* d_f,
@@ -205,15 +519,15 @@ int dsp_recurrence_backward(const dsp_recurrence_desc* d, const void* d_dh, cons
                     on(d_dstate_out, 4) && on(d_dstate_in, 4),
                 DSP_EINVAL, "dsp_recurrence_backward: misaligned buffer");
     DSP_REQUIRE((!d_dx || (d_dx != d_h && d_dx != d_f && d_dx != d_df)) && (!d_df || (d_df != d_h && d_df != d_x && d_df != d_dh)) &&
-                    (!d_dx || d_dx != d_dh || stride_of(d->x_stride, d->C) == stride_of(d->h_stride, d->C)),
-                DSP_EINVAL, "dsp_recurrence_backward: dx may take the place of x or (with its stride) of dh, df that of f, and no other's");
-    (void)d_workspace;
-    (void)workspace_bytes;
+                    (!d_dstate_in || d_dstate_in != d_state_in) && (!d_dx || d_dx != d_dh || stride_of(d->x_stride, d->C) == stride_of(d->h_stride, d->C)),
+                DSP_EINVAL, "dsp_recurrence_backward: dx may take the place of x or (with its stride) of dh, df that of f, dstate_in that of dstate_out, and no other's");
+    const size_t want = plan_of(d).bytes;
+    DSP_REQUIRE(!want || (d_workspace && workspace_bytes >= want && on(d_workspace, 16)), DSP_EINVAL,
+                "dsp_recurrence_backward: workspace too small or not 16-byte aligned (%zu < %zu)", workspace_bytes, want);
     ScanArgs a = args_of(d);
     a.dh = d_dh; a.dlast = d_dstate_out; a.x = d_x; a.f = d_f; a.h = d_h; a.offsets = d_offsets; a.state = d_state_in;
     a.dx = d_dx; a.df = d_df; a.left = d_dstate_in;
-    ProfScope ps("recurrence_bwd", 6.0 * e * d->rows * d->C, 1);
-    return d->dtype == DSP_BF16 ? walk<bf16_t>(a, true, (hipStream_t)stream, ps) : walk<float>(a, true, (hipStream_t)stream, ps);
+    return d->dtype == DSP_BF16 ? run<bf16_t, true>(d, a, d_workspace, (hipStream_t)stream) : run<float, true>(d, a, d_workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

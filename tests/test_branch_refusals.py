@@ -41,7 +41,7 @@ def test_recurrence_refuses(dtype):
     bwd = lambda d, dh=A, dl=None, x=2 * A, f=3 * A, h=4 * A, o=None, s=None, dx=5 * A, df=6 * A, ds=None, ws=8 * A, n=1 << 40: D.dsp_recurrence_backward(  # noqa: E731
         d, dh, dl, x, f, h, o, s, dx, df, ds, ws, n, stream=0)
     good = dict(sequences=3, steps=5000, rows=15000, C_=64, dtype=dtype)
-    for over in ({"sequences": 0}, {"sequences": 1 << 17}, {"steps": 0}, {"steps": -1}, {"rows": -1}, {"rows": 1 << 31}, {"C_": 0}, {"C_": 1 << 21}, {"dtype": 3},
+    for over in ({"sequences": 0}, {"sequences": 1 << 17}, {"steps": 0}, {"steps": (1 << 30) + 1}, {"steps": -1}, {"rows": -1}, {"rows": 1 << 31}, {"C_": 0}, {"C_": 1 << 21}, {"dtype": 3},
                  {"decay": 2}, {"x_stride": 63}, {"f_stride": -1}, {"h_stride": 1 << 31}):
         d = D.make_recurrence_desc(**{**good, **over})
         refused(lambda: fwd(d)), refused(lambda: bwd(d)), refused(lambda: D.dsp_recurrence_workspace_bytes(d))
@@ -54,7 +54,8 @@ def test_recurrence_refuses(dtype):
     for over in ({"x": None}, {"f": None}, {"h": None}, {"x": A + 1}, {"f": A + 1}, {"h": A + 1}, {"o": A + 2}, {"s": A + 2}, {"t": A + 2}, {"h": A}, {"h": 2 * A}):
         refused(lambda: fwd(d, **over))
     for over in ({"dh": None}, {"x": None}, {"f": None}, {"h": None}, {"dx": None, "df": None}, {"dh": A + 1}, {"dx": A + 1}, {"df": A + 1}, {"ds": A + 2},
-                 {"dl": A + 2}, {"dx": 4 * A}, {"df": 4 * A}, {"dx": 3 * A}, {"df": 2 * A}, {"df": A}, {"df": 5 * A}):
+                 {"dl": A + 2}, {"dx": 4 * A}, {"df": 4 * A}, {"dx": 3 * A}, {"df": 2 * A}, {"df": A}, {"df": 5 * A},
+                 {"s": 9 * A, "ds": 9 * A}):
         refused(lambda: bwd(d, **over))
     d.x_stride = 72  # in another tensor's place, with another stride
     refused(lambda: bwd(d, dx=A))
