@@ -406,6 +406,64 @@ struct VecIO<bf16_t, 1> {
     __device__ static inline void store(bf16_t* p, const float (&v)[1]) { *p = float_to_bf16(v[0]); }
 };
 
+// The 16 bytes of consecutive elements from p on, at any alignment of elements; of the last run of a row only `count` of them (the others: fill).
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <size_t BYTES>
+struct AnyRun16;
+template <>
+struct AnyRun16<2> {
+    typedef u32x4_t V __attribute__((aligned(2)));
+};
+template <>
+struct AnyRun16<4> {
+    typedef u32x4_t V __attribute__((aligned(4)));
+};
+template <typename T>
+__device__ inline u32x4_t load_run16(const T* p, int count, T fill)
+{
+    constexpr int E = 16 / sizeof(T);
+    u32x4_t v;
+    if (count >= E) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+        T t[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) t[i] = i < count ? p[i] : fill;
+        __builtin_memcpy(&v, t, 16);
+    }
+    return v;
+}
+template <typename T>
+__device__ inline void store_run16(T* p, int count, u32x4_t v)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (count >= E) {
+        __builtin_nontemporal_store(v, (typename AnyRun16<sizeof(T)>::V*)p);
+    } else {
+        T t[E];
+        __builtin_memcpy(t, &v, 16);
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < count) p[i] = t[i];
+    }
+}
+template <typename T>
+__device__ inline void unpack_run16(u32x4_t r, float (&v)[16 / sizeof(T)])
+{
+    VecIO<T, 16 / sizeof(T)>::unpack(__builtin_bit_cast(typename VecIO<T, 16 / sizeof(T)>::Raw, r), v);
+}
+template <typename T>
+__device__ inline u32x4_t pack_run16(const float (&v)[16 / sizeof(T)])
+{
+    u32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) r[i] = __float_as_uint(v[i]);
+        else r[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    }
+    return r;
+}
+
 // exp(-a) for a >= 0 (or NaN) from the hardware's power of two, within one unit of its last place.  The exponent's product is rounded,
 // which alone would cost a 2^-24 of the result: what hi ln(2), with ln(2) in two parts, lacks of -a is a factor 1 + off.  Relative error
 // 3 * 2^-24; 0 below 2^-126.  (Where a is infinite off is no number, and the bound makes it one; p is NaN only where a is.)

@@ -221,23 +221,6 @@ struct OperandTile {
     }
 };
 
-// Up to E consecutive elements from p on, any alignment; zeros behind them.
-template <typename T>
-__device__ inline U4 load_chunk(const T* p, int count)
-{
-    constexpr int E = 16 / sizeof(T);
-    U4 v = {};
-    if (count >= E) {
-        __builtin_memcpy(&v, p, 16);
-    } else if (count > 0) {
-        T t[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) t[i] = i < count ? p[i] : T{};
-        __builtin_memcpy(&v, t, 16);
-    }
-    return v;
-}
-
 template <typename T_, bool AM_, bool BM_MAJOR, int BM_, int BN_, int WM_, int WN_, int KB_>
 struct StagedTile {
     typedef T_ T;
@@ -307,7 +290,7 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
             const int64_t r = r0 + (MAJOR ? c : row);
             const int k = k0 + (MAJOR ? row : c);
             int left = r < rows && k < g.K ? (int)(MAJOR ? (rows - r < O::E ? rows - r : O::E) : (g.K - k < O::E ? g.K - k : O::E)) : 0;
-            reg[i] = load_chunk<T>(left ? p + (MAJOR ? k * stride + r : r * stride + k) : p, left);
+            reg[i] = load_run16<T>(left ? p + (MAJOR ? k * stride + r : r * stride + k) : p, left, T{});
         }
     };
     auto keep = [&](auto op, char* to, auto& reg, auto count) {

@@ -10,8 +10,6 @@
 namespace dsp {
 namespace {
 
-constexpr int kRowThreads = 256;
-
 struct PolicyArgs {
     const void* z;
     const int32_t* labels;
@@ -20,58 +18,68 @@ struct PolicyArgs {
     void* dz;
     int64_t zs, gs;
     int R, V, full;  // full: the loss; otherwise the log probabilities alone
-    float inv_t, low, high, kl, ent;
+    double inv_t;
+    float k, low, high, kl, ent;  // k = log2(e) / T
 };
 
-// What of a row's loss its gradient needs: dz_j = p_j (c0 - c1 d_j), d_j = (max - z_j) / T, and `at_label` more at the label.
+// What of a row's loss its gradient needs: dz_j = p_j (c0 - c1 d_j), d_j = max - z_j, and `at_label` more at the label.
 struct RowGrad {
     float inv_sum, c0, c1, at_label;
 };
 
-template <bool MAX>
-__device__ inline float over_block(float v, float* lds)
+// exp(x) and exp(x) - 1, each to a few units of itself; and exp(x) - 1 - x: by the series from x^2 on below 0.35 (the next terms are 2e-8 of it).
+__device__ inline float exp_any(float x)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    for (int off = 32; off > 0; off >>= 1) {
-        const float o = __shfl_xor(v, off, 64);
-        v = MAX ? fmaxf(v, o) : v + o;
-    }
-    __syncthreads();
-    if (lane == 0) lds[wave] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < waves; ++w) v = MAX ? fmaxf(v, lds[w]) : v + lds[w];
-    return v;
+    const float e = exp_of_minus(fabsf(x));
+    return x > 0.f ? __builtin_amdgcn_rcpf(e) : e;
+}
+__device__ inline float series2(float x)
+{
+    return x * x * (1.f / 2 + x * (1.f / 6 + x * (1.f / 24 + x * (1.f / 120 + x * (1.f / 720 + x * (1.f / 5040 + x * (1.f / 40320)))))));
 }
 
-// A row's results from its largest logit, sum of exponentials and sum of exponentials times d; by one thread, in 64 bits: a KL term of
-// a difference of a tenth keeps five digits of it, and the ratio those of the log probabilities.
-__device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, int label, float top, float at_label, float sum, float dsum)
+// A row's results from its largest logit, sum of exponentials and sum of exponentials times top - z; by one thread.  The log probability is added
+// up in 64 bits and its differences to the old and the reference's are taken there: a KL term of a difference of a tenth keeps five digits of it.
+// All that is left is small and goes in floats (the library's logarithm and exponentials of 64 bits would take the registers in which the
+// row is held).
+__device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top, float at_label, float sum, float dsum)
 {
-    const double logs = log((double)sum), lp = ((double)at_label - (double)top) * (double)a.inv_t - logs, H = logs + (double)dsum / (double)sum;
+    // log(sum) = log(2) exponent + log(m), m in [sqrt(1/2), sqrt(2)): 2 artanh((m - 1) / (m + 1)), the next term is 3e-9
+    int ex = __builtin_amdgcn_frexp_expf(sum);
+    float m = __builtin_amdgcn_frexp_mantf(sum);
+    if (m < 0.707106781f) {
+        m *= 2.f;
+        --ex;
+    }
+    const float q = (m - 1.f) / (m + 1.f), q2 = q * q, log_m = 2.f * q * (1.f + q2 * (1.f / 3 + q2 * (1.f / 5 + q2 * (1.f / 7 + q2 * (1.f / 9)))));
+    const double logs = ex * 0.69314718055994531 + (double)log_m;
+    const double lp = ((double)at_label - (double)top) * a.inv_t - logs;
+    const float spread = dsum / sum * (float)a.inv_t, H = (float)logs + spread;
     if (a.logp) a.logp[row] = (float)lp;
-    if (a.entropy) a.entropy[row] = (float)H;
+    if (a.entropy) a.entropy[row] = H;
     RowGrad g = {0.f, 0.f, 0.f, 0.f};
     if (!a.full) return g;
-    const double A = a.advantage[row], rho = a.old ? exp(lp - (double)a.old[row]) : 1.0;
-    const double bounded = rho < (double)a.low ? (double)a.low : rho > (double)a.high ? (double)a.high : rho;
-    const double free = -A * rho, held = -A * bounded;
+    const float A = a.advantage[row], rho = a.old ? exp_any((float)(lp - (double)a.old[row])) : 1.f;
+    const float bounded = rho < a.low ? a.low : rho > a.high ? a.high : rho;
+    const float free = -A * rho, held = -A * bounded;
     const bool clipped = held > free;
-    double c = clipped ? 0.0 : free, kl = 0.0;
+    float c = clipped ? 0.f : free, kl = 0.f;
     if (a.ref) {
-        const double d = (double)a.ref[row] - lp, more = expm1(d);
-        kl = more - d;
-        c -= (double)a.kl * more;
+        const float d = (float)((double)a.ref[row] - lp);
+        const bool near = fabsf(d) < 0.35f;
+        const float more = exp_any(d) - 1.f;
+        kl = near ? series2(d) : more - d;
+        c -= a.kl * (near ? d + kl : more);
     }
-    a.terms[row] = (float)(clipped ? held : free);
-    a.terms[(int64_t)a.R + row] = (float)kl;
-    a.terms[2 * (int64_t)a.R + row] = (float)H;
+    a.terms[row] = clipped ? held : free;
+    a.terms[(int64_t)a.R + row] = kl;
+    a.terms[2 * (int64_t)a.R + row] = H;
     a.terms[3 * (int64_t)a.R + row] = clipped ? 1.f : 0.f;
-    const double w = (a.weight ? (double)a.weight[row] : 1.0 / a.R) * (double)a.inv_t;
-    g.inv_sum = (float)(1.0 / (double)sum);
-    g.at_label = (float)(w * c);
-    g.c0 = (float)(w * (a.ent * (H - logs) - c));
-    g.c1 = (float)(w * a.ent);
+    const float w = (a.weight ? a.weight[row] : 1.f / a.R) * (float)a.inv_t;
+    g.inv_sum = 1.f / sum;
+    g.at_label = w * c;
+    g.c0 = w * (a.ent * spread - c);
+    g.c1 = w * a.ent * (float)a.inv_t;
     return g;
 }
 // A row without a token, or without a logit that is not -infinity: it has no part in the loss.
@@ -83,55 +91,256 @@ __device__ inline void empty_row(const PolicyArgs& a, int64_t row)
         for (int k = 0; k < 4; ++k) a.terms[k * (int64_t)a.R + row] = 0.f;
 }
 
-// d = (top - z) / T, bounded where exp(-d) is 0 so that no product with it is infinite; NaN stays NaN.
-__device__ inline float below_top(float top, float z, float inv_t)
+// A row lies with WAVES waves; with one of them a workgroup has four rows, otherwise one.
+template <int WAVES>
+struct RowGroup {
+    static constexpr int THREADS = 64 * WAVES, BLOCK = WAVES == 1 ? 256 : THREADS, ROWS = BLOCK / THREADS;
+    float (*lds)[2];  // [WAVES], unused with one wave
+
+    __device__ inline int tid() const { return threadIdx.x % THREADS; }
+    template <bool MAX>
+    __device__ inline void reduce(float& u, float& v) const
+    {
+        for (int off = 32; off > 0; off >>= 1) {
+            const float a = __shfl_xor(u, off, 64), b = __shfl_xor(v, off, 64);
+            u = MAX ? fmaxf(u, a) : u + a;
+            v = MAX ? fmaxf(v, b) : v + b;
+        }
+        if constexpr (WAVES > 1) {
+            __syncthreads();
+            if (threadIdx.x % 64 == 0) {
+                lds[threadIdx.x / 64][0] = u;
+                lds[threadIdx.x / 64][1] = v;
+            }
+            __syncthreads();
+            u = lds[0][0];
+            v = lds[0][1];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                u = MAX ? fmaxf(u, lds[w][0]) : u + lds[w][0];
+                v = MAX ? fmaxf(v, lds[w][1]) : v + lds[w][1];
+            }
+        }
+    }
+};
+
+// exp(-d / T) of a difference d >= 0 to the largest logit, k = log2(e) / T: a product and the hardware's power of two, off by 2 d U + 2 U of
+// itself.  What that makes of a row's probabilities goes by the spread of d under them, a few units.
+__device__ inline float exp_below(float d, float k) { return __builtin_amdgcn_exp2f(-d * k); }
+// (A product of e = 0 with the difference to a logit of -infinity is 0; where e is NaN so is the product.)
+__device__ inline float finite(float d) { return fminf(d, 1e30f); }
+
+// The row in registers stays as it was loaded: the compiler may keep nothing that it made of it on the way (floats, exponentials).
+template <int NV>
+__device__ inline void as_loaded(u32x4_t (&raw)[NV])
 {
-    const float d = (top - z) * inv_t;
-    return d > 200.f ? 200.f : d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(raw[i]));
 }
 
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void policy_row_kernel(PolicyArgs a)
+__device__ inline T lowest()
 {
-    __shared__ float lds[kRowThreads / 64];
-    __shared__ RowGrad shared;
-    const int64_t row = blockIdx.x;
+    return from_float<T>(-INFINITY);
+}
+
+// The row is held in registers: NV runs of 16 bytes a thread, run i of a thread behind those of all threads before.
+template <typename T, int WAVES, int NV>
+__global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_held_kernel(PolicyArgs a)
+{
+    typedef RowGroup<WAVES> G;
+    constexpr int E = 16 / sizeof(T);
+    __shared__ float lds[WAVES][2];
+    __shared__ RowGrad shared[G::ROWS];
+    const int64_t row = (int64_t)blockIdx.x * G::ROWS + threadIdx.x / G::THREADS;
+    if (row >= a.R) return;  // (a whole wave of those that need no barrier)
+    const G group = {lds};
+    const int tid = group.tid(), label = a.labels[row];
     const T* const z = (const T*)a.z + row * a.zs;
     T* const dz = a.dz ? (T*)a.dz + row * a.gs : nullptr;
-    const int label = a.labels[row], tid = threadIdx.x;
-    float top = -INFINITY;
-    if (label >= 0)
-        for (int j = tid; j < a.V; j += kRowThreads) top = fmaxf(top, to_float<T>(z[j]));
-    top = over_block<true>(top, lds);
-    if (top == -INFINITY) {  // nothing, or nothing but -infinity and NaN
-        float nan = 0.f;
-        if (label >= 0)
-            for (int j = tid; j < a.V; j += kRowThreads)
-                if (to_float<T>(z[j]) != to_float<T>(z[j])) nan = 1.f;
-        if (over_block<true>(nan, lds) == 0.f) {
-            if (tid == 0) empty_row(a, row);
-            if (dz)
-                for (int j = tid; j < a.V; j += kRowThreads) dz[j] = from_float<T>(0.f);
-            return;
+    u32x4_t raw[NV];
+    bool empty = label < 0;
+    float top = -INFINITY, other = -INFINITY;
+    if (!empty) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = (i * G::THREADS + tid) * E;
+            raw[i] = load_run16<T>(z + (j < a.V ? j : 0), a.V - j, lowest<T>());
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float v[E];
+            unpack_run16<T>(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) top = fmaxf(top, v[e]);
+        }
+        group.template reduce<true>(top, other);
+        as_loaded(raw);
+        if (top == -INFINITY) {  // nothing but -infinity, or that and NaN
+            float nan = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float v[E];
+                unpack_run16<T>(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < E; ++e) nan = v[e] == v[e] ? nan : 1.f;
+            }
+            group.template reduce<true>(nan, other);
+            empty = nan == 0.f;
         }
     }
-    float sum = 0.f, dsum = 0.f;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-        const float d = below_top(top, to_float<T>(z[j]), a.inv_t), e = exp_of_minus(d);
-        sum += e;
-        dsum += e * d;
+    if (empty) {
+        if (tid == 0) empty_row(a, row);
+        if (dz)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int j = (i * G::THREADS + tid) * E;
+                if (j < a.V) store_run16<T>(dz + j, a.V - j, u32x4_t{0, 0, 0, 0});
+            }
+        return;
     }
-    sum = over_block<false>(sum, lds);
-    dsum = over_block<false>(dsum, lds);
-    if (tid == 0) shared = row_result(a, row, label, top, label < a.V ? to_float<T>(z[label]) : NAN, sum, dsum);
+    as_loaded(raw);
+    float sum = 0.f, dsum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float v[E];
+        unpack_run16<T>(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = top - v[e], x = exp_below(d, a.k);
+            sum += x;
+            dsum = fmaf(x, finite(d), dsum);
+        }
+    }
+    group.template reduce<false>(sum, dsum);
+    RowGrad g;
+    const float at_label = label < a.V ? to_float<T>(z[label]) : NAN;
+    if constexpr (WAVES == 1) {
+        if (tid == 0) g = row_result(a, row, top, at_label, sum, dsum);
+        g.inv_sum = __shfl(g.inv_sum, 0, 64);
+        g.c0 = __shfl(g.c0, 0, 64);
+        g.c1 = __shfl(g.c1, 0, 64);
+        g.at_label = __shfl(g.at_label, 0, 64);
+    } else {
+        if (tid == 0) shared[0] = row_result(a, row, top, at_label, sum, dsum);
+        __syncthreads();
+        g = shared[0];
+    }
+    if (!dz) return;
+    const float c0 = g.c0 * g.inv_sum, c1 = g.c1 * g.inv_sum;
+    as_loaded(raw);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int j = (i * G::THREADS + tid) * E;
+        float v[E];
+        unpack_run16<T>(raw[i], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = top - v[e];
+            v[e] = exp_below(d, a.k) * fmaf(-c1, finite(d), c0);
+        }
+        if (label >= j && label < j + E) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (label == j + e) v[e] += g.at_label;
+        }
+        if (j < a.V) store_run16<T>(dz + j, a.V - j, pack_run16<T>(v));
+    }
+}
+
+// Rows that no workgroup holds, and calls that want no gradient: the sums follow the largest logit so far.  For the gradient the row is read once more.
+constexpr int kStreamAhead = 4;
+
+template <typename T, int WAVES>
+__global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel(PolicyArgs a)
+{
+    typedef RowGroup<WAVES> G;
+    constexpr int E = 16 / sizeof(T), AHEAD = kStreamAhead;
+    __shared__ float lds[WAVES][2];
+    __shared__ RowGrad shared;
+    const int64_t row = blockIdx.x;
+    const G group = {lds};
+    const int tid = group.tid(), label = a.labels[row];
+    const T* const z = (const T*)a.z + row * a.zs;
+    T* const dz = a.dz ? (T*)a.dz + row * a.gs : nullptr;
+    float top = -INFINITY, some = -INFINITY, sum = 0.f, dsum = 0.f;
+    if (label >= 0)
+        for (int64_t j0 = tid * E; j0 < a.V; j0 += (int64_t)AHEAD * G::THREADS * E) {
+            u32x4_t raw[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int64_t j = j0 + i * G::THREADS * E, left = a.V - j;
+                raw[i] = load_run16<T>(z + (left > 0 ? j : 0), left < E ? (int)(left > 0 ? left : 0) : E, lowest<T>());
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                float v[E], m = top;
+                unpack_run16<T>(raw[i], v);
+#pragma unroll
+                for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
+                if (m > top) {  // (from nothing: both sums are 0)
+                    const float d = finite(m - top), x = exp_below(d, a.k);
+                    dsum = fmaf(sum, d, dsum) * x;
+                    sum *= x;
+                    top = m;
+                }
+                if (m == -INFINITY) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) some = v[e] == v[e] ? some : 1.f;
+                    continue;
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float d = top - v[e], x = exp_below(d, a.k);
+                    sum += x;
+                    dsum = fmaf(x, finite(d), dsum);
+                }
+            }
+        }
+    float high = top;
+    group.template reduce<true>(high, some);
+    if (label < 0 || (high == -INFINITY && some == -INFINITY)) {
+        if (tid == 0) empty_row(a, row);
+        if (dz)
+            for (int64_t j = tid * E; j < a.V; j += G::THREADS * E)
+                store_run16<T>(dz + j, a.V - j < E ? (int)(a.V - j) : E, u32x4_t{0, 0, 0, 0});
+        return;
+    }
+    const float d = finite(high - top), x = exp_below(d, a.k);
+    dsum = fmaf(sum, d, dsum) * x;
+    sum *= x;
+    if (some == 1.f) sum = NAN;  // (a thread that saw nothing but -infinity beside it kept no sum of it)
+    group.template reduce<false>(sum, dsum);
+    if (tid == 0) shared = row_result(a, row, high, label < a.V ? to_float<T>(z[label]) : NAN, sum, dsum);
     __syncthreads();
     if (!dz) return;
     const RowGrad g = shared;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-        const float d = below_top(top, to_float<T>(z[j]), a.inv_t), p = exp_of_minus(d) * g.inv_sum;
-        float v = p * (g.c0 - g.c1 * d);
-        if (j == label) v += g.at_label;
-        dz[j] = from_float<T>(v);
+    const float c0 = g.c0 * g.inv_sum, c1 = g.c1 * g.inv_sum;
+    for (int64_t j0 = tid * E; j0 < a.V; j0 += (int64_t)AHEAD * G::THREADS * E) {
+        u32x4_t raw[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t j = j0 + i * G::THREADS * E, left = a.V - j;
+            raw[i] = load_run16<T>(z + (left > 0 ? j : 0), left < E ? (int)(left > 0 ? left : 0) : E, lowest<T>());
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t j = j0 + i * G::THREADS * E;
+            if (j >= a.V) break;
+            float v[E];
+            unpack_run16<T>(raw[i], v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float below = high - v[e];
+                v[e] = exp_below(below, a.k) * fmaf(-c1, finite(below), c0);
+            }
+            if (label >= j && label < j + E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (label == j + e) v[e] += g.at_label;
+            }
+            store_run16<T>(dz + j, a.V - j < E ? (int)(a.V - j) : E, pack_run16<T>(v));
+        }
     }
 }
 
@@ -142,12 +351,26 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a, f
 {
     __shared__ double part[4][kSumThreads / 64];
     double s[4] = {};
-    for (int64_t r = threadIdx.x; r < a.R; r += kSumThreads) {
-        const double w = a.weight ? (double)a.weight[r] : 1.0 / a.R;
-        const bool there = a.labels[r] >= 0;
+    constexpr int AHEAD = 4;
+    for (int64_t r0 = threadIdx.x; r0 < a.R; r0 += AHEAD * kSumThreads) {
+        float w[AHEAD], t[AHEAD][4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] += there ? w * (double)a.terms[k * (int64_t)a.R + r] : 0.0;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int64_t r = r0 + i * kSumThreads;
+            const bool in = r < a.R;
+            w[i] = in ? (a.weight ? a.weight[r] : 1.f) : 0.f;
+            if (in && a.labels[r] < 0) w[i] = 0.f;  // (whatever its weight is)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[i][k] = in ? a.terms[k * (int64_t)a.R + r] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] += (double)w[i] * (double)t[i][k];
     }
+    if (!a.weight)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] /= a.R;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         for (int off = 32; off > 0; off >>= 1) s[k] += __shfl_down(s[k], off, 64);
@@ -185,18 +408,43 @@ PolicyArgs args_of(const dsp_policy_loss_desc* d, const void* d_logits, const in
     PolicyArgs a{};
     a.z = d_logits; a.labels = d_labels;
     a.zs = stride_of(d->logits_stride, d->vocab); a.gs = stride_of(d->grad_stride, d->vocab);
-    a.R = d->rows; a.V = d->vocab; a.inv_t = 1.f / d->temperature;
+    a.R = d->rows; a.V = d->vocab; a.inv_t = 1.0 / (double)d->temperature; a.k = (float)(1.4426950408889634 / (double)d->temperature);
     a.low = 1.f - d->clip_low; a.high = 1.f + d->clip_high; a.kl = d->kl_coef; a.ent = d->entropy_coef;
     return a;
+}
+
+template <typename T, int WAVES, int NV>
+int held(const PolicyArgs& a, hipStream_t st, ProfScope& ps)
+{
+    typedef RowGroup<WAVES> G;
+    DSP_LAUNCH(ps, (policy_held_kernel<T, WAVES, NV>), dim3(ceil_div(a.R, G::ROWS)), dim3(G::BLOCK), 0, st, a);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+template <typename T, int WAVES>
+int streamed(const PolicyArgs& a, hipStream_t st, ProfScope& ps)
+{
+    DSP_LAUNCH(ps, (policy_streamed_kernel<T, WAVES>), dim3(a.R), dim3(64 * WAVES), 0, st, a);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+template <typename T>
+int rows_t(const PolicyArgs& a, hipStream_t st, ProfScope& ps)
+{
+    const int runs = ceil_div(a.V, 16 / sizeof(T));
+    if (runs <= 64) return held<T, 1, 1>(a, st, ps);
+    if (runs <= 256) return held<T, 1, 4>(a, st, ps);
+    if (runs <= 1024) return held<T, 4, 4>(a, st, ps);
+    if (runs <= 2048) return held<T, 8, 4>(a, st, ps);
+    if (runs <= 4096) return held<T, 8, 8>(a, st, ps);
+    return streamed<T, 16>(a, st, ps);
 }
 
 int rows_pass(int dtype, const char* name, double bytes, const PolicyArgs& a, hipStream_t st)
 {
     ProfScope ps(name, bytes, 1);
-    if (dtype == DSP_BF16) DSP_LAUNCH(ps, policy_row_kernel<bf16_t>, dim3(a.R), dim3(kRowThreads), 0, st, a);
-    else DSP_LAUNCH(ps, policy_row_kernel<float>, dim3(a.R), dim3(kRowThreads), 0, st, a);
-    DSP_HIP(hipGetLastError());
-    return DSP_OK;
+    return dtype == DSP_BF16 ? rows_t<bf16_t>(a, st, ps) : rows_t<float>(a, st, ps);
 }
 
 }  // namespace
