@@ -406,8 +406,31 @@ struct VecIO<bf16_t, 1> {
     __device__ static inline void store(bf16_t* p, const float (&v)[1]) { *p = float_to_bf16(v[0]); }
 };
 
-// The 16 bytes of consecutive elements from p on, at any alignment of elements; of the last run of a row only `count` of them (the others: fill).
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// The direct load as an asm block: behind the builtin the compiler makes every transpose read wait for ALL outstanding
+// direct loads (it takes the read to alias their LDS writes), which leaves no load in flight across a k step.  The block
+// has no output; the waits for what it puts in LDS are written out in the kernel.  The s_nop covers the wait states that
+// M0 and a descriptor register fresh from a vector instruction need before a load reads them.  M0 is listed as overwritten, so
+// that the compiler keeps no value of its own there across the block (it warns that it does not save a reserved register
+// itself, which nothing here asks for).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ inline void dma16_untracked(u32x4_t rsrc, uint32_t lds_wave_base, uint32_t byte_off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(lds_wave_base), "v"(byte_off), "s"(rsrc)
+                 : "m0", "memory");
+}
+#pragma clang diagnostic pop
+__device__ inline u32x4_t rsrc_words(const void* p, uint32_t bytes)
+{
+    const uint64_t a = (uint64_t)p;
+    return u32x4_t{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+
+// The 16 bytes of consecutive elements from p on, at any alignment of elements; of the last run of a row only `count` of them (the others: fill).
 template <size_t BYTES>
 struct AnyRun16;
 template <>

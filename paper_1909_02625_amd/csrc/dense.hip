@@ -7,6 +7,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <atomic>
 
 namespace dsp {
 namespace {
@@ -255,7 +256,7 @@ __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const O
                 *(F4*)(mine + (lane & 31) * ROW + j * 32 + 8 * q + 4 * (lane >> 5)) =
                     F4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
+#pragma unroll 1
         for (int r = 0; r < 32; r += RPP) {
             const int row = r + lane / LPR, col = lane % LPR * 8;
             const F4 u = *(const F4*)(mine + row * ROW + col), w = *(const F4*)(mine + row * ROW + col + 4);
@@ -339,6 +340,168 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
         __syncthreads();
     }
     finish_tile<TL>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
+}
+
+// ---- the same for bf16 rows of whole 16-byte runs: tiles go from memory to LDS directly ---------------
+//
+// ST stages of a ring hold KB bytes of k each.  Tiles kt .. kt + ST - 2 are in LDS or on their way.  One barrier per tile, in the middle of
+// its k steps: by then each wave has waited until only its loads of later tiles are outstanding, and all have finished reading tile kt - 1,
+// whose stage takes tile kt + ST - 1.  The operands of a k step are read while the step before is multiplied.
+template <bool AM_, bool BMJ_, int BM_, int BN_, int WM_, int WN_, int KB_, int ST_>
+struct DirectTile {
+    typedef bf16_t T;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, ST = ST_;
+    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES, TM = BM / (32 * WM), TN = BN / (32 * WN), NKS = KB / 32;
+    typedef OperandTile<T, AM_, BM, KB> A;
+    typedef OperandTile<T, BMJ_, BN, KB> B;
+    static constexpr int BK = KB / 2, STAGE = (BM + BN) * KB, LA = BM * KB / 1024 / WAVES, LB = BN * KB / 1024 / WAVES, LOADS = LA + LB;
+    static_assert(LA * 1024 * WAVES == BM * KB && LB * 1024 * WAVES == BN * KB, "whole loads for every wave");
+    static constexpr int OUT_ROW = TN * 32 + 4, OUT = WAVES * 32 * OUT_ROW * 4;
+    static constexpr int LDS = ST * STAGE > OUT ? ST * STAGE : OUT;
+    static_assert(ST >= 3 && LDS <= 160 * 1024, "a ring of three stages");
+};
+
+// The place of a tile: those that run together, 32 of an XCD, are eight rows high.
+__device__ inline void place_of(unsigned tile, int tiles_m, int tiles_n, int& tm, int& tn)
+{
+    constexpr unsigned kHigh = 8;
+    const unsigned group = tile / (kHigh * tiles_n), in = tile - group * kHigh * tiles_n;
+    const unsigned high = tiles_m - group * kHigh < kHigh ? tiles_m - group * kHigh : kHigh;
+    tm = group * kHigh + in % high;
+    tn = in / high;
+}
+
+// One operand's loads of a tile: 1 KB each, the lanes' 16 bytes one behind the other in LDS; a lane fetches the chunk that belongs at its place.
+// What lies behind the rows or behind k reads 0: with k outside by the descriptor's length alone, with k inside by that for the rows and by the
+// lane's offset for k.
+template <typename O, int KB, int LOADS, int WAVES>
+struct DirectLoads {
+    const char* base;  // of the next tile (k0)
+    int64_t step;      // bytes to the one behind it
+    int64_t rows_bytes;  // K inside: bytes from the first to the last row; outside: of a row, from the first column of the tile on
+    int64_t stride;    // bytes
+    uint32_t off[LOADS];
+    int chunk_k[LOADS];
+
+    __device__ inline DirectLoads(const void* p, int64_t stride_e, int64_t r0, int rows, int wave, int lane)
+    {
+        constexpr int RPL = 1024 / O::ROWB;  // rows of LDS in a load
+        stride = stride_e * 2;
+        base = (const char*)p + (O::K_OUTSIDE ? r0 * 2 : r0 * stride);
+        step = O::K_OUTSIDE ? stride * O::BK : KB;
+        const int64_t left = rows - r0;
+        const int64_t tile_rows = O::K_OUTSIDE ? O::ROWB / 2 : O::CHUNKS * 16 / KB;
+        rows_bytes = O::K_OUTSIDE ? left * 2 : ((left < tile_rows ? left : tile_rows) - 1) * stride;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int row = (i * WAVES + wave) * RPL + lane / O::CPR, chunk = (lane % O::CPR) ^ O::swz(row);
+            off[i] = (uint32_t)(row * stride) + chunk * 16;
+            chunk_k[i] = chunk * 8;
+        }
+    }
+    // k_left: elements of k from this tile's first on
+    __device__ inline void issue(uint32_t lds, int k_left, int first, int last, int wave)
+    {
+        const int64_t length = k_left <= 0 ? 0
+                               : O::K_OUTSIDE ? (int64_t)((k_left < O::BK ? k_left : O::BK) - 1) * stride + rows_bytes
+                                              : rows_bytes + (int64_t)k_left * 2;
+        const u32x4_t r = rsrc_words(base, (uint32_t)(length < 0x7fffffff ? length : 0x7fffffff));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            if (i < first || i >= last) continue;
+            dma16_untracked(r, lds + (i * WAVES + wave) * 1024, O::K_OUTSIDE || chunk_k[i] < k_left ? off[i] : 0x80000000u);
+        }
+    }
+    __device__ inline void advance() { base += step; }
+};
+
+template <typename TL>
+__global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL::WAVES / 4, TL::WAVES / 4))) void dense_direct_kernel(GemmArgs g)
+{
+    typedef typename TL::A A;
+    typedef typename TL::B B;
+    constexpr int TM = TL::TM, TN = TL::TN, NKS = TL::NKS, ST = TL::ST, LA = TL::LA, LOADS = TL::LOADS;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / TL::WN, wn = wave % TL::WN;
+    int tm, tn;
+    place_of(xcd_order(blockIdx.x, gridDim.x), g.tiles_m, g.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * TL::BM;
+    const int n0 = tn * TL::BN;
+    DirectLoads<A, TL::KB, LA, TL::WAVES> la(g.a, g.as, m0, g.M, wave, lane);
+    DirectLoads<B, TL::KB, TL::LB, TL::WAVES> lb(g.b, g.bs, n0, g.N, wave, lane);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    int k_left = g.K;
+    auto issue = [&](int stage, int first, int last) {
+        la.issue(ring + stage * TL::STAGE, k_left, first, last, wave);
+        lb.issue(ring + stage * TL::STAGE + TL::BM * TL::KB, k_left, first - LA, last - LA, wave);
+    };
+    auto next = [&]() {
+        la.advance();
+        lb.advance();
+        k_left -= TL::BK;
+    };
+    F16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    auto read = [&](const char* s, int ks, U4 (&a)[TM], U4 (&b)[TN]) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) a[i] = A::fragment(s, wm * TM + i, ks, lane);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[j] = B::fragment(s + TL::BM * TL::KB, wn * TN + j, ks, lane);
+    };
+    auto multiply = [&](const U4 (&a)[TM], const U4 (&b)[TN]) {
+        __builtin_amdgcn_sched_barrier(0);  // the reads of the next step go out before this step's products
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) Mma32<bf16_t>::run(b[j], a[i], acc[i][j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int AHEAD = (ST - 3) * LOADS, SLOTS = NKS / 2 + 1;
+#pragma unroll
+    for (int t = 0; t < ST - 1; ++t) {
+        issue(t, 0, LOADS);
+        next();
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): no scalar load is pending when the counted waits begin
+    U4 fa[2][TM], fb[2][TN];
+    read(smem, 0, fa[0], fb[0]);
+    const int nk = (g.K + TL::BK - 1) / TL::BK;
+    int st = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        const char* s = smem + st * TL::STAGE;
+        const int st1 = st + 1 == ST ? 0 : st + 1, stl = st == 0 ? ST - 1 : st - 1;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            if (ks + 1 < NKS) read(s, ks + 1, fa[(ks + 1) & 1], fb[(ks + 1) & 1]);
+            else read(smem + st1 * TL::STAGE, 0, fa[0], fb[0]);
+            multiply(fa[ks & 1], fb[ks & 1]);
+            if (ks == NKS / 2 - 1) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(AHEAD) : "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+            if (ks >= NKS / 2 - 1) {
+                const int slot = ks - (NKS / 2 - 1);
+                issue(stl, LOADS * slot / SLOTS, LOADS * (slot + 1) / SLOTS);
+                if (slot == SLOTS - 1) next();
+            }
+        }
+        st = st1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads behind the end must not land in what follows
+    __syncthreads();
+    finish_tile<TL>(smem, acc, g.o, m0 + wm * TM * 32, n0 + wn * TN * 32, wave, lane);
 }
 
 // ---- the gradient in front of the activation, and its column sums ------------------------------------
@@ -446,6 +609,30 @@ int launch_staged(GemmArgs& g, hipStream_t st, ProfScope& ps)
     return DSP_OK;
 }
 
+template <typename TL>
+int launch_direct(GemmArgs& g, hipStream_t st, ProfScope& ps)
+{
+    g.tiles_m = ceil_div(g.M, TL::BM);
+    g.tiles_n = ceil_div(g.N, TL::BN);
+    auto kern = dense_direct_kernel<TL>;
+    static std::atomic<bool> attr_done{false};
+    if (!attr_done) {
+        DSP_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS));
+        attr_done = true;
+    }
+    DSP_LAUNCH(ps, kern, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(TL::THREADS), TL::LDS, st, g);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+// Rows of whole 16-byte runs on 16-byte addresses, whose tiles 32-bit offsets reach.
+template <bool AM, bool BMJ>
+bool direct_ok(const GemmArgs& g)
+{
+    const int64_t most = (1ll << 31) / 1024;
+    return on(g.a, 16) && on(g.b, 16) && g.as % 8 == 0 && g.bs % 8 == 0 && (AM ? g.M : g.K) % 8 == 0 && (BMJ ? g.N : g.K) % 8 == 0 && g.as < most && g.bs < most;
+}
+
 template <bool AM, bool BMJ>
 int contract(int dtype, const char* name, GemmArgs& g, hipStream_t st)
 {
@@ -454,6 +641,9 @@ int contract(int dtype, const char* name, GemmArgs& g, hipStream_t st)
     g.o.N = g.N;
     g.o.whole = g.N % 8 == 0 && g.o.stride * e % 16 == 0 && on(g.o.out, 16) && on(g.o.residual, 16) && on(g.o.pre, 16);
     ProfScope ps(name, 2.0 * g.M * g.N * g.K, 0);
+    if (dtype == DSP_BF16 && direct_ok<AM, BMJ>(g) && g.M > 64) {
+        return launch_direct<DirectTile<AM, BMJ, 256, 256, 2, 4, 64, 4>>(g, st, ps);
+    }
     return dtype == DSP_BF16 ? launch_staged<bf16_t, AM, BMJ>(g, st, ps) : launch_staged<float, AM, BMJ>(g, st, ps);
 }
 
