@@ -361,6 +361,16 @@ struct DirectTile {
     static_assert(ST >= 3 && LDS <= 160 * 1024, "a ring of three stages");
 };
 
+// f(0), f(1), .. f(N - 1) with constants
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F&& f)
+{
+    if constexpr (N > 0) {
+        unrolled<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
 // The place of a tile: those that run together, 32 of an XCD, are eight rows high.
 __device__ inline void place_of(unsigned tile, int tiles_m, int tiles_n, int& tm, int& tn)
 {
@@ -372,47 +382,57 @@ __device__ inline void place_of(unsigned tile, int tiles_m, int tiles_n, int& tm
 }
 
 // One operand's loads of a tile: 1 KB each, the lanes' 16 bytes one behind the other in LDS; a lane fetches the chunk that belongs at its place.
-// What lies behind the rows or behind k reads 0: with k outside by the descriptor's length alone, with k inside by that for the rows and by the
-// lane's offset for k.
+// What lies behind the rows reads 0 by the descriptor's length, and so does what lies behind k where k is outside; where k is inside the lanes of
+// the last tile leave it out.
 template <typename O, int KB, int LOADS, int WAVES>
 struct DirectLoads {
-    const char* base;  // of the next tile (k0)
-    int64_t step;      // bytes to the one behind it
-    int64_t rows_bytes;  // K inside: bytes from the first to the last row; outside: of a row, from the first column of the tile on
-    int64_t stride;    // bytes
+    u32x4_t desc;          // of the next tile
+    uint32_t whole, last;  // its length: with all of k, and in a tile in which k ends
+    uint64_t base, step;
     uint32_t off[LOADS];
     int chunk_k[LOADS];
 
-    __device__ inline DirectLoads(const void* p, int64_t stride_e, int64_t r0, int rows, int wave, int lane)
+    __device__ inline DirectLoads(const void* p, int64_t stride_e, int64_t r0, int rows, int K, int wave, int lane)
     {
         constexpr int RPL = 1024 / O::ROWB;  // rows of LDS in a load
-        stride = stride_e * 2;
-        base = (const char*)p + (O::K_OUTSIDE ? r0 * 2 : r0 * stride);
+        const int64_t stride = stride_e * 2, left = rows - r0, rest = K % O::BK;
+        base = (uint64_t)p + (O::K_OUTSIDE ? r0 * 2 : r0 * stride);
         step = O::K_OUTSIDE ? stride * O::BK : KB;
-        const int64_t left = rows - r0;
-        const int64_t tile_rows = O::K_OUTSIDE ? O::ROWB / 2 : O::CHUNKS * 16 / KB;
-        rows_bytes = O::K_OUTSIDE ? left * 2 : ((left < tile_rows ? left : tile_rows) - 1) * stride;
+        if (O::K_OUTSIDE) {
+            whole = (uint32_t)((O::BK - 1) * stride + left * 2 < 0x7fffffff ? (O::BK - 1) * stride + left * 2 : 0x7fffffff);
+            last = rest ? (uint32_t)((rest - 1) * stride + left * 2 < 0x7fffffff ? (rest - 1) * stride + left * 2 : 0x7fffffff) : whole;
+        } else {  // (rows behind the last one start behind its end)
+            constexpr int64_t TILE = O::CHUNKS * 16 / KB;
+            whole = last = (uint32_t)(((left < TILE ? left : TILE) - 1) * stride + (int64_t)K * 2);
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int row = (i * WAVES + wave) * RPL + lane / O::CPR, chunk = (lane % O::CPR) ^ O::swz(row);
             off[i] = (uint32_t)(row * stride) + chunk * 16;
             chunk_k[i] = chunk * 8;
         }
+        desc = rsrc_words((const void*)base, 0);
+        describe(K);
     }
-    // k_left: elements of k from this tile's first on
-    __device__ inline void issue(uint32_t lds, int k_left, int first, int last, int wave)
+    // k_left: elements of k from the next tile's first on
+    __device__ inline void describe(int k_left)
     {
-        const int64_t length = k_left <= 0 ? 0
-                               : O::K_OUTSIDE ? (int64_t)((k_left < O::BK ? k_left : O::BK) - 1) * stride + rows_bytes
-                                              : rows_bytes + (int64_t)k_left * 2;
-        const u32x4_t r = rsrc_words(base, (uint32_t)(length < 0x7fffffff ? length : 0x7fffffff));
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            if (i < first || i >= last) continue;
-            dma16_untracked(r, lds + (i * WAVES + wave) * 1024, O::K_OUTSIDE || chunk_k[i] < k_left ? off[i] : 0x80000000u);
-        }
+        desc[0] = (uint32_t)base;
+        desc[1] = (uint32_t)(base >> 32) & 0xffffu;
+        desc[2] = k_left >= O::BK ? whole : k_left > 0 ? last : 0u;
     }
-    __device__ inline void advance() { base += step; }
+    __device__ inline void advance(int k_left)
+    {
+        base += step;
+        describe(k_left);
+    }
+    template <int I>
+    __device__ inline void issue(uint32_t lds, int k_left, int wave) const
+    {
+        uint32_t at = off[I];
+        if (!O::K_OUTSIDE && k_left < O::BK) at = chunk_k[I] < k_left ? at : 0x80000000u;
+        dma16_untracked(desc, lds + (I * WAVES + wave) * 1024, at);
+    }
 };
 
 template <typename TL>
@@ -428,18 +448,20 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     place_of(xcd_order(blockIdx.x, gridDim.x), g.tiles_m, g.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * TL::BM;
     const int n0 = tn * TL::BN;
-    DirectLoads<A, TL::KB, LA, TL::WAVES> la(g.a, g.as, m0, g.M, wave, lane);
-    DirectLoads<B, TL::KB, TL::LB, TL::WAVES> lb(g.b, g.bs, n0, g.N, wave, lane);
+    DirectLoads<A, TL::KB, LA, TL::WAVES> la(g.a, g.as, m0, g.M, g.K, wave, lane);
+    DirectLoads<B, TL::KB, TL::LB, TL::WAVES> lb(g.b, g.bs, n0, g.N, g.K, wave, lane);
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     int k_left = g.K;
-    auto issue = [&](int stage, int first, int last) {
-        la.issue(ring + stage * TL::STAGE, k_left, first, last, wave);
-        lb.issue(ring + stage * TL::STAGE + TL::BM * TL::KB, k_left, first - LA, last - LA, wave);
+    // load i of the next tile
+    auto issue = [&](int stage, auto i) {
+        constexpr int I = decltype(i)::value;
+        if constexpr (I < LA) la.template issue<I>(ring + stage * TL::STAGE, k_left, wave);
+        else lb.template issue<I - LA>(ring + stage * TL::STAGE + TL::BM * TL::KB, k_left, wave);
     };
     auto next = [&]() {
-        la.advance();
-        lb.advance();
         k_left -= TL::BK;
+        la.advance(k_left);
+        lb.advance(k_left);
     };
     F16 acc[TM][TN];
 #pragma unroll
@@ -454,20 +476,33 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
 #pragma unroll
         for (int j = 0; j < TN; ++j) b[j] = B::fragment(s + TL::BM * TL::KB, wn * TN + j, ks, lane);
     };
-    auto multiply = [&](const U4 (&a)[TM], const U4 (&b)[TN]) {
-        __builtin_amdgcn_sched_barrier(0);  // the reads of the next step go out before this step's products
+    // The products of a k step.  Between them go out the reads of the next step's operands, one behind each from the first on, and loads [F, L) of the
+    // next tile: what takes the wave's time to issue the matrix unit has for itself, and it has products at once behind a barrier.
+    auto multiply = [&](const U4 (&a)[TM], const U4 (&b)[TN], U4 (&na)[TM], U4 (&nb)[TN], const char* from, auto ks, int stage, auto first, auto last) {
+        constexpr int KS = decltype(ks)::value, F = decltype(first)::value, L = decltype(last)::value, N = TM * TN;
+        __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) Mma32<bf16_t>::run(b[j], a[i], acc[i][j]);
+        unrolled<N>([&](auto q) {
+            constexpr int Q = decltype(q)::value;
+            Mma32<bf16_t>::run(b[Q % TN], a[Q / TN], acc[Q / TN][Q % TN]);
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int R0 = (TM + TN) * Q / N, R1 = (TM + TN) * (Q + 1) / N, L0 = F + (L - F) * Q / N, L1 = F + (L - F) * (Q + 1) / N;
+            unrolled<R1 - R0>([&](auto r) {
+                constexpr int I = R0 + decltype(r)::value;
+                if constexpr (I < TN) nb[I] = B::fragment(from + TL::BM * TL::KB, wn * TN + I, KS, lane);
+                else na[I - TN] = A::fragment(from, wm * TM + I - TN, KS, lane);
+            });
+            unrolled<L1 - L0>([&](auto r) { issue(stage, std::integral_constant<int, L0 + decltype(r)::value>{}); });
+            __builtin_amdgcn_sched_barrier(0);
+        });
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    constexpr int AHEAD = (ST - 3) * LOADS, SLOTS = NKS / 2 + 1;
+    constexpr int AHEAD = (ST - 3) * LOADS, SLOTS = NKS / 2;  // (the k steps behind the barrier)
+    static_assert(NKS % 2 == 0, "the operands change places with every step");
 #pragma unroll
     for (int t = 0; t < ST - 1; ++t) {
-        issue(t, 0, LOADS);
+        unrolled<LOADS>([&](auto i) { issue(t, i); });
         next();
     }
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * LOADS) : "memory");
@@ -481,22 +516,18 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     for (int kt = 0; kt < nk; ++kt) {
         const char* s = smem + st * TL::STAGE;
         const int st1 = st + 1 == ST ? 0 : st + 1, stl = st == 0 ? ST - 1 : st - 1;
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) {
-            if (ks + 1 < NKS) read(s, ks + 1, fa[(ks + 1) & 1], fb[(ks + 1) & 1]);
-            else read(smem + st1 * TL::STAGE, 0, fa[0], fb[0]);
-            multiply(fa[ks & 1], fb[ks & 1]);
-            if (ks == NKS / 2 - 1) {
+        unrolled<NKS>([&](auto k) {
+            constexpr int KS = decltype(k)::value, SLOT = KS - NKS / 2;
+            multiply(fa[KS & 1], fb[KS & 1], fa[(KS + 1) & 1], fb[(KS + 1) & 1], KS + 1 < NKS ? s : smem + st1 * TL::STAGE,
+                     std::integral_constant<int, (KS + 1) % NKS>{}, stl, std::integral_constant<int, SLOT < 0 ? 0 : LOADS * SLOT / SLOTS>{},
+                     std::integral_constant<int, SLOT < 0 ? 0 : LOADS * (SLOT + 1) / SLOTS>{});
+            if constexpr (KS == NKS / 2 - 1) {
                 asm volatile("s_waitcnt vmcnt(%0)" ::"n"(AHEAD) : "memory");
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
             }
-            if (ks >= NKS / 2 - 1) {
-                const int slot = ks - (NKS / 2 - 1);
-                issue(stl, LOADS * slot / SLOTS, LOADS * (slot + 1) / SLOTS);
-                if (slot == SLOTS - 1) next();
-            }
-        }
+        });
+        next();
         st = st1;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads behind the end must not land in what follows
