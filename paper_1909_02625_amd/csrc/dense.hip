@@ -86,16 +86,30 @@ struct OutArgs {
     bool whole;      // runs of eight: whole ones, all on 16-byte addresses
 };
 
+// Eight results of a row as floats: bias, activation and residual are taken in float, and what is stored is rounded once.
 template <typename T>
-__device__ inline void load8(const T* p, float (&v)[8])
+struct Run8 {
+    static constexpr int PIECES = 8 * sizeof(T) / 16;
+    u32x4_t r[PIECES];
+};
+template <typename T>
+__device__ inline Run8<T> load8(const T* p)
+{
+    Run8<T> v;
+#pragma unroll
+    for (int h = 0; h < Run8<T>::PIECES; ++h) v.r[h] = ((const u32x4_t*)p)[h];
+    return v;
+}
+template <typename T>
+__device__ inline void add8(float (&v)[8], const Run8<T>& r)
 {
     constexpr int VW = 16 / sizeof(T);
 #pragma unroll
-    for (int h = 0; h < 8; h += VW) {
+    for (int h = 0; h < Run8<T>::PIECES; ++h) {
         float t[VW];
-        VecIO<T, VW>::load(p + h, t);
+        unpack_run16<T>(r.r[h], t);
 #pragma unroll
-        for (int i = 0; i < VW; ++i) v[h + i] = t[i];
+        for (int i = 0; i < VW; ++i) v[h * VW + i] += t[i];
     }
 }
 template <typename T>
@@ -103,39 +117,18 @@ __device__ inline void store8(T* p, const float (&v)[8])
 {
     constexpr int VW = 16 / sizeof(T);
 #pragma unroll
-    for (int h = 0; h < 8; h += VW) {
+    for (int h = 0; h < Run8<T>::PIECES; ++h) {
         float t[VW];
 #pragma unroll
-        for (int i = 0; i < VW; ++i) t[i] = v[h + i];
-        VecIO<T, VW>::store(p + h, t);
+        for (int i = 0; i < VW; ++i) t[i] = v[h * VW + i];
+        ((u32x4_t*)p)[h] = pack_run16<T>(t);
     }
 }
-
-// Results m, n .. n + 7 (those within N).  Rounded once: bias, activation and residual are taken in float.
+// Results m, n .. of which `count` are within the row, one by one.
 template <typename T>
-__device__ inline void finish_run(const OutArgs& o, int64_t m, int n, float (&v)[8])
+__device__ inline void finish_single(const OutArgs& o, int64_t m, int n, float (&v)[8])
 {
-    if (m >= o.M || n >= o.N) return;
     const int64_t at = m * o.stride + n;
-    if (o.whole) {
-        if (o.bias) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += o.bias[n + i];
-        }
-        if (o.pre) store8<T>((T*)o.pre + at, v);
-        if (o.act != DSP_ACT_IDENTITY) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = act_of(o.act, v[i]);
-        }
-        if (o.residual) {
-            float r[8];
-            load8<T>((const T*)o.residual + at, r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += r[i];
-        }
-        store8<T>((T*)o.out + at, v);
-        return;
-    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (n + i >= o.N) break;
@@ -241,12 +234,30 @@ __device__ inline unsigned xcd_order(unsigned b, unsigned nb)
 }
 
 // The accumulators hold the transposed tile: a lane has, for row lane % 32 of a block, runs of four consecutive columns.  Through LDS,
-// 32 rows of a wave at a time, they become runs of eight, whole lines of a row.
-template <typename TL, int TM, int TN>
+// 32 rows of a wave at a time, they become runs of eight, whole lines of a row.  WHOLE: all runs are, on 16-byte addresses, and the
+// activation is ACT.  Then the residual of the next 32 rows is on its way meanwhile.  (Code that runs once a tile is fetched once a tile: with all four
+// activations in it, unrolled, 8192 x 2048 x 4096 with relu takes 167 us instead of 156.)
+template <typename TL, bool WHOLE, int ACT, bool RES, int TM, int TN>
 __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const OutArgs& o, int64_t m0, int n0, int wave, int lane)
 {
-    constexpr int ROW = TL::OUT_ROW, LPR = TN * 4, RPP = 64 / LPR;
+    typedef typename TL::T T;
+    constexpr int ROW = TL::OUT_ROW, LPR = TN * 4, RPP = 64 / LPR, PASSES = 32 / RPP;
     float* const mine = (float*)smem + wave * 32 * ROW;
+    const int col = lane % LPR * 8, n = n0 + col, row = lane / LPR;
+    float bias[8] = {};
+    if (WHOLE && o.bias && n < o.N) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bias[i] = o.bias[n + i];
+    }
+    Run8<T> res[2][PASSES];
+    auto fetch = [&](int i, Run8<T> (&r)[PASSES]) {
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+            const int64_t m = m0 + i * 32 + q * RPP + row;
+            r[q] = load8<T>((const T*)o.residual + (m < o.M && n < o.N ? m * o.stride + n : 0));
+        }
+    };
+    if constexpr (RES) fetch(0, res[0]);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -256,12 +267,35 @@ __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const O
                 *(F4*)(mine + (lane & 31) * ROW + j * 32 + 8 * q + 4 * (lane >> 5)) =
                     F4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int r = 0; r < 32; r += RPP) {
-            const int row = r + lane / LPR, col = lane % LPR * 8;
-            const F4 u = *(const F4*)(mine + row * ROW + col), w = *(const F4*)(mine + row * ROW + col + 4);
+        if constexpr (RES)
+            if (i + 1 < TM) fetch(i + 1, res[(i + 1) & 1]);
+        auto pass = [&](int q, const Run8<T>& r) {
+            const int64_t m = m0 + i * 32 + q * RPP + row;
+            const float* from = mine + (q * RPP + row) * ROW + col;
+            const F4 u = *(const F4*)from, w = *(const F4*)(from + 4);
             float v[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
-            finish_run<typename TL::T>(o, m0 + i * 32 + row, n0 + col, v);
+            if (m >= o.M || n >= o.N) return;
+            if constexpr (!WHOLE) {
+                finish_single<T>(o, m, n, v);
+            } else {
+                const int64_t at = m * o.stride + n;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += bias[e];
+                if (o.pre) store8<T>((T*)o.pre + at, v);
+                if constexpr (ACT != DSP_ACT_IDENTITY) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = act_of(ACT, v[e]);
+                }
+                if constexpr (RES) add8<T>(v, r);
+                store8<T>((T*)o.out + at, v);
+            }
+        };
+        if constexpr (RES) {
+#pragma unroll
+            for (int q = 0; q < PASSES; ++q) pass(q, res[i & 1][q]);
+        } else {
+#pragma unroll 1
+            for (int q = 0; q < PASSES; ++q) pass(q, Run8<T>{});
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -339,7 +373,7 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
         if (kt + 1 < nk) keep_both((kt + 1) & 1);
         __syncthreads();
     }
-    finish_tile<TL>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
+    finish_tile<TL, false, 0, false>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
 }
 
 // ---- the same for bf16 rows of whole 16-byte runs: tiles go from memory to LDS directly ---------------
@@ -435,7 +469,7 @@ struct DirectLoads {
     }
 };
 
-template <typename TL>
+template <typename TL, int ACT, bool RES>
 __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL::WAVES / 4, TL::WAVES / 4))) void dense_direct_kernel(GemmArgs g)
 {
     typedef typename TL::A A;
@@ -532,7 +566,7 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads behind the end must not land in what follows
     __syncthreads();
-    finish_tile<TL>(smem, acc, g.o, m0 + wm * TM * 32, n0 + wn * TN * 32, wave, lane);
+    finish_tile<TL, true, ACT, RES>(smem, acc, g.o, m0 + wm * TM * 32, n0 + wn * TN * 32, wave, lane);
 }
 
 // ---- the gradient in front of the activation, and its column sums ------------------------------------
@@ -640,12 +674,12 @@ int launch_staged(GemmArgs& g, hipStream_t st, ProfScope& ps)
     return DSP_OK;
 }
 
-template <typename TL>
+template <typename TL, int ACT = DSP_ACT_IDENTITY, bool RES = false>
 int launch_direct(GemmArgs& g, hipStream_t st, ProfScope& ps)
 {
     g.tiles_m = ceil_div(g.M, TL::BM);
     g.tiles_n = ceil_div(g.N, TL::BN);
-    auto kern = dense_direct_kernel<TL>;
+    auto kern = dense_direct_kernel<TL, ACT, RES>;
     static std::atomic<bool> attr_done{false};
     if (!attr_done) {
         DSP_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS));
@@ -654,6 +688,18 @@ int launch_direct(GemmArgs& g, hipStream_t st, ProfScope& ps)
     DSP_LAUNCH(ps, kern, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(TL::THREADS), TL::LDS, st, g);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
+}
+
+template <typename TL>
+int with_act(GemmArgs& g, hipStream_t st, ProfScope& ps)
+{
+    const bool res = g.o.residual != nullptr;
+    switch (g.o.act) {
+    case DSP_ACT_RELU: return res ? launch_direct<TL, DSP_ACT_RELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_RELU, false>(g, st, ps);
+    case DSP_ACT_GELU: return res ? launch_direct<TL, DSP_ACT_GELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_GELU, false>(g, st, ps);
+    case DSP_ACT_SILU: return res ? launch_direct<TL, DSP_ACT_SILU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_SILU, false>(g, st, ps);
+    default: return res ? launch_direct<TL, DSP_ACT_IDENTITY, true>(g, st, ps) : launch_direct<TL, DSP_ACT_IDENTITY, false>(g, st, ps);
+    }
 }
 
 // Rows of whole 16-byte runs on 16-byte addresses, whose tiles 32-bit offsets reach.
@@ -672,8 +718,10 @@ int contract(int dtype, const char* name, GemmArgs& g, hipStream_t st)
     g.o.N = g.N;
     g.o.whole = g.N % 8 == 0 && g.o.stride * e % 16 == 0 && on(g.o.out, 16) && on(g.o.residual, 16) && on(g.o.pre, 16);
     ProfScope ps(name, 2.0 * g.M * g.N * g.K, 0);
-    if (dtype == DSP_BF16 && direct_ok<AM, BMJ>(g) && g.M > 64) {
-        return launch_direct<DirectTile<AM, BMJ, 256, 256, 2, 4, 64, 4>>(g, st, ps);
+    if (dtype == DSP_BF16 && g.o.whole && direct_ok<AM, BMJ>(g) && g.M > 64) {
+        typedef DirectTile<AM, BMJ, 256, 256, 2, 4, 64, 4> TL;
+        if constexpr (AM || BMJ) return launch_direct<TL>(g, st, ps);
+        else return with_act<TL>(g, st, ps);
     }
     return dtype == DSP_BF16 ? launch_staged<bf16_t, AM, BMJ>(g, st, ps) : launch_staged<float, AM, BMJ>(g, st, ps);
 }
