@@ -82,6 +82,7 @@ struct OutArgs {
     const void* residual;
     void* pre;
     int64_t stride;  // of out, residual and pre
+    float* partial;  // of a contraction cut into parts: [parts][M][N rounded up to 8], or nullptr
     int M, N, act;
     bool whole;      // runs of eight: whole ones, all on 16-byte addresses
 };
@@ -147,8 +148,12 @@ struct GemmArgs {
     int64_t as, bs;
     int M, N, K;
     int tiles_m, tiles_n;
+    int parts, part_k;  // elements of k of each part (whole tiles)
+    bool padded;        // A's rows go on with zeros up to a multiple of eight
     OutArgs o;
 };
+
+__host__ __device__ inline int64_t partial_stride(int N) { return ((int64_t)N + 7) / 8 * 8; }
 
 template <typename T>
 struct Mma32;
@@ -180,10 +185,11 @@ struct OperandTile {
     static constexpr bool K_OUTSIDE = MAJOR;
     static constexpr int ROWB = MAJOR ? R * (int)sizeof(T) : KB, CPR = ROWB / 16;
     static_assert(KB == 128 || KB == 64, "bytes of k in a row");
-    static_assert(!MAJOR || ROWB >= 256, "rows of four banks' turns");
+    static_assert(!MAJOR || ROWB >= 128, "eight chunks a row");
     __device__ static inline int swz(int row)
     {
         if (!MAJOR) return KB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+        if (ROWB == 128) return (row & 2) << 1;
         return sizeof(T) == 2 ? (row & 3) << 2 : ((row >> 2) & 1) << 3;
     }
     // chunk i of the tile: row and chunk within it, and where it lies
@@ -237,7 +243,7 @@ __device__ inline unsigned xcd_order(unsigned b, unsigned nb)
 // 32 rows of a wave at a time, they become runs of eight, whole lines of a row.  WHOLE: all runs are, on 16-byte addresses, and the
 // activation is ACT.  Then the residual of the next 32 rows is on its way meanwhile.  (Code that runs once a tile is fetched once a tile: with all four
 // activations in it, unrolled, 8192 x 2048 x 4096 with relu takes 167 us instead of 156.)
-template <typename TL, bool WHOLE, int ACT, bool RES, int TM, int TN>
+template <typename TL, bool WHOLE, int ACT, bool RES, bool PART = false, int TM, int TN>
 __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const OutArgs& o, int64_t m0, int n0, int wave, int lane)
 {
     typedef typename TL::T T;
@@ -275,7 +281,11 @@ __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const O
             const F4 u = *(const F4*)from, w = *(const F4*)(from + 4);
             float v[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
             if (m >= o.M || n >= o.N) return;
-            if constexpr (!WHOLE) {
+            if constexpr (PART) {
+                float* to = o.partial + ((int64_t)blockIdx.y * o.M + m) * partial_stride(o.N) + n;
+                *(F4*)to = u;
+                *(F4*)(to + 4) = w;
+            } else if constexpr (!WHOLE) {
                 finish_single<T>(o, m, n, v);
             } else {
                 const int64_t at = m * o.stride + n;
@@ -301,7 +311,7 @@ __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const O
     }
 }
 
-template <typename TL>
+template <typename TL, bool PART>
 __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
 {
     typedef typename TL::T T;
@@ -351,12 +361,12 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
         for (int j = 0; j < TL::TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const int nk = (g.K + A::BK - 1) / A::BK;
-    load_both(0);
+    const int k0 = PART ? blockIdx.y * g.part_k : 0, k1 = PART && k0 + g.part_k < g.K ? k0 + g.part_k : g.K, nk = (k1 - k0 + A::BK - 1) / A::BK;
+    load_both(k0);
     keep_both(0);
     __syncthreads();
     for (int kt = 0; kt < nk; ++kt) {
-        if (kt + 1 < nk) load_both((kt + 1) * A::BK);
+        if (kt + 1 < nk) load_both(k0 + (kt + 1) * A::BK);
         const char* s = smem + (kt & 1) * TL::STAGE;
 #pragma unroll
         for (int ks = 0; ks < TL::NKS; ++ks) {
@@ -373,7 +383,7 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
         if (kt + 1 < nk) keep_both((kt + 1) & 1);
         __syncthreads();
     }
-    finish_tile<TL, false, 0, false>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
+    finish_tile<TL, false, 0, false, PART>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
 }
 
 // ---- the same for bf16 rows of whole 16-byte runs: tiles go from memory to LDS directly ---------------
@@ -426,18 +436,18 @@ struct DirectLoads {
     uint32_t off[LOADS];
     int chunk_k[LOADS];
 
-    __device__ inline DirectLoads(const void* p, int64_t stride_e, int64_t r0, int rows, int K, int wave, int lane)
+    __device__ inline DirectLoads(const void* p, int64_t stride_e, int64_t r0, int rows, int k0, int k1, int K, bool padded, int wave, int lane)
     {
         constexpr int RPL = 1024 / O::ROWB;  // rows of LDS in a load
-        const int64_t stride = stride_e * 2, left = rows - r0, rest = K % O::BK;
-        base = (uint64_t)p + (O::K_OUTSIDE ? r0 * 2 : r0 * stride);
+        const int64_t stride = stride_e * 2, left = (padded && O::K_OUTSIDE ? (rows + 7) / 8 * 8 : rows) - r0, rest = (k1 - k0) % O::BK;
+        base = (uint64_t)p + (O::K_OUTSIDE ? r0 * 2 + k0 * stride : r0 * stride + (int64_t)k0 * 2);
         step = O::K_OUTSIDE ? stride * O::BK : KB;
         if (O::K_OUTSIDE) {
             whole = (uint32_t)((O::BK - 1) * stride + left * 2 < 0x7fffffff ? (O::BK - 1) * stride + left * 2 : 0x7fffffff);
             last = rest ? (uint32_t)((rest - 1) * stride + left * 2 < 0x7fffffff ? (rest - 1) * stride + left * 2 : 0x7fffffff) : whole;
         } else {  // (rows behind the last one start behind its end)
             constexpr int64_t TILE = O::CHUNKS * 16 / KB;
-            whole = last = (uint32_t)(((left < TILE ? left : TILE) - 1) * stride + (int64_t)K * 2);
+            whole = last = (uint32_t)(((left < TILE ? left : TILE) - 1) * stride + (int64_t)((padded ? (K + 7) / 8 * 8 : K) - k0) * 2);
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
@@ -446,7 +456,7 @@ struct DirectLoads {
             chunk_k[i] = chunk * 8;
         }
         desc = rsrc_words((const void*)base, 0);
-        describe(K);
+        describe(k1 - k0);
     }
     // k_left: elements of k from the next tile's first on
     __device__ inline void describe(int k_left)
@@ -469,7 +479,7 @@ struct DirectLoads {
     }
 };
 
-template <typename TL, int ACT, bool RES>
+template <typename TL, int ACT, bool RES, bool PART>
 __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL::WAVES / 4, TL::WAVES / 4))) void dense_direct_kernel(GemmArgs g)
 {
     typedef typename TL::A A;
@@ -482,10 +492,11 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     place_of(xcd_order(blockIdx.x, gridDim.x), g.tiles_m, g.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * TL::BM;
     const int n0 = tn * TL::BN;
-    DirectLoads<A, TL::KB, LA, TL::WAVES> la(g.a, g.as, m0, g.M, g.K, wave, lane);
-    DirectLoads<B, TL::KB, TL::LB, TL::WAVES> lb(g.b, g.bs, n0, g.N, g.K, wave, lane);
+    const int k0 = PART ? blockIdx.y * g.part_k : 0, k1 = PART && k0 + g.part_k < g.K ? k0 + g.part_k : g.K;
+    DirectLoads<A, TL::KB, LA, TL::WAVES> la(g.a, g.as, m0, g.M, k0, k1, g.K, g.padded, wave, lane);
+    DirectLoads<B, TL::KB, TL::LB, TL::WAVES> lb(g.b, g.bs, n0, g.N, k0, k1, g.K, false, wave, lane);
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    int k_left = g.K;
+    int k_left = k1 - k0;
     // load i of the next tile
     auto issue = [&](int stage, auto i) {
         constexpr int I = decltype(i)::value;
@@ -545,7 +556,7 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): no scalar load is pending when the counted waits begin
     U4 fa[2][TM], fb[2][TN];
     read(smem, 0, fa[0], fb[0]);
-    const int nk = (g.K + TL::BK - 1) / TL::BK;
+    const int nk = (k1 - k0 + TL::BK - 1) / TL::BK;
     int st = 0;
     for (int kt = 0; kt < nk; ++kt) {
         const char* s = smem + st * TL::STAGE;
@@ -566,7 +577,7 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads behind the end must not land in what follows
     __syncthreads();
-    finish_tile<TL, true, ACT, RES>(smem, acc, g.o, m0 + wm * TM * 32, n0 + wn * TN * 32, wave, lane);
+    finish_tile<TL, true, ACT, RES, PART>(smem, acc, g.o, m0 + wm * TM * 32, n0 + wn * TN * 32, wave, lane);
 }
 
 // ---- the gradient in front of the activation, and its column sums ------------------------------------
@@ -577,45 +588,185 @@ struct GradArgs {
     int64_t ys, gs;
     int M, N, act, rows_per_part;
 };
-constexpr int kGradThreads = 256, kGradCols = 64;
+constexpr int kGradThreads = 256, kGradAhead = 4;
 
-// A workgroup has 64 columns, 8 lanes a row, 32 rows at a time, and a part of the rows.  g is rounded to the storage type because
-// the matrix instructions read that; the column sums are of the values before.
-template <typename T>
+// A workgroup has LPR lanes of eight columns side by side, the rest of it rows, and a part of the rows.  g is rounded to the storage type because
+// the matrix instructions read that; the column sums are of the values before.  Behind the last column g's rows are filled up with zeros.
+template <typename T, int LPR>
 __global__ __launch_bounds__(kGradThreads) void dense_grad_kernel(GradArgs a)
 {
-    __shared__ float sums[32][kGradCols + 4];
-    const int c = threadIdx.x % 8 * 8, r = threadIdx.x / 8, n = blockIdx.x * kGradCols + c;
+    constexpr int E = 16 / sizeof(T), PIECES = 8 / E, ROWS = kGradThreads / LPR;
+    __shared__ float sums[ROWS][LPR * 8 + 4];
+    const int c = threadIdx.x % LPR * 8, r = threadIdx.x / LPR, n = blockIdx.x * LPR * 8 + c, count = a.N - n;
     const int64_t first = (int64_t)blockIdx.y * a.rows_per_part, last = first + a.rows_per_part < a.M ? first + a.rows_per_part : a.M;
     float s[8] = {};
-    for (int64_t m = first + r; m < last; m += 32)
+    if (count > 0)
+        for (int64_t m0 = first + r; m0 < last; m0 += ROWS * kGradAhead) {
+            u32x4_t d[kGradAhead][PIECES], p[kGradAhead][PIECES];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (n + i >= a.N) continue;
-            float v = to_float<T>(((const T*)a.dy)[m * a.ys + n + i]);
-            if (a.pre) v *= act_slope(a.act, to_float<T>(((const T*)a.pre)[m * a.ys + n + i]));
-            if (a.g) ((T*)a.g)[m * a.gs + n + i] = from_float<T>(v);
-            s[i] += v;
+            for (int i = 0; i < kGradAhead; ++i) {
+                const int64_t m = m0 + i * ROWS < last ? m0 + i * ROWS : m0;
+#pragma unroll
+                for (int h = 0; h < PIECES; ++h) {
+                    const int left = count - h * E;
+                    d[i][h] = load_run16<T>((const T*)a.dy + m * a.ys + n + (left > 0 ? h * E : 0), left > 0 ? left : 0, T{});
+                    if (a.pre) p[i][h] = load_run16<T>((const T*)a.pre + m * a.ys + n + (left > 0 ? h * E : 0), left > 0 ? left : 0, T{});
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kGradAhead; ++i) {
+                const int64_t m = m0 + i * ROWS;
+                if (m >= last) break;
+#pragma unroll
+                for (int h = 0; h < PIECES; ++h) {
+                    float v[E], q[E];
+                    unpack_run16<T>(d[i][h], v);
+                    if (a.pre) {
+                        unpack_run16<T>(p[i][h], q);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) v[e] *= act_slope(a.act, q[e]);
+                    }
+                    if (a.g) *(u32x4_t*)((T*)a.g + m * a.gs + n + h * E) = pack_run16<T>(v);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s[h * E + e] += v[e];
+                }
+            }
         }
     if (!a.partial) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[r][c + i] = s[i];
     __syncthreads();
-    const int col = threadIdx.x;
-    if (col < kGradCols && blockIdx.x * kGradCols + col < a.N) {
+    for (int col = threadIdx.x; col < LPR * 8 && blockIdx.x * LPR * 8 + col < a.N; col += kGradThreads) {
         float t = 0.f;
-        for (int q = 0; q < 32; ++q) t += sums[q][col];
-        a.partial[(int64_t)blockIdx.y * a.N + blockIdx.x * kGradCols + col] = t;
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) t += sums[q][col];
+        a.partial[(int64_t)blockIdx.y * a.N + blockIdx.x * LPR * 8 + col] = t;
     }
 }
 
-__global__ __launch_bounds__(256) void dense_bias_kernel(const float* partial, float* dbias, int parts, int N)
+constexpr int kBiasWaves = 16;
+
+__global__ __launch_bounds__(64 * kBiasWaves) void dense_bias_kernel(const float* partial, float* dbias, int parts, int N)
 {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
+    __shared__ float sums[kBiasWaves][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = blockIdx.x * 64 + lane;
     float s = 0.f;
-    for (int p = 0; p < parts; ++p) s += partial[(int64_t)p * N + n];
+    if (n < N) {
+#pragma unroll 4
+        for (int p = wave; p < parts; p += kBiasWaves) s += partial[(int64_t)p * N + n];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave || n >= N) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kBiasWaves; ++w) s += sums[w][lane];
     dbias[n] = s;
+}
+
+// ---- the parts of a contraction, added up in their order ---------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void dense_parts_kernel(OutArgs o, int parts)
+{
+    const int64_t stride = partial_stride(o.N), runs = stride / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= runs * o.M) return;
+    const int64_t m = i / runs;
+    const int n = (int)(i - m * runs) * 8;
+    const float* from = o.partial + m * stride + n;
+    F4 u = {}, w = {};
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p, from += o.M * stride) {
+        u += *(const F4*)from;
+        w += *(const F4*)(from + 4);
+    }
+    float v[8] = {u[0], u[1], u[2], u[3], w[0], w[1], w[2], w[3]};
+    if (!o.whole) {
+        finish_single<T>(o, m, n, v);
+        return;
+    }
+    const int64_t at = m * o.stride + n;
+    if (o.bias) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += o.bias[n + e];
+    }
+    if (o.pre) store8<T>((T*)o.pre + at, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act_of(o.act, v[e]);
+    if (o.residual) add8<T>(v, load8<T>((const T*)o.residual + at));
+    store8<T>((T*)o.out + at, v);
+}
+
+// ---- few rows: every wave reads filters once, for all of them ---------------------------------------
+//
+// A workgroup has 16 filters; its waves share their k in steps of 64 bytes a row, and their sums meet in LDS.  The filters are one operand of a 16 x 16
+// product and MT times 16 rows of x the other, both straight from memory.  What bounds it is the filters' bytes.
+template <typename T>
+struct Mma16;
+template <>
+struct Mma16<bf16_t> {
+    __device__ static inline void run(U4 a, U4 b, F4& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), __builtin_bit_cast(B8, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma16<float> {
+    __device__ static inline void run(U4 a, U4 b, F4& c)
+    {
+        const F4 fa = __builtin_bit_cast(F4, a), fb = __builtin_bit_cast(F4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[i], c, 0, 0, 0);
+    }
+};
+constexpr int kFewWaves = 8;
+
+template <typename T, int MT>
+__global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(GemmArgs g)
+{
+    constexpr int E = 16 / sizeof(T), STEP = 4 * E, AHEAD = MT == 4 ? 2 : 4;
+    __shared__ float sums[kFewWaves][MT * 16][16 + 1];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n0 = blockIdx.x * 16, r = lane % 16, ko = lane / 16 * E;
+    const bool there = n0 + r < g.N;
+    const T* const w = (const T*)g.b + (there ? (int64_t)(n0 + r) * g.bs : 0);
+    F4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = F4{0.f, 0.f, 0.f, 0.f};
+    for (int k0 = wave * AHEAD * STEP; k0 < g.K; k0 += kFewWaves * AHEAD * STEP) {
+        U4 fw[AHEAD], fx[AHEAD][MT];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int k = k0 + i * STEP + ko, left = g.K - k > 0 ? g.K - k : 0;
+            fw[i] = load_run16<T>(w + (left ? k : 0), there ? left : 0, T{});
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const int m = t * 16 + r;
+                fx[i][t] = load_run16<T>((const T*)g.a + (m < g.M && left ? m * g.as + k : 0), m < g.M ? left : 0, T{});
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) Mma16<T>::run(fw[i], fx[i][t], acc[t]);
+    }
+    // lane: row lane % 16 of x, filters 4 (lane / 16) .. + 3
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[wave][t * 16 + r][lane / 16 * 4 + e] = acc[t][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < MT * 256; i += 64 * kFewWaves) {
+        const int m = i / 16, c = i % 16, n = n0 + c;
+        if (m >= g.M || n >= g.N) continue;
+        float u = 0.f;
+#pragma unroll
+        for (int q = 0; q < kFewWaves; ++q) u += sums[q][m][c];
+        const int64_t at = m * g.o.stride + n;
+        if (g.o.bias) u += g.o.bias[n];
+        if (g.o.pre) ((T*)g.o.pre)[at] = from_float<T>(u);
+        u = act_of(g.o.act, u);
+        if (g.o.residual) u += to_float<T>(((const T*)g.o.residual)[at]);
+        ((T*)g.o.out)[at] = from_float<T>(u);
+    }
 }
 
 // ---- host --------------------------------------------------------------------------------------------
@@ -643,49 +794,101 @@ int check_desc(const dsp_dense_desc* d, const char* who)
 
 bool on(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
 
-// The rows of the column sums' parts: as many workgroups as four for a compute unit.
-struct BackPlan {
-    int parts, rows_per_part;
-    int64_t gs;
-    size_t g_bytes, bytes;
-};
 size_t rounded16(size_t n) { return (n + 15) / 16 * 16; }
-BackPlan back_plan(const dsp_dense_desc* d)
+
+enum Kernel { kFew, kDirect256, kDirect128, kStaged128, kStaged64 };
+
+// Who forms a contraction, and into how many parts its k is cut.
+struct ContractPlan {
+    Kernel kernel;
+    int parts, part_k;
+    size_t bytes;
+};
+struct Shape {
+    int64_t M;
+    int N, K;
+    int dtype;
+    bool direct;  // bf16 rows of whole 16-byte runs on 16-byte addresses throughout
+    bool k_inside;
+};
+ContractPlan contract_plan(const Shape& s)
 {
-    BackPlan p;
-    const int strips = ceil_div(d->cout, kGradCols);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(1024 / strips, ceil_div(d->M, 32)));
-    p.rows_per_part = (int)((d->M + want - 1) / want);
-    p.parts = ceil_div(d->M, p.rows_per_part);
-    p.gs = (d->cout + 7) / 8 * 8;
-    p.g_bytes = d->act == DSP_ACT_IDENTITY ? 0 : rounded16((size_t)d->M * p.gs * dtype_size(d->dtype));
-    p.bytes = p.g_bytes + rounded16((size_t)p.parts * d->cout * 4);
+    ContractPlan p{kStaged128, 1, 0, 0};
+    if (s.k_inside && s.M <= 64) {
+        p.kernel = kFew;
+        return p;
+    }
+    auto tiles = [&](int t) { return (int64_t)ceil_div(s.M, t) * ceil_div(s.N, t); };
+    int64_t n;
+    if (s.direct && tiles(256) >= 128) p.kernel = kDirect256, n = tiles(256);
+    else if (s.direct && tiles(128) >= 64) p.kernel = kDirect128, n = tiles(128);
+    else if (tiles(128) >= 256) p.kernel = kStaged128, n = tiles(128);
+    else p.kernel = kStaged64, n = tiles(64);
+    // few tiles and a long k: parts, of 512 elements at least, until there are two workgroups for a compute unit
+    const int64_t want = p.kernel == kDirect256 ? 1 : std::min<int64_t>(512 / n, s.K / 512);
+    if (want > 1) {
+        p.part_k = ceil_div(ceil_div(s.K, want), 64) * 64;
+        p.parts = ceil_div(s.K, p.part_k);
+        if (p.parts > 1) p.bytes = (size_t)p.parts * s.M * partial_stride(s.N) * sizeof(float);
+    }
     return p;
 }
 
-template <typename T, bool AM, bool BMJ>
+// Behind dy and pre: g in the storage type, then the column sums' parts (as many workgroups as four for a compute unit), then the parts of whichever
+// product has more.  (What the products may do without a look at the addresses is what they are given memory for.)
+struct BackPlan {
+    int lpr, parts, rows_per_part;
+    int64_t gs;
+    size_t g_bytes, sums, bytes;
+};
+size_t most_bytes(Shape s)
+{
+    s.direct = false;
+    const size_t a = contract_plan(s).bytes;
+    s.direct = s.dtype == DSP_BF16;
+    return std::max(a, contract_plan(s).bytes);
+}
+BackPlan back_plan(const dsp_dense_desc* d)
+{
+    BackPlan p;
+    p.lpr = d->cout >= 256 ? 64 : 8;
+    const int strips = ceil_div(d->cout, p.lpr * 8), rows = kGradThreads / p.lpr * kGradAhead;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(1024 / strips, ceil_div(d->M, rows)));
+    p.rows_per_part = ceil_div(ceil_div(d->M, want), rows) * rows;
+    p.parts = ceil_div(d->M, p.rows_per_part);
+    p.gs = (d->cout + 7) / 8 * 8;
+    p.g_bytes = d->act == DSP_ACT_IDENTITY ? 0 : rounded16((size_t)d->M * p.gs * dtype_size(d->dtype));
+    p.sums = rounded16((size_t)p.parts * d->cout * 4);
+    p.bytes = p.g_bytes + p.sums + std::max(most_bytes({d->M, d->cin, d->cout, d->dtype, false, false}),
+                                            most_bytes({d->cout, d->cin, (int)d->M, d->dtype, false, false}));
+    return p;
+}
+
+template <typename T, bool AM, bool BMJ, int TILE>
 int launch_staged(GemmArgs& g, hipStream_t st, ProfScope& ps)
 {
-    typedef StagedTile<T, AM, BMJ, 128, 128, 2, 2, 64> TL;
+    typedef StagedTile<T, AM, BMJ, TILE, TILE, 2, 2, 64> TL;
     g.tiles_m = ceil_div(g.M, TL::BM);
     g.tiles_n = ceil_div(g.N, TL::BN);
-    DSP_LAUNCH(ps, dense_staged_kernel<TL>, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(TL::THREADS), 0, st, g);
+    const dim3 grid((unsigned)g.tiles_m * g.tiles_n, g.parts);
+    if (g.parts > 1) DSP_LAUNCH(ps, (dense_staged_kernel<TL, true>), grid, dim3(TL::THREADS), 0, st, g);
+    else DSP_LAUNCH(ps, (dense_staged_kernel<TL, false>), grid, dim3(TL::THREADS), 0, st, g);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
 
-template <typename TL, int ACT = DSP_ACT_IDENTITY, bool RES = false>
+template <typename TL, int ACT = DSP_ACT_IDENTITY, bool RES = false, bool PART = false>
 int launch_direct(GemmArgs& g, hipStream_t st, ProfScope& ps)
 {
     g.tiles_m = ceil_div(g.M, TL::BM);
     g.tiles_n = ceil_div(g.N, TL::BN);
-    auto kern = dense_direct_kernel<TL, ACT, RES>;
+    auto kern = dense_direct_kernel<TL, ACT, RES, PART>;
     static std::atomic<bool> attr_done{false};
     if (!attr_done) {
         DSP_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS));
         attr_done = true;
     }
-    DSP_LAUNCH(ps, kern, dim3((unsigned)g.tiles_m * g.tiles_n), dim3(TL::THREADS), TL::LDS, st, g);
+    DSP_LAUNCH(ps, kern, dim3((unsigned)g.tiles_m * g.tiles_n, g.parts), dim3(TL::THREADS), TL::LDS, st, g);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
@@ -693,6 +896,8 @@ int launch_direct(GemmArgs& g, hipStream_t st, ProfScope& ps)
 template <typename TL>
 int with_act(GemmArgs& g, hipStream_t st, ProfScope& ps)
 {
+    if (g.parts > 1) return launch_direct<TL, DSP_ACT_IDENTITY, false, true>(g, st, ps);
+    if constexpr (TL::A::K_OUTSIDE || TL::B::K_OUTSIDE) return launch_direct<TL>(g, st, ps);
     const bool res = g.o.residual != nullptr;
     switch (g.o.act) {
     case DSP_ACT_RELU: return res ? launch_direct<TL, DSP_ACT_RELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_RELU, false>(g, st, ps);
@@ -702,28 +907,71 @@ int with_act(GemmArgs& g, hipStream_t st, ProfScope& ps)
     }
 }
 
+template <typename T>
+int launch_few(GemmArgs& g, hipStream_t st, ProfScope& ps)
+{
+    const dim3 grid(ceil_div(g.N, 16)), block(64 * kFewWaves);
+    if (g.M <= 16) DSP_LAUNCH(ps, (dense_few_kernel<T, 1>), grid, block, 0, st, g);
+    else if (g.M <= 32) DSP_LAUNCH(ps, (dense_few_kernel<T, 2>), grid, block, 0, st, g);
+    else DSP_LAUNCH(ps, (dense_few_kernel<T, 4>), grid, block, 0, st, g);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
 // Rows of whole 16-byte runs on 16-byte addresses, whose tiles 32-bit offsets reach.
 template <bool AM, bool BMJ>
 bool direct_ok(const GemmArgs& g)
 {
     const int64_t most = (1ll << 31) / 1024;
-    return on(g.a, 16) && on(g.b, 16) && g.as % 8 == 0 && g.bs % 8 == 0 && (AM ? g.M : g.K) % 8 == 0 && (BMJ ? g.N : g.K) % 8 == 0 && g.as < most && g.bs < most;
+    return on(g.a, 16) && on(g.b, 16) && g.as % 8 == 0 && g.bs % 8 == 0 && (g.padded || (AM ? g.M : g.K) % 8 == 0) && (BMJ ? g.N : g.K) % 8 == 0 &&
+           g.as < most && g.bs < most;
+}
+
+template <bool AM, bool BMJ, typename T>
+int contract_t(const ContractPlan& p, GemmArgs& g, hipStream_t st, ProfScope& ps)
+{
+    if constexpr (!AM && !BMJ)
+        if (p.kernel == kFew) return launch_few<T>(g, st, ps);
+    if constexpr (sizeof(T) == 2) {
+        if (p.kernel == kDirect256) return with_act<DirectTile<AM, BMJ, 256, 256, 2, 4, 64, 4>>(g, st, ps);
+        if (p.kernel == kDirect128) return with_act<DirectTile<AM, BMJ, 128, 128, 2, 2, 64, 4>>(g, st, ps);
+    }
+    return p.kernel == kStaged128 ? launch_staged<T, AM, BMJ, 128>(g, st, ps) : launch_staged<T, AM, BMJ, 64>(g, st, ps);
 }
 
 template <bool AM, bool BMJ>
-int contract(int dtype, const char* name, GemmArgs& g, hipStream_t st)
+int contract(int dtype, const char* name, GemmArgs& g, void* workspace, hipStream_t st)
 {
     const size_t e = dtype_size(dtype);
     g.o.M = g.M;
     g.o.N = g.N;
     g.o.whole = g.N % 8 == 0 && g.o.stride * e % 16 == 0 && on(g.o.out, 16) && on(g.o.residual, 16) && on(g.o.pre, 16);
-    ProfScope ps(name, 2.0 * g.M * g.N * g.K, 0);
-    if (dtype == DSP_BF16 && g.o.whole && direct_ok<AM, BMJ>(g) && g.M > 64) {
-        typedef DirectTile<AM, BMJ, 256, 256, 2, 4, 64, 4> TL;
-        if constexpr (AM || BMJ) return launch_direct<TL>(g, st, ps);
-        else return with_act<TL>(g, st, ps);
+    const ContractPlan p = contract_plan({g.M, g.N, g.K, dtype, dtype == DSP_BF16 && g.o.whole && direct_ok<AM, BMJ>(g), !AM && !BMJ});
+    g.parts = p.parts;
+    g.part_k = p.part_k;
+    g.o.partial = (float*)workspace;
+    {
+        ProfScope ps(name, 2.0 * g.M * g.N * g.K, 0);
+        if (dtype == DSP_BF16) DSP_TRY((contract_t<AM, BMJ, bf16_t>(p, g, st, ps)));
+        else DSP_TRY((contract_t<AM, BMJ, float>(p, g, st, ps)));
     }
-    return dtype == DSP_BF16 ? launch_staged<bf16_t, AM, BMJ>(g, st, ps) : launch_staged<float, AM, BMJ>(g, st, ps);
+    if (p.parts == 1) return DSP_OK;
+    ProfScope ps("dense_parts", (double)p.bytes, 1);
+    const dim3 grid(ceil_div(g.M * (partial_stride(g.N) / 8), 256));
+    if (dtype == DSP_BF16) DSP_LAUNCH(ps, dense_parts_kernel<bf16_t>, grid, dim3(256), 0, st, g.o, p.parts);
+    else DSP_LAUNCH(ps, dense_parts_kernel<float>, grid, dim3(256), 0, st, g.o, p.parts);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
+}
+
+template <typename T>
+int launch_grad(const GradArgs& a, const BackPlan& p, hipStream_t st, ProfScope& ps)
+{
+    const dim3 grid(ceil_div(a.N, p.lpr * 8), p.parts);
+    if (p.lpr == 64) DSP_LAUNCH(ps, (dense_grad_kernel<T, 64>), grid, dim3(kGradThreads), 0, st, a);
+    else DSP_LAUNCH(ps, (dense_grad_kernel<T, 8>), grid, dim3(kGradThreads), 0, st, a);
+    DSP_HIP(hipGetLastError());
+    return DSP_OK;
 }
 
 }  // namespace
@@ -737,7 +985,7 @@ int dsp_dense_workspace_bytes(const dsp_dense_desc* d, int32_t backward, size_t*
 {
     DSP_REQUIRE(bytes, DSP_EINVAL, "dsp_dense_workspace_bytes: null argument");
     DSP_TRY(check_desc(d, "dsp_dense_workspace_bytes"));
-    *bytes = backward ? back_plan(d).bytes : 0;
+    *bytes = backward ? back_plan(d).bytes : most_bytes({d->M, d->cout, d->cin, d->dtype, false, true});
     return DSP_OK;
 }
 
@@ -751,14 +999,15 @@ int dsp_dense_forward(const dsp_dense_desc* d, const void* d_x, const void* d_w,
                 "dsp_dense_forward: misaligned buffer");
     DSP_REQUIRE(d_y != d_x && d_y != d_w && d_pre != d_x && d_pre != d_w && d_pre != d_y && (!d_pre || d_pre != d_residual), DSP_EINVAL,
                 "dsp_dense_forward: y and pre want buffers of their own (y may be the residual)");
-    (void)d_workspace;
-    (void)workspace_bytes;
+    const size_t want = most_bytes({d->M, d->cout, d->cin, d->dtype, false, true});
+    DSP_REQUIRE(!want || (d_workspace && workspace_bytes >= want && on(d_workspace, 16)), DSP_EINVAL,
+                "dsp_dense_forward: workspace too small or not 16-byte aligned (%zu < %zu)", workspace_bytes, want);
     GemmArgs g{};
     g.a = d_x; g.b = d_w; g.as = stride_of(d->x_stride, d->cin); g.bs = d->cin;
     g.M = (int)d->M; g.N = d->cout; g.K = d->cin;
     g.o.out = d_y; g.o.bias = d_bias; g.o.residual = d_residual; g.o.pre = d_pre; g.o.act = d->act;
     g.o.stride = stride_of(d->y_stride, d->cout);
-    return contract<false, false>(d->dtype, "dense_fwd", g, (hipStream_t)stream);
+    return contract<false, false>(d->dtype, "dense_fwd", g, d_workspace, (hipStream_t)stream);
 }
 
 int dsp_dense_backward(const dsp_dense_desc* d, const void* d_dy, const void* d_x, const void* d_w, const void* d_pre, void* d_dx, void* d_dw,
@@ -787,30 +1036,31 @@ int dsp_dense_backward(const dsp_dense_desc* d, const void* d_dy, const void* d_
         a.dy = d_dy; a.pre = act ? d_pre : nullptr; a.g = g_read ? d_workspace : nullptr;
         a.partial = d_dbias ? (float*)((char*)d_workspace + p.g_bytes) : nullptr;
         a.ys = ys; a.gs = p.gs; a.M = (int)d->M; a.N = d->cout; a.act = d->act; a.rows_per_part = p.rows_per_part;
-        const dim3 grid(ceil_div(d->cout, kGradCols), p.parts);
         ProfScope ps("dense_grad", (double)d->M * d->cout * e * (1 + act + g_read), 1);
-        if (d->dtype == DSP_BF16) DSP_LAUNCH(ps, dense_grad_kernel<bf16_t>, grid, dim3(kGradThreads), 0, st, a);
-        else DSP_LAUNCH(ps, dense_grad_kernel<float>, grid, dim3(kGradThreads), 0, st, a);
-        DSP_HIP(hipGetLastError());
+        if (d->dtype == DSP_BF16) DSP_TRY(launch_grad<bf16_t>(a, p, st, ps));
+        else DSP_TRY(launch_grad<float>(a, p, st, ps));
         if (d_dbias) {
             ProfScope pb("dense_bias", 4.0 * p.parts * d->cout, 1);
-            DSP_LAUNCH(pb, dense_bias_kernel, dim3(ceil_div(d->cout, 256)), dim3(256), 0, st, a.partial, d_dbias, p.parts, d->cout);
+            DSP_LAUNCH(pb, dense_bias_kernel, dim3(ceil_div(d->cout, 64)), dim3(64 * kBiasWaves), 0, st, a.partial, d_dbias, p.parts, d->cout);
             DSP_HIP(hipGetLastError());
         }
     }
+    void* const rest = (char*)d_workspace + p.g_bytes + p.sums;
     if (d_dx) {
         GemmArgs g{};
+        g.padded = act;
         g.a = grad; g.as = gs; g.b = d_w; g.bs = d->cin;
         g.M = (int)d->M; g.N = d->cin; g.K = d->cout;
         g.o.out = d_dx; g.o.stride = xs;
-        DSP_TRY((contract<false, true>(d->dtype, "dense_dx", g, st)));
+        DSP_TRY((contract<false, true>(d->dtype, "dense_dx", g, rest, st)));
     }
     if (d_dw) {
         GemmArgs g{};
+        g.padded = act;
         g.a = grad; g.as = gs; g.b = d_x; g.bs = xs;
         g.M = d->cout; g.N = d->cin; g.K = (int)d->M;
         g.o.out = d_dw; g.o.stride = d->cin;
-        DSP_TRY((contract<true, true>(d->dtype, "dense_dw", g, st)));
+        DSP_TRY((contract<true, true>(d->dtype, "dense_dw", g, rest, st)));
     }
     return DSP_OK;
 }

@@ -88,7 +88,8 @@ def whole(rng, shape, most=3):
 # one row, a few, tiles that end early in every direction, tiles of every size, long sums
 SHAPES = [(1, 1, 1), (1, 64, 64), (2, 7, 3), (1, 520, 136), (5, 40, 24), (16, 256, 128), (17, 100, 33), (33, 31, 65), (64, 64, 64), (65, 129, 127),
           (100, 8, 264), (128, 128, 128), (130, 192, 136), (257, 65, 130), (300, 264, 520), (9, 2048, 72), (3, 4097, 40), (640, 72, 16),
-          (1100, 136, 264), (513, 1000, 257)]
+          (1100, 136, 264), (513, 1000, 257), (48, 2056, 40), (33, 520, 264), (64, 1001, 33), (70, 2600, 72), (66, 5000, 8), (1100, 1032, 1000), (4100, 136, 1936),
+          (2050, 2008, 1032), (1500, 77, 4099)]
 
 
 @pytest.mark.parametrize("M,K,N", SHAPES)
