@@ -456,6 +456,33 @@ __device__ inline u32x4_t load_run16(const T* p, int count, T fill)
     }
     return v;
 }
+// The same without a branch around the load, for rows of n >= 16 / sizeof(T) elements: element j on, from an address that has all sixteen bytes in
+// the row, and (ended_run16, where a run may pass the end) what is behind the end replaced.  With a branch the loads of a thread wait for
+// one another.
+template <typename T>
+__device__ inline u32x4_t inside_run16(const T* row, int64_t j, int64_t n)
+{
+    constexpr int E = 16 / sizeof(T);
+    u32x4_t v;
+    __builtin_memcpy(&v, row + (j + E <= n ? j : n - E), 16);
+    return v;
+}
+template <typename T>
+__device__ inline u32x4_t ended_run16(u32x4_t v, int64_t j, int64_t n, T fill)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (j + E <= n) return v;
+    const int s = j >= n ? E : (int)(j + E - n);  // elements that v begins too early by
+    uint32_t f;
+    if constexpr (sizeof(T) == 4) f = __builtin_bit_cast(uint32_t, fill);
+    else f = fill.bits * 0x10001u;
+    if (sizeof(T) == 2 && (s & 1)) v = u32x4_t{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16 | f << 16};
+    const int d = s * (int)sizeof(T) / 4;
+    if (d & 1) v = u32x4_t{v[1], v[2], v[3], f};
+    if (d & 2) v = u32x4_t{v[2], v[3], f, f};
+    if (d & 4) v = u32x4_t{f, f, f, f};
+    return v;
+}
 template <typename T>
 __device__ inline void store_run16(T* p, int count, u32x4_t v)
 {

@@ -326,16 +326,32 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
     constexpr int PA = A::CHUNKS / TL::THREADS, PB = B::CHUNKS / TL::THREADS;
     static_assert(PA * TL::THREADS == A::CHUNKS && PB * TL::THREADS == B::CHUNKS, "whole chunks for every thread");
     U4 ra[PA], rb[PB];
+    // Chunks are fetched from where all their bytes are in the row; where a tile passes an edge, what is behind it becomes 0 when it is kept.  (Rows behind
+    // the last one, k inside, are the last one again: they give results that nobody keeps.)
     auto load = [&](auto op, const T* p, int64_t stride, int64_t r0, int rows, int k0, auto& reg, auto count) {
         typedef decltype(op) O;
         constexpr bool MAJOR = O::K_OUTSIDE;
+        const bool tiny = (MAJOR ? rows : g.K) < O::E;
 #pragma unroll
         for (int i = 0; i < decltype(count)::value; ++i) {
             const int idx = tid + i * TL::THREADS, row = O::row_of(idx), c = idx % O::CPR * O::E;
             const int64_t r = r0 + (MAJOR ? c : row);
             const int k = k0 + (MAJOR ? row : c);
-            int left = r < rows && k < g.K ? (int)(MAJOR ? (rows - r < O::E ? rows - r : O::E) : (g.K - k < O::E ? g.K - k : O::E)) : 0;
-            reg[i] = load_run16<T>(left ? p + (MAJOR ? k * stride + r : r * stride + k) : p, left, T{});
+            const T* const line = p + (MAJOR ? (int64_t)(k < g.K ? k : g.K - 1) * stride : (r < rows ? r : rows - 1) * stride);
+            const int64_t j = MAJOR ? r : k, n = MAJOR ? rows : g.K;
+            reg[i] = tiny ? load_run16<T>(line + (j < n ? j : 0), j < n ? (int)(n - j) : 0, T{}) : inside_run16<T>(line, j, n);
+        }
+    };
+    auto end = [&](auto op, int64_t r0, int rows, int k0, auto& reg, auto count) {
+        typedef decltype(op) O;
+        constexpr bool MAJOR = O::K_OUTSIDE;
+        if (k0 + O::BK <= g.K && (!MAJOR || r0 + O::ROWB / (int)sizeof(T) <= rows)) return;
+        const bool tiny = (MAJOR ? rows : g.K) < O::E;
+#pragma unroll
+        for (int i = 0; i < decltype(count)::value; ++i) {
+            const int idx = tid + i * TL::THREADS, row = O::row_of(idx), c = idx % O::CPR * O::E;
+            if (!tiny) reg[i] = ended_run16<T>(reg[i], MAJOR ? r0 + c : k0 + c, MAJOR ? rows : g.K, T{});
+            if (MAJOR && k0 + row >= g.K) reg[i] = U4{0, 0, 0, 0};
         }
     };
     auto keep = [&](auto op, char* to, auto& reg, auto count) {
@@ -350,7 +366,9 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
         load(A{}, (const T*)g.a, g.as, m0, g.M, k0, ra, std::integral_constant<int, PA>{});
         load(B{}, (const T*)g.b, g.bs, n0, g.N, k0, rb, std::integral_constant<int, PB>{});
     };
-    auto keep_both = [&](int stage) {
+    auto keep_both = [&](int stage, int k0) {
+        end(A{}, m0, g.M, k0, ra, std::integral_constant<int, PA>{});
+        end(B{}, n0, g.N, k0, rb, std::integral_constant<int, PB>{});
         keep(A{}, smem + stage * TL::STAGE, ra, std::integral_constant<int, PA>{});
         keep(B{}, smem + stage * TL::STAGE + TL::BM * TL::KB, rb, std::integral_constant<int, PB>{});
     };
@@ -363,7 +381,7 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     const int k0 = PART ? blockIdx.y * g.part_k : 0, k1 = PART && k0 + g.part_k < g.K ? k0 + g.part_k : g.K, nk = (k1 - k0 + A::BK - 1) / A::BK;
     load_both(k0);
-    keep_both(0);
+    keep_both(0, k0);
     __syncthreads();
     for (int kt = 0; kt < nk; ++kt) {
         if (kt + 1 < nk) load_both(k0 + (kt + 1) * A::BK);
@@ -380,7 +398,7 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
 #pragma unroll
                 for (int j = 0; j < TL::TN; ++j) Mma32<T>::run(fb[j], fa[i], acc[i][j]);
         }
-        if (kt + 1 < nk) keep_both((kt + 1) & 1);
+        if (kt + 1 < nk) keep_both((kt + 1) & 1, k0 + (kt + 1) * A::BK);
         __syncthreads();
     }
     finish_tile<TL, false, 0, false, PART>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
@@ -600,17 +618,17 @@ __global__ __launch_bounds__(kGradThreads) void dense_grad_kernel(GradArgs a)
     const int c = threadIdx.x % LPR * 8, r = threadIdx.x / LPR, n = blockIdx.x * LPR * 8 + c, count = a.N - n;
     const int64_t first = (int64_t)blockIdx.y * a.rows_per_part, last = first + a.rows_per_part < a.M ? first + a.rows_per_part : a.M;
     float s[8] = {};
-    if (count > 0)
+    auto rows = [&](auto whole) {
         for (int64_t m0 = first + r; m0 < last; m0 += ROWS * kGradAhead) {
             u32x4_t d[kGradAhead][PIECES], p[kGradAhead][PIECES];
 #pragma unroll
             for (int i = 0; i < kGradAhead; ++i) {
-                const int64_t m = m0 + i * ROWS < last ? m0 + i * ROWS : m0;
+                const int64_t at = (m0 + i * ROWS < last ? m0 + i * ROWS : m0) * a.ys + n;
 #pragma unroll
                 for (int h = 0; h < PIECES; ++h) {
-                    const int left = count - h * E;
-                    d[i][h] = load_run16<T>((const T*)a.dy + m * a.ys + n + (left > 0 ? h * E : 0), left > 0 ? left : 0, T{});
-                    if (a.pre) p[i][h] = load_run16<T>((const T*)a.pre + m * a.ys + n + (left > 0 ? h * E : 0), left > 0 ? left : 0, T{});
+                    const int left = decltype(whole)::value ? E : count - h * E, to = left > 0 ? h * E : 0;
+                    d[i][h] = load_run16<T>((const T*)a.dy + at + to, left, T{});
+                    if (a.pre) p[i][h] = load_run16<T>((const T*)a.pre + at + to, left, T{});
                 }
             }
 #pragma unroll
@@ -632,6 +650,9 @@ __global__ __launch_bounds__(kGradThreads) void dense_grad_kernel(GradArgs a)
                 }
             }
         }
+    };
+    if (count >= 8) rows(std::true_type{});
+    else if (count > 0) rows(std::false_type{});
     if (!a.partial) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sums[r][c + i] = s[i];
@@ -726,22 +747,38 @@ __global__ __launch_bounds__(64 * kFewWaves) void dense_few_kernel(GemmArgs g)
     constexpr int E = 16 / sizeof(T), STEP = 4 * E, AHEAD = MT == 4 ? 2 : 4;
     __shared__ float sums[kFewWaves][MT * 16][16 + 1];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n0 = blockIdx.x * 16, r = lane % 16, ko = lane / 16 * E;
-    const bool there = n0 + r < g.N;
-    const T* const w = (const T*)g.b + (there ? (int64_t)(n0 + r) * g.bs : 0);
+    // (filters and rows behind the last are the last again: results that nobody keeps)
+    const T* const w = (const T*)g.b + (int64_t)(n0 + r < g.N ? n0 + r : g.N - 1) * g.bs;
+    const T* x[MT];
     F4 acc[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = F4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < MT; ++t) {
+        x[t] = (const T*)g.a + (int64_t)(t * 16 + r < g.M ? t * 16 + r : g.M - 1) * g.as;
+        acc[t] = F4{0.f, 0.f, 0.f, 0.f};
+    }
     for (int k0 = wave * AHEAD * STEP; k0 < g.K; k0 += kFewWaves * AHEAD * STEP) {
         U4 fw[AHEAD], fx[AHEAD][MT];
+        auto fetch = [&](auto&& run) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int k = k0 + i * STEP + ko, left = g.K - k > 0 ? g.K - k : 0;
-            fw[i] = load_run16<T>(w + (left ? k : 0), there ? left : 0, T{});
+            for (int i = 0; i < AHEAD; ++i) {
+                const int k = k0 + i * STEP + ko;
+                fw[i] = run(w, k);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                const int m = t * 16 + r;
-                fx[i][t] = load_run16<T>((const T*)g.a + (m < g.M && left ? m * g.as + k : 0), m < g.M ? left : 0, T{});
+                for (int t = 0; t < MT; ++t) fx[i][t] = run(x[t], k);
             }
+        };
+        if (g.K < E) {
+            fetch([&](const T* p, int k) { return load_run16<T>(p + (k < g.K ? k : 0), g.K > k ? g.K - k : 0, T{}); });
+        } else {
+            fetch([&](const T* p, int k) { return inside_run16<T>(p, k, g.K); });
+            if (k0 + AHEAD * STEP > g.K)
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int k = k0 + i * STEP + ko;
+                    fw[i] = ended_run16<T>(fw[i], k, g.K, T{});
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) fx[i][t] = ended_run16<T>(fx[i][t], k, g.K, T{});
+                }
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)

@@ -162,10 +162,15 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_held_kernel(Pol
     bool empty = label < 0;
     float top = -INFINITY, other = -INFINITY;
     if (!empty) {
+        if (a.V < E) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int j = (i * G::THREADS + tid) * E;
-            raw[i] = load_run16<T>(z + (j < a.V ? j : 0), a.V - j, lowest<T>());
+            for (int i = 0; i < NV; ++i) raw[i] = load_run16<T>(z, i + tid ? 0 : a.V, lowest<T>());
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) raw[i] = inside_run16<T>(z, (i * G::THREADS + tid) * E, a.V);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((i + 1) * G::THREADS * E > a.V) raw[i] = ended_run16<T>(raw[i], (i * G::THREADS + tid) * E, a.V, lowest<T>());
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -264,14 +269,17 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel
     const T* const z = (const T*)a.z + row * a.zs;
     T* const dz = a.dz ? (T*)a.dz + row * a.gs : nullptr;
     float top = -INFINITY, some = -INFINITY, sum = 0.f, dsum = 0.f;
+    auto fetch = [&](u32x4_t (&raw)[AHEAD], int64_t j0) {  // (these rows are long)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) raw[i] = inside_run16<T>(z, j0 + i * G::THREADS * E, a.V);
+        if (j0 + (AHEAD * G::THREADS - tid) * E > a.V)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) raw[i] = ended_run16<T>(raw[i], j0 + i * G::THREADS * E, a.V, lowest<T>());
+    };
     if (label >= 0)
         for (int64_t j0 = tid * E; j0 < a.V; j0 += (int64_t)AHEAD * G::THREADS * E) {
             u32x4_t raw[AHEAD];
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int64_t j = j0 + i * G::THREADS * E, left = a.V - j;
-                raw[i] = load_run16<T>(z + (left > 0 ? j : 0), left < E ? (int)(left > 0 ? left : 0) : E, lowest<T>());
-            }
+            fetch(raw, j0);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 float v[E], m = top;
@@ -318,11 +326,7 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel
     const float c0 = g.c0 * g.inv_sum, c1 = g.c1 * g.inv_sum;
     for (int64_t j0 = tid * E; j0 < a.V; j0 += (int64_t)AHEAD * G::THREADS * E) {
         u32x4_t raw[AHEAD];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int64_t j = j0 + i * G::THREADS * E, left = a.V - j;
-            raw[i] = load_run16<T>(z + (left > 0 ? j : 0), left < E ? (int)(left > 0 ? left : 0) : E, lowest<T>());
-        }
+        fetch(raw, j0);
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int64_t j = j0 + i * G::THREADS * E;
