@@ -381,14 +381,13 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a, f
         if (threadIdx.x % 64 == 0) part[k][threadIdx.x / 64] = s[k];
     }
     __syncthreads();
-    if (threadIdx.x) return;
-    double t[4];
-    for (int k = 0; k < 4; ++k) {
-        t[k] = 0.0;
-        for (int w = 0; w < kSumThreads / 64; ++w) t[k] += part[k][w];
-        loss[1 + k] = (float)t[k];
-    }
-    loss[0] = (float)(t[0] + (double)a.kl * t[1] - (double)a.ent * t[2]);
+    if (threadIdx.x >= 64) return;
+    static_assert(kSumThreads / 64 == 16, "a wave adds up four times sixteen");
+    double t = part[threadIdx.x / 16][threadIdx.x % 16];
+    for (int off = 8; off > 0; off >>= 1) t += __shfl_xor(t, off, 16);
+    const double policy = __shfl(t, 0, 64), kl = __shfl(t, 16, 64), H = __shfl(t, 32, 64);
+    if (threadIdx.x % 16 == 0) loss[1 + threadIdx.x / 16] = (float)t;
+    if (threadIdx.x == 0) loss[0] = (float)(policy + (double)a.kl * kl - (double)a.ent * H);
 }
 
 // ---- host --------------------------------------------------------------------------------------------

@@ -236,7 +236,7 @@ __device__ inline void lds_barrier()
 
 // MODE 0: the scan; 1: what each part does, for the kernel behind.
 template <typename T, bool BACK, int DECAY, bool COUPLED, int MODE>
-__global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
+__global__ __launch_bounds__(kScanThreads, BACK && MODE == 0 ? 2 : 4) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
 {
     typedef Lane4<T> L;
     constexpr int VW = L::VW, W = 32 * VW, TT = kLaneRows;
@@ -255,20 +255,23 @@ __global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanAr
     const T* const d = (const T*)p.dh + first * p.hs + c;
 
     struct Raw {
-        uint32_t x[TT], f[TT], d[TT], h[TT];
+        uint32_t f[TT], u[TT], x[TT], h[TT];  // u: x, backward dh; x and h: backward, for the gradients
     };
+    auto row_of = [&](int k) { return (int64_t)(BACK ? whole - 1 - (begin + k) : begin + k); };
     auto load = [&](int t0, Raw& r) {
 #pragma unroll
         for (int i = 0; i < TT; ++i) {
             const int k = t0 + slot * TT + i;
-            r.x[i] = r.d[i] = r.h[i] = 0u;
+            r.u[i] = r.x[i] = r.h[i] = 0u;
             r.f[i] = kNone;
             if (!in || k >= n) continue;
-            const int64_t row = BACK ? whole - 1 - (begin + k) : begin + k;
+            const int64_t row = row_of(k);
             r.f[i] = L::load(f + row * p.fs, both);
-            if (BACK) r.d[i] = L::load(d + row * p.hs, both);
-            if (!BACK || (COUPLED && MODE == 0)) r.x[i] = L::load(x + row * p.xs, both);
-            if (BACK && MODE == 0 && row > 0) r.h[i] = L::load(h + (row - 1) * p.hs, both);
+            r.u[i] = BACK ? L::load(d + row * p.hs, both) : L::load(x + row * p.xs, both);
+            if (BACK && MODE == 0) {
+                if (COUPLED) r.x[i] = L::load(x + row * p.xs, both);
+                if (row > 0) r.h[i] = L::load(h + (row - 1) * p.hs, both);
+            }
         }
     };
 
@@ -305,7 +308,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanAr
         for (int i = 0; i < TT; ++i) {
             float fv[VW], xv[VW];
             L::unpack(r.f[i], fv);
-            L::unpack(BACK ? r.d[i] : r.x[i], xv);
+            L::unpack(r.u[i], xv);
 #pragma unroll
             for (int v = 0; v < VW; ++v) {
                 float b;
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanAr
                 u[i][v] = BACK || !COUPLED ? xv[v] : b * xv[v];
                 B[v] = fmaf(A[v], b, B[v]);
                 A[v] *= a[i][v];
-                H[v] = BACK ? step_of(a[i][v], rest[i][v], H[v] + u[i][v], 0.f) : step_of(a[i][v], rest[i][v], H[v], u[i][v]);
+                H[v] = BACK ? step_of(a[i][v], rest[i][v], H[v] + xv[v], 0.f) : step_of(a[i][v], rest[i][v], H[v], u[i][v]);
             }
         }
 #pragma unroll
@@ -346,11 +349,12 @@ __global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanAr
 #pragma unroll
         for (int i = 0; i < TT; ++i) {
             const int k = t0 + slot * TT + i;
-            const int64_t row = BACK ? whole - 1 - (begin + k) : begin + k;
-            float o[VW], o2[VW], xv[VW], hv[VW];
+            const int64_t row = row_of(k);
+            float o[VW], o2[VW], xv[VW], hv[VW], dv[VW];
             if (BACK) {
                 L::unpack(r.x[i], xv);
                 L::unpack(r.h[i], hv);
+                L::unpack(r.u[i], dv);
             }
 #pragma unroll
             for (int v = 0; v < VW; ++v) {
@@ -358,7 +362,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void recurrence_scan_kernel(ScanAr
                     st[v] = step_of(a[i][v], rest[i][v], st[v], u[i][v]);
                     o[v] = st[v];
                 } else {
-                    const float g = u[i][v] + st[v], b = (1.f - a[i][v]) - rest[i][v], hp = row == 0 ? before[v] : hv[v];
+                    const float g = dv[v] + st[v], b = (1.f - a[i][v]) - rest[i][v], hp = row == 0 ? before[v] : hv[v];
                     st[v] = step_of(a[i][v], rest[i][v], g, 0.f);
                     o[v] = COUPLED ? b * g : g;
                     o2[v] = (DECAY == DSP_DECAY_SIGMOID ? a[i][v] * b : a[i][v]) * g * (COUPLED ? hp - xv[v] : hp);
@@ -425,7 +429,7 @@ Plan plan_of(const dsp_recurrence_desc* d)
     p.walk = d->steps <= 32 || (int64_t)d->sequences * strips >= 8192;
     if (p.walk) return p;
     const int64_t groups = (int64_t)strips * d->sequences;
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->steps, 4 * kTileRows), groups >= 192 ? 1 : 256 / groups));
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->steps, 4 * kTileRows), groups >= 192 ? 1 : 512 / groups));
     p.part_rows = ceil_div(ceil_div(d->steps, want), kTileRows) * kTileRows;
     p.parts = ceil_div(d->steps, p.part_rows);
     if (p.parts > 1) {
