@@ -206,14 +206,14 @@ __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_back_kernel(Scan
 
 // ---- long sequences: a workgroup scans a strip of channels tile by tile ---------------------------------
 //
-// A tile is kTileRows rows of 128 bytes.  A lane has the four bytes of kLaneRows consecutive rows, half a wave a row's 128 bytes: a slot.  (1) Every
+// A tile is 2 WAVES kLaneRows rows of 128 bytes.  A lane has the four bytes of kLaneRows consecutive rows, half a wave a row's 128 bytes: a slot.  (1) Every
 // slot finds what its rows do to a state, h -> A h + H, from h = 0; (2) the first wave goes through the slots with the state and leaves in
 // LDS what each one starts from; (3) every slot goes through its rows once more, which it still has in registers.  Backward the same from
 // the last row on, with r = a g in the place of h.  Rows behind the end are steps that change nothing (a = 1, u = 0).
 //
 // A sequence with too few strips to fill the card is cut into parts, whose A and H a first kernel finds (it reads the inputs of the scan once
 // more: what comes back is all compute units).
-constexpr int kLaneRows = 8, kWaves = 8, kSlots = 2 * kWaves, kTileRows = kSlots * kLaneRows, kScanThreads = 64 * kWaves;
+constexpr int kLaneRows = 4;
 
 struct PartArgs {
     float* sums;      // [sequences][parts - 1][3][C]: a, c, H of each part but the last
@@ -222,9 +222,9 @@ struct PartArgs {
 };
 
 // LDS of a workgroup: what the slots do, and what they start from.
-template <int W>
+template <int SLOTS, int W>
 struct Slots {
-    float a[kSlots][W], c[kSlots][W], h[kSlots][W], in[kSlots][W];
+    float a[SLOTS][W], c[SLOTS][W], h[SLOTS][W], in[SLOTS][W];
 };
 
 __device__ inline void lds_barrier()
@@ -235,13 +235,13 @@ __device__ inline void lds_barrier()
 }
 
 // MODE 0: the scan; 1: what each part does, for the kernel behind.
-template <typename T, bool BACK, int DECAY, bool COUPLED, int MODE>
-__global__ __launch_bounds__(kScanThreads, BACK && MODE == 0 ? 2 : 4) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
+template <typename T, int WAVES, bool BACK, int DECAY, bool COUPLED, int MODE>
+__global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
 {
     typedef Lane4<T> L;
-    constexpr int VW = L::VW, W = 32 * VW, TT = kLaneRows;
+    constexpr int VW = L::VW, W = 32 * VW, TT = kLaneRows, SLOTS = 2 * WAVES, TILE = SLOTS * TT;
     constexpr uint32_t kNone = DECAY == DSP_DECAY_SIGMOID ? L::kInfinity : 0u;  // the f of a = 1
-    __shared__ Slots<W> lds;
+    __shared__ Slots<SLOTS, W> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = wave * 2 + lane / 32;
     const int s = blockIdx.y, part = blockIdx.z, c = blockIdx.x * W + lane % 32 * VW;
     const bool in = c < p.C, both = c + VW <= p.C;
@@ -298,9 +298,9 @@ __global__ __launch_bounds__(kScanThreads, BACK && MODE == 0 ? 2 : 4) void recur
 
     Raw next;
     if (n > 0) load(0, next);
-    for (int t0 = 0; t0 < n; t0 += kTileRows) {
+    for (int t0 = 0; t0 < n; t0 += TILE) {
         const Raw r = next;
-        if (t0 + kTileRows < n) load(t0 + kTileRows, next);
+        if (t0 + TILE < n) load(t0 + TILE, next);
         float a[TT][VW], rest[TT][VW], u[TT][VW], A[VW], B[VW], H[VW];
 #pragma unroll
         for (int v = 0; v < VW; ++v) A[v] = 1.f, B[v] = H[v] = 0.f;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kScanThreads, BACK && MODE == 0 ? 2 : 4) void recur
         lds_barrier();
         if (wave == 0 && lane < W) {
 #pragma unroll 4
-            for (int j = 0; j < kSlots; ++j) {
+            for (int j = 0; j < SLOTS; ++j) {
                 const float ja = lds.a[j][lane], jc = lds.c[j][lane], jh = lds.h[j][lane];
                 lds.in[j][lane] = carry;
                 carry = step_of(ja, jc, carry, jh);
@@ -417,7 +417,7 @@ ScanArgs args_of(const dsp_recurrence_desc* d)
 // Who does it, and how a sequence is cut.
 struct Plan {
     bool walk;
-    int parts, part_rows;
+    int waves, parts, part_rows;
     size_t sums, bytes;
 };
 Plan plan_of(const dsp_recurrence_desc* d)
@@ -429,9 +429,11 @@ Plan plan_of(const dsp_recurrence_desc* d)
     p.walk = d->steps <= 32 || (int64_t)d->sequences * strips >= 8192;
     if (p.walk) return p;
     const int64_t groups = (int64_t)strips * d->sequences;
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->steps, 4 * kTileRows), groups >= 192 ? 1 : 512 / groups));
-    p.part_rows = ceil_div(ceil_div(d->steps, want), kTileRows) * kTileRows;
+    constexpr int kTile = 2 * 8 * kLaneRows;
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->steps, 8 * kTile), groups >= 192 ? 1 : 512 / groups));
+    p.part_rows = ceil_div(ceil_div(d->steps, want), 2 * kTile) * 2 * kTile;
     p.parts = ceil_div(d->steps, p.part_rows);
+    p.waves = groups * p.parts >= 384 ? 8 : 16;
     if (p.parts > 1) {
         p.sums = (size_t)d->sequences * (p.parts - 1) * 3 * d->C * sizeof(float);
         p.bytes = (p.sums + (size_t)d->sequences * d->C * sizeof(float) + 15) / 16 * 16;
@@ -439,19 +441,24 @@ Plan plan_of(const dsp_recurrence_desc* d)
     return p;
 }
 
-template <typename T, bool BACK, int DECAY, bool COUPLED>
-int scan(const ScanArgs& a, const PartArgs& q, hipStream_t st, const char* name, double bytes)
+template <typename T, int WAVES, bool BACK, int DECAY, bool COUPLED>
+int scan_by(const ScanArgs& a, const PartArgs& q, hipStream_t st, const char* name, double bytes)
 {
-    const dim3 grid(ceil_div(a.C, 32 * Lane4<T>::VW), a.sequences, q.parts);
+    const dim3 grid(ceil_div(a.C, 32 * Lane4<T>::VW), a.sequences, q.parts), block(64 * WAVES);
     if (q.parts > 1) {
         ProfScope ps("recurrence_parts", bytes * 2 / (BACK ? 6 : 3), 1);
-        DSP_LAUNCH(ps, (recurrence_scan_kernel<T, BACK, DECAY, COUPLED, 1>), dim3(grid.x, grid.y, grid.z - 1), dim3(kScanThreads), 0, st, a, q);
+        DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, 1>), dim3(grid.x, grid.y, grid.z - 1), block, 0, st, a, q);
         DSP_HIP(hipGetLastError());
     }
     ProfScope ps(name, bytes, 1);
-    DSP_LAUNCH(ps, (recurrence_scan_kernel<T, BACK, DECAY, COUPLED, 0>), grid, dim3(kScanThreads), 0, st, a, q);
+    DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, 0>), grid, block, 0, st, a, q);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
+}
+template <typename T, bool BACK, int DECAY, bool COUPLED>
+int scan(const ScanArgs& a, const PartArgs& q, int waves, hipStream_t st, const char* name, double bytes)
+{
+    return waves == 16 ? scan_by<T, 16, BACK, DECAY, COUPLED>(a, q, st, name, bytes) : scan_by<T, 8, BACK, DECAY, COUPLED>(a, q, st, name, bytes);
 }
 
 template <typename T, bool BACK>
@@ -474,8 +481,8 @@ int run(const dsp_recurrence_desc* d, const ScanArgs& a, void* workspace, hipStr
     q.parts = p.parts;
     q.part_rows = p.part_rows;
     if (d->decay == DSP_DECAY_SIGMOID)
-        return d->coupled ? scan<T, BACK, DSP_DECAY_SIGMOID, true>(a, q, st, name, bytes) : scan<T, BACK, DSP_DECAY_SIGMOID, false>(a, q, st, name, bytes);
-    return d->coupled ? scan<T, BACK, DSP_DECAY_EXP, true>(a, q, st, name, bytes) : scan<T, BACK, DSP_DECAY_EXP, false>(a, q, st, name, bytes);
+        return d->coupled ? scan<T, BACK, DSP_DECAY_SIGMOID, true>(a, q, p.waves, st, name, bytes) : scan<T, BACK, DSP_DECAY_SIGMOID, false>(a, q, p.waves, st, name, bytes);
+    return d->coupled ? scan<T, BACK, DSP_DECAY_EXP, true>(a, q, p.waves, st, name, bytes) : scan<T, BACK, DSP_DECAY_EXP, false>(a, q, p.waves, st, name, bytes);
 }
 
 }  // namespace
