@@ -514,6 +514,14 @@ __device__ inline u32x4_t pack_run16(const float (&v)[16 / sizeof(T)])
     return r;
 }
 
+// A workgroup's barrier for what is in LDS; loads on their way to registers go on.
+__device__ inline void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // exp(-a) for a >= 0 (or NaN) from the hardware's power of two, within one unit of its last place.  The exponent's product is rounded,
 // which alone would cost a 2^-24 of the result: what hi ln(2), with ln(2) in two parts, lacks of -a is a factor 1 + off.  Relative error
 // 3 * 2^-24; 0 below 2^-126.  (Where a is infinite off is no number, and the bound makes it one; p is NaN only where a is.)

@@ -325,7 +325,10 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
     const int n0 = (int)(tile % g.tiles_n) * TL::BN;
     constexpr int PA = A::CHUNKS / TL::THREADS, PB = B::CHUNKS / TL::THREADS;
     static_assert(PA * TL::THREADS == A::CHUNKS && PB * TL::THREADS == B::CHUNKS, "whole chunks for every thread");
-    U4 ra[PA], rb[PB];
+    // DEPTH tiles are on their way to registers.  (us with 2 and 1: 64 x 64 tiles, the odd fp32 backward 171, 175; 128 x 128, where two cost half of the waves, 2048 x 2048 x
+    // 2048 fp32 176, 160.)
+    constexpr int DEPTH = TL::BM == 64 ? 2 : 1;
+    U4 ra[DEPTH][PA], rb[DEPTH][PB];
     // Chunks are fetched from where all their bytes are in the row; where a tile passes an edge, what is behind it becomes 0 when it is kept.  (Rows behind
     // the last one, k inside, are the last one again: they give results that nobody keeps.)
     auto load = [&](auto op, const T* p, int64_t stride, int64_t r0, int rows, int k0, auto& reg, auto count) {
@@ -362,15 +365,17 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
             *(U4*)(to + O::place(O::row_of(idx), idx % O::CPR)) = reg[i];
         }
     };
-    auto load_both = [&](int k0) {
-        load(A{}, (const T*)g.a, g.as, m0, g.M, k0, ra, std::integral_constant<int, PA>{});
-        load(B{}, (const T*)g.b, g.bs, n0, g.N, k0, rb, std::integral_constant<int, PB>{});
+    auto load_both = [&](auto which, int k0) {
+        constexpr int S = decltype(which)::value % DEPTH;
+        load(A{}, (const T*)g.a, g.as, m0, g.M, k0, ra[S], std::integral_constant<int, PA>{});
+        load(B{}, (const T*)g.b, g.bs, n0, g.N, k0, rb[S], std::integral_constant<int, PB>{});
     };
-    auto keep_both = [&](int stage, int k0) {
-        end(A{}, m0, g.M, k0, ra, std::integral_constant<int, PA>{});
-        end(B{}, n0, g.N, k0, rb, std::integral_constant<int, PB>{});
-        keep(A{}, smem + stage * TL::STAGE, ra, std::integral_constant<int, PA>{});
-        keep(B{}, smem + stage * TL::STAGE + TL::BM * TL::KB, rb, std::integral_constant<int, PB>{});
+    auto keep_both = [&](auto which, int stage, int k0) {
+        constexpr int D = decltype(which)::value % DEPTH;
+        end(A{}, m0, g.M, k0, ra[D], std::integral_constant<int, PA>{});
+        end(B{}, n0, g.N, k0, rb[D], std::integral_constant<int, PB>{});
+        keep(A{}, smem + stage * TL::STAGE, ra[D], std::integral_constant<int, PA>{});
+        keep(B{}, smem + stage * TL::STAGE + TL::BM * TL::KB, rb[D], std::integral_constant<int, PB>{});
     };
     F16 acc[TL::TM][TL::TN];
 #pragma unroll
@@ -380,12 +385,13 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     const int k0 = PART ? blockIdx.y * g.part_k : 0, k1 = PART && k0 + g.part_k < g.K ? k0 + g.part_k : g.K, nk = (k1 - k0 + A::BK - 1) / A::BK;
-    load_both(k0);
-    keep_both(0, k0);
-    __syncthreads();
-    for (int kt = 0; kt < nk; ++kt) {
-        if (kt + 1 < nk) load_both(k0 + (kt + 1) * A::BK);
-        const char* s = smem + (kt & 1) * TL::STAGE;
+    typedef std::integral_constant<int, 0> Even;
+    typedef std::integral_constant<int, 1> Odd;
+    load_both(Even{}, k0);
+    if (DEPTH > 1 && nk > 1) load_both(Odd{}, k0 + A::BK);
+    keep_both(Even{}, 0, k0);
+    lds_barrier();
+    auto multiply = [&](const char* s) {
 #pragma unroll
         for (int ks = 0; ks < TL::NKS; ++ks) {
             U4 fa[TL::TM], fb[TL::TN];
@@ -398,8 +404,25 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
 #pragma unroll
                 for (int j = 0; j < TL::TN; ++j) Mma32<T>::run(fb[j], fa[i], acc[i][j]);
         }
-        if (kt + 1 < nk) keep_both((kt + 1) & 1, k0 + (kt + 1) * A::BK);
-        __syncthreads();
+    };
+    if constexpr (DEPTH == 1) {
+        for (int kt = 0; kt < nk; ++kt) {
+            if (kt + 1 < nk) load_both(Even{}, k0 + (kt + 1) * A::BK);
+            multiply(smem + (kt & 1) * TL::STAGE);
+            if (kt + 1 < nk) keep_both(Even{}, (kt + 1) & 1, k0 + (kt + 1) * A::BK);
+            lds_barrier();
+        }
+    } else {
+        auto tile_of = [&](auto mine, auto other, int kt) {
+            if (kt + 2 < nk) load_both(mine, k0 + (kt + 2) * A::BK);
+            multiply(smem + decltype(mine)::value * TL::STAGE);
+            if (kt + 1 < nk) keep_both(other, decltype(other)::value, k0 + (kt + 1) * A::BK);
+            lds_barrier();
+        };
+        for (int kt = 0; kt < nk; kt += 2) {
+            tile_of(Even{}, Odd{}, kt);
+            if (kt + 1 < nk) tile_of(Odd{}, Even{}, kt + 1);
+        }
     }
     finish_tile<TL, false, 0, false, PART>(smem, acc, g.o, m0 + wm * TL::TM * 32, n0 + wn * TL::TN * 32, wave, lane);
 }
@@ -414,10 +437,11 @@ struct DirectTile {
     typedef bf16_t T;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, ST = ST_;
     static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES, TM = BM / (32 * WM), TN = BN / (32 * WN), NKS = KB / 32;
-    typedef OperandTile<T, AM_, BM, KB> A;
+    static constexpr int RA = BM == 192 ? 256 : BM;  // (rows of A that are fetched, so that every wave has whole loads: of 256 the last 64 are not used)
+    typedef OperandTile<T, AM_, RA, KB> A;
     typedef OperandTile<T, BMJ_, BN, KB> B;
-    static constexpr int BK = KB / 2, STAGE = (BM + BN) * KB, LA = BM * KB / 1024 / WAVES, LB = BN * KB / 1024 / WAVES, LOADS = LA + LB;
-    static_assert(LA * 1024 * WAVES == BM * KB && LB * 1024 * WAVES == BN * KB, "whole loads for every wave");
+    static constexpr int BK = KB / 2, STAGE = (RA + BN) * KB, LA = RA * KB / 1024 / WAVES, LB = BN * KB / 1024 / WAVES, LOADS = LA + LB;
+    static_assert(LA * 1024 * WAVES == RA * KB && LB * 1024 * WAVES == BN * KB, "whole loads for every wave");
     static constexpr int OUT_ROW = TN * 32 + 4, OUT = WAVES * 32 * OUT_ROW * 4;
     static constexpr int LDS = ST * STAGE > OUT ? ST * STAGE : OUT;
     static_assert(ST >= 3 && LDS <= 160 * 1024, "a ring of three stages");
@@ -519,7 +543,7 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
     auto issue = [&](int stage, auto i) {
         constexpr int I = decltype(i)::value;
         if constexpr (I < LA) la.template issue<I>(ring + stage * TL::STAGE, k_left, wave);
-        else lb.template issue<I - LA>(ring + stage * TL::STAGE + TL::BM * TL::KB, k_left, wave);
+        else lb.template issue<I - LA>(ring + stage * TL::STAGE + TL::RA * TL::KB, k_left, wave);
     };
     auto next = [&]() {
         k_left -= TL::BK;
@@ -537,7 +561,7 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
 #pragma unroll
         for (int i = 0; i < TM; ++i) a[i] = A::fragment(s, wm * TM + i, ks, lane);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = B::fragment(s + TL::BM * TL::KB, wn * TN + j, ks, lane);
+        for (int j = 0; j < TN; ++j) b[j] = B::fragment(s + TL::RA * TL::KB, wn * TN + j, ks, lane);
     };
     // The products of a k step.  Between them go out the reads of the next step's operands, one behind each from the first on, and loads [F, L) of the
     // next tile: what takes the wave's time to issue the matrix unit has for itself, and it has products at once behind a barrier.
@@ -552,7 +576,7 @@ __global__ __launch_bounds__(TL::THREADS) __attribute__((amdgpu_waves_per_eu(TL:
             constexpr int R0 = (TM + TN) * Q / N, R1 = (TM + TN) * (Q + 1) / N, L0 = F + (L - F) * Q / N, L1 = F + (L - F) * (Q + 1) / N;
             unrolled<R1 - R0>([&](auto r) {
                 constexpr int I = R0 + decltype(r)::value;
-                if constexpr (I < TN) nb[I] = B::fragment(from + TL::BM * TL::KB, wn * TN + I, KS, lane);
+                if constexpr (I < TN) nb[I] = B::fragment(from + TL::RA * TL::KB, wn * TN + I, KS, lane);
                 else na[I - TN] = A::fragment(from, wm * TM + I - TN, KS, lane);
             });
             unrolled<L1 - L0>([&](auto r) { issue(stage, std::integral_constant<int, L0 + decltype(r)::value>{}); });
@@ -833,7 +857,7 @@ bool on(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
 
 size_t rounded16(size_t n) { return (n + 15) / 16 * 16; }
 
-enum Kernel { kFew, kDirect256, kDirect128, kStaged128, kStaged64 };
+enum Kernel { kFew, kDirect256, kDirect192, kDirect128, kStaged128, kStaged64 };
 
 // Who forms a contraction, and into how many parts its k is cut.
 struct ContractPlan {
@@ -856,13 +880,18 @@ ContractPlan contract_plan(const Shape& s)
         return p;
     }
     auto tiles = [&](int t) { return (int64_t)ceil_div(s.M, t) * ceil_div(s.N, t); };
-    int64_t n;
-    if (s.direct && tiles(256) >= 128) p.kernel = kDirect256, n = tiles(256);
-    else if (s.direct && tiles(128) >= 64) p.kernel = kDirect128, n = tiles(128);
-    else if (tiles(128) >= 256) p.kernel = kStaged128, n = tiles(128);
-    else p.kernel = kStaged64, n = tiles(64);
-    // few tiles and a long k: parts, of 512 elements at least, until there are two workgroups for a compute unit
-    const int64_t want = p.kernel == kDirect256 ? 1 : std::min<int64_t>(512 / n, s.K / 512);
+    int64_t n = tiles(256), want = std::max<int64_t>(1, std::min<int64_t>(256 / n, s.K / 2048));
+    if (s.direct && n * want >= 128) {
+        // a workgroup has a compute unit to itself: rounds of 256 tiles, of 256 or 192 rows, whichever are done first
+        const int64_t low = (int64_t)ceil_div(s.M, 192) * ceil_div(s.N, 256);
+        p.kernel = want > 1 || ceil_div(n, 256) * 256 <= ceil_div(low, 256) * 200 ? kDirect256 : kDirect192;
+    } else {
+        n = tiles(128);
+        p.kernel = s.direct && n >= 64 ? kDirect128 : n >= 256 ? kStaged128 : kStaged64;
+        if (p.kernel == kStaged64) n = tiles(64);
+        want = std::min<int64_t>((p.kernel == kStaged64 ? 1024 : 512) / n, s.K / 512);
+    }
+    // few tiles and a long k: parts, until there is a workgroup for a compute unit, two of the 128 x 128 tiles and four of the 64 x 64
     if (want > 1) {
         p.part_k = ceil_div(ceil_div(s.K, want), 64) * 64;
         p.parts = ceil_div(s.K, p.part_k);
@@ -904,7 +933,7 @@ BackPlan back_plan(const dsp_dense_desc* d)
 template <typename T, bool AM, bool BMJ, int TILE>
 int launch_staged(GemmArgs& g, hipStream_t st, ProfScope& ps)
 {
-    typedef StagedTile<T, AM, BMJ, TILE, TILE, 2, 2, 64> TL;
+    typedef StagedTile<T, AM, BMJ, TILE, TILE, 2, 2, TILE == 64 ? 128 : 64> TL;
     g.tiles_m = ceil_div(g.M, TL::BM);
     g.tiles_n = ceil_div(g.N, TL::BN);
     const dim3 grid((unsigned)g.tiles_m * g.tiles_n, g.parts);
@@ -933,14 +962,18 @@ int launch_direct(GemmArgs& g, hipStream_t st, ProfScope& ps)
 template <typename TL>
 int with_act(GemmArgs& g, hipStream_t st, ProfScope& ps)
 {
-    if (g.parts > 1) return launch_direct<TL, DSP_ACT_IDENTITY, false, true>(g, st, ps);
-    if constexpr (TL::A::K_OUTSIDE || TL::B::K_OUTSIDE) return launch_direct<TL>(g, st, ps);
-    const bool res = g.o.residual != nullptr;
-    switch (g.o.act) {
-    case DSP_ACT_RELU: return res ? launch_direct<TL, DSP_ACT_RELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_RELU, false>(g, st, ps);
-    case DSP_ACT_GELU: return res ? launch_direct<TL, DSP_ACT_GELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_GELU, false>(g, st, ps);
-    case DSP_ACT_SILU: return res ? launch_direct<TL, DSP_ACT_SILU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_SILU, false>(g, st, ps);
-    default: return res ? launch_direct<TL, DSP_ACT_IDENTITY, true>(g, st, ps) : launch_direct<TL, DSP_ACT_IDENTITY, false>(g, st, ps);
+    if constexpr (TL::BM != 192)
+        if (g.parts > 1) return launch_direct<TL, DSP_ACT_IDENTITY, false, true>(g, st, ps);
+    if constexpr (TL::A::K_OUTSIDE || TL::B::K_OUTSIDE) {
+        return launch_direct<TL>(g, st, ps);
+    } else {
+        const bool res = g.o.residual != nullptr;
+        switch (g.o.act) {
+        case DSP_ACT_RELU: return res ? launch_direct<TL, DSP_ACT_RELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_RELU, false>(g, st, ps);
+        case DSP_ACT_GELU: return res ? launch_direct<TL, DSP_ACT_GELU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_GELU, false>(g, st, ps);
+        case DSP_ACT_SILU: return res ? launch_direct<TL, DSP_ACT_SILU, true>(g, st, ps) : launch_direct<TL, DSP_ACT_SILU, false>(g, st, ps);
+        default: return res ? launch_direct<TL, DSP_ACT_IDENTITY, true>(g, st, ps) : launch_direct<TL, DSP_ACT_IDENTITY, false>(g, st, ps);
+        }
     }
 }
 
@@ -971,6 +1004,7 @@ int contract_t(const ContractPlan& p, GemmArgs& g, hipStream_t st, ProfScope& ps
         if (p.kernel == kFew) return launch_few<T>(g, st, ps);
     if constexpr (sizeof(T) == 2) {
         if (p.kernel == kDirect256) return with_act<DirectTile<AM, BMJ, 256, 256, 2, 4, 64, 4>>(g, st, ps);
+        if (p.kernel == kDirect192) return with_act<DirectTile<AM, BMJ, 192, 256, 2, 4, 64, 4>>(g, st, ps);
         if (p.kernel == kDirect128) return with_act<DirectTile<AM, BMJ, 128, 128, 2, 2, 64, 4>>(g, st, ps);
     }
     return p.kernel == kStaged128 ? launch_staged<T, AM, BMJ, 128>(g, st, ps) : launch_staged<T, AM, BMJ, 64>(g, st, ps);

@@ -227,13 +227,6 @@ struct Slots {
     float a[SLOTS][W], c[SLOTS][W], h[SLOTS][W], in[SLOTS][W];
 };
 
-__device__ inline void lds_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (loads on their way to registers go on)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // MODE 0: the scan; 1: what each part does, for the kernel behind.
 template <typename T, int WAVES, bool BACK, int DECAY, bool COUPLED, int MODE>
 __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
