@@ -31,6 +31,10 @@ def test_dense_refuses(dtype):
                  {"ws": None}, {"ws": 8 * A + 8}, {"n": D.dsp_dense_workspace_bytes(d, True) - 1}, {"dx": A}, {"dx": 2 * A}, {"dx": 3 * A}, {"dw": A}, {"dw": 3 * A},
                  {"dw": 5 * A}, {"dx": 4 * A}):
         refused(lambda: bwd(d, **over))
+    cut = D.make_dense_desc(100, 8192, 64, dtype)  # few tiles, a long sum: cut into parts
+    assert D.dsp_dense_workspace_bytes(cut) > 0 and D.dsp_dense_workspace_bytes(D.make_dense_desc(1, 8192, 64, dtype)) == 0
+    refused(lambda: D.dsp_dense_forward(cut, A, 2 * A, None, None, 3 * A, None, None, 0, stream=0), "workspace")
+    refused(lambda: D.dsp_dense_forward(cut, A, 2 * A, None, None, 3 * A, None, 8 * A, D.dsp_dense_workspace_bytes(cut) - 1, stream=0), "workspace")
     refused(lambda: D.check(D.lib().dsp_dense_forward(None, *[None] * 7, 0, None), "null"), "null descriptor")
     refused(lambda: D.check(D.lib().dsp_dense_workspace_bytes(None, 0, None), "null"))
 
@@ -51,6 +55,10 @@ def test_recurrence_refuses(dtype):
     d = D.make_recurrence_desc(**{**good, "rows": 14999})
     refused(lambda: fwd(d), "fewer rows"), refused(lambda: bwd(d), "fewer rows")
     d = D.make_recurrence_desc(**good)
+    want = D.dsp_recurrence_workspace_bytes(d)
+    assert want > 0 and D.dsp_recurrence_workspace_bytes(D.make_recurrence_desc(9, 1, 9, 64, dtype)) == 0
+    for bad in ({"ws": None}, {"ws": 8 * A + 8}, {"n": want - 1}):
+        refused(lambda: fwd(d, **bad), "workspace"), refused(lambda: bwd(d, **bad), "workspace")
     for over in ({"x": None}, {"f": None}, {"h": None}, {"x": A + 1}, {"f": A + 1}, {"h": A + 1}, {"o": A + 2}, {"s": A + 2}, {"t": A + 2}, {"h": A}, {"h": 2 * A}):
         refused(lambda: fwd(d, **over))
     for over in ({"dh": None}, {"x": None}, {"f": None}, {"h": None}, {"dx": None, "df": None}, {"dh": A + 1}, {"dx": A + 1}, {"df": A + 1}, {"ds": A + 2},

@@ -89,7 +89,7 @@ def whole(rng, shape, most=3):
 SHAPES = [(1, 1, 1), (1, 64, 64), (2, 7, 3), (1, 520, 136), (5, 40, 24), (16, 256, 128), (17, 100, 33), (33, 31, 65), (64, 64, 64), (65, 129, 127),
           (100, 8, 264), (128, 128, 128), (130, 192, 136), (257, 65, 130), (300, 264, 520), (9, 2048, 72), (3, 4097, 40), (640, 72, 16),
           (1100, 136, 264), (513, 1000, 257), (48, 2056, 40), (33, 520, 264), (64, 1001, 33), (70, 2600, 72), (66, 5000, 8), (1100, 1032, 1000), (4100, 136, 1936),
-          (2050, 2008, 1032), (1500, 77, 4099)]
+          (2050, 2008, 1032), (1500, 77, 4099), (2050, 1000, 1003), (4100, 1000, 4104), (6000, 72, 2048)]
 
 
 @pytest.mark.parametrize("M,K,N", SHAPES)
@@ -272,7 +272,29 @@ def test_rows_far_apart(dtype):
     assert np.array_equal(gw.float().cpu().numpy(), rounded(dy.T @ x, td))
 
 
-@pytest.mark.parametrize("M,K,N", [(1, 2048, 520), (300, 264, 520), (1100, 512, 256), (600, 100, 77)])
+def test_tiles_beyond_32_bits():
+    """Tiles of bf16 rows of which the last lie more than 2^32 bytes behind the first, in every operand and output."""
+    code, td, _ = TYPES["bf16"]
+    M, K, N, stride = 1100, 1032, 1040, 2000000
+    rng = np.random.default_rng(6)
+    x, w, dy = whole(rng, (M, K)), whole(rng, (N, K)), whole(rng, (M, N))
+    big = [torch.empty((M - 1) * stride + 1048, dtype=td, device="cuda") for _ in range(2)]
+    xs, ys = big[0].as_strided((M, K), (stride, 1)), big[1].as_strided((M, N), (stride, 1))
+    dw = torch.from_numpy(w).cuda().to(td)
+    xs.copy_(torch.from_numpy(x).cuda().to(td))
+    desc = D.make_dense_desc(M, K, N, code, 0, stride, stride)
+    ws, n = workspace(desc, False)
+    D.dsp_dense_forward(desc, xs, dw, None, None, ys, None, ws, n)
+    assert np.array_equal(ys.float().cpu().numpy(), rounded(x @ w.T, td))
+    ys.copy_(torch.from_numpy(dy).cuda().to(td))
+    ws, n = workspace(desc, True)
+    gw, gx = torch.empty(N, K, dtype=td, device="cuda"), torch.empty((M - 1) * stride + 1048, dtype=td, device="cuda").as_strided((M, K), (stride, 1))
+    D.dsp_dense_backward(desc, ys, xs, dw, None, gx, gw, None, ws, n)
+    assert np.array_equal(gx.float().cpu().numpy(), rounded(dy @ w, td))
+    assert np.array_equal(gw.float().cpu().numpy(), rounded(dy.T @ x, td))
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 2048, 520), (300, 264, 520), (1100, 512, 256), (600, 100, 77), (300, 2600, 72), (1100, 1032, 1000)])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_streams_graphs_and_repetition(dtype, M, K, N):
     """The same bits on another stream, twice, and from a captured graph replayed with eager calls in between."""
