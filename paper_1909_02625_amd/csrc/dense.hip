@@ -122,7 +122,7 @@ __device__ inline void store8(T* p, const float (&v)[8])
         float t[VW];
 #pragma unroll
         for (int i = 0; i < VW; ++i) t[i] = v[h * VW + i];
-        ((u32x4_t*)p)[h] = pack_run16<T>(t);
+        __builtin_nontemporal_store(pack_run16<T>(t), (u32x4_t*)p + h);
     }
 }
 // Results m, n .. of which `count` are within the row, one by one.
