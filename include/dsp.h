@@ -677,9 +677,10 @@ int dsp_recurrence_backward(const dsp_recurrence_desc* desc, const void* d_dh, c
  *     policy = max(-A rho, -A min(max(rho, 1 - clip_low), 1 + clip_high)),  kl = exp(ref - lp) - (ref - lp) - 1
  *     L = sum over the rows of weight (policy + kl_coef kl - entropy_coef H)
  * dsp_token_logprob gives lp and H (the old and the reference model's, say; the clip range and the coefficients are not looked at).
- * dsp_policy_loss gives L and, reading every logit once, its gradient.  A row with a negative label (a prompt, padding) has no part in L: its
- * lp, terms and gradient are 0, and so are those of a row whose logits are all -infinity.  A logit of -infinity has probability 0.  A label of
- * vocab or more indexes nothing: its row's results are NaN, as are those of a row that holds NaN or +infinity.
+ * dsp_policy_loss gives L and its gradient, reading every logit once (twice in rows of more than 64 KiB).  A row with a negative
+ * label (a prompt, padding) has no part in L: its lp, terms and gradient are 0, and so are those of a row whose logits are all
+ * -infinity.  A logit of -infinity has probability 0.  A label of vocab or more indexes nothing: its row's results are NaN, as
+ * are those of a row that holds NaN or +infinity.
  */
 typedef struct dsp_policy_loss_desc {
     int32_t rows, vocab;

@@ -4,6 +4,11 @@
 //
 // All three products are one contraction C[m][n] = sum_k A(m, k) B(n, k), whose operands lie with k or with their row as the
 // fast index.  Both go into LDS as they lie in memory.
+//
+// The matrix unit bounds large ones: bf16 on 256 x 256 tiles 1334 TFLOP/s inside a tile (8192 x 4096 rows with k from 4096 to 8192), 1260 with k = 8192,
+// 1190 with 4096 (the libraries' product of 8192^3 1369); a tile's beginning and end have its compute unit to themselves.  8192 x 2048 -> 5632 with bias,
+// gelu and both outputs takes 195 us (970 TFLOP/s, three rounds of 256 tiles of which the last is three quarters full), its backward pass 370.
+// fp32: 127 TFLOP/s at 4096^3 of 153.  One row reads its filters in 8.3 us (2.8 TB/s, the launch included).
 #include "common.h"
 
 #include <algorithm>
@@ -122,6 +127,7 @@ __device__ inline void store8(T* p, const float (&v)[8])
         float t[VW];
 #pragma unroll
         for (int i = 0; i < VW; ++i) t[i] = v[h * VW + i];
+        // (marked as streamed: 8192 x 2048 -> 5632 with two outputs 213 -> 195 us, 4096 x 2048 -> 32000 497 -> 470)
         __builtin_nontemporal_store(pack_run16<T>(t), (u32x4_t*)p + h);
     }
 }
@@ -431,7 +437,9 @@ __global__ __launch_bounds__(TL::THREADS) void dense_staged_kernel(GemmArgs g)
 //
 // ST stages of a ring hold KB bytes of k each.  Tiles kt .. kt + ST - 2 are in LDS or on their way.  One barrier per tile, in the middle of
 // its k steps: by then each wave has waited until only its loads of later tiles are outstanding, and all have finished reading tile kt - 1,
-// whose stage takes tile kt + ST - 1.  The operands of a k step are read while the step before is multiplied.
+// whose stage takes tile kt + ST - 1.  The operands of a k step are read while the step before is multiplied.  (256 x 256 by eight waves of 128 x 64 with
+// four stages of 64 bytes, us for 8192 x 5632 -> 2048: 176; by four waves of 128 x 128 193; 256 x 128 with three stages of 128 bytes 218; 128 x 128, two a compute
+// unit, 312.  Of five stages the rest of a step costs more than they bring: 8192 x 2048 -> 5632 217, with four 213.)
 template <bool AM_, bool BMJ_, int BM_, int BN_, int WM_, int WN_, int KB_, int ST_>
 struct DirectTile {
     typedef bf16_t T;
@@ -859,7 +867,13 @@ size_t rounded16(size_t n) { return (n + 15) / 16 * 16; }
 
 enum Kernel { kFew, kDirect256, kDirect192, kDirect128, kStaged128, kStaged64 };
 
-// Who forms a contraction, and into how many parts its k is cut.
+// Who forms a contraction, and into how many parts its k is cut (us).
+//   few rows: bf16 32 rows of 2048 -> 5632 13.5, by tiles 14.3; 64 rows 21.0, 15.3, of 5632 -> 2048 26.9, 16.3; fp32 48 rows of 1000 -> 1000 11.4, 38.1.
+//   direct 256 x 256 from 128 workgroups on: 2048 x 2048 -> 4096 39.9, on 128 x 128 44.8; 2048 x 1024 -> 4096 22.7, 25.2.  8192 x 5632 x 2048 on 128 x 128: 312, 176.
+//   192 rows where the rounds are done first: the filters' gradient 5632 x 2048 over 8192 rows 195, 171 (176 tiles of 256 rows, 240 of 192).
+//   parts of 2048 elements for large tiles: backward of 8192 x 1024 -> 4096 250, with two parts 218; of 4096 x 2048 -> 2048 135, 117.
+//   staged 128 x 128 from 512 tiles on: 2048 x 2000 -> 2001 bf16 (256 tiles) 58.4, on 64 x 64 47.5; 2048^3 fp32 163, 167.
+//   parts of the staged ones: the odd fp32 backward (1913 x 1431 -> 777) 171 with none, 136.
 struct ContractPlan {
     Kernel kernel;
     int parts, part_k;
@@ -875,7 +889,7 @@ struct Shape {
 ContractPlan contract_plan(const Shape& s)
 {
     ContractPlan p{kStaged128, 1, 0, 0};
-    if (s.k_inside && s.M <= 64) {
+    if (s.k_inside && s.M <= (s.dtype == DSP_BF16 ? 32 : 64)) {
         p.kernel = kFew;
         return p;
     }
@@ -887,7 +901,7 @@ ContractPlan contract_plan(const Shape& s)
         p.kernel = want > 1 || ceil_div(n, 256) * 256 <= ceil_div(low, 256) * 200 ? kDirect256 : kDirect192;
     } else {
         n = tiles(128);
-        p.kernel = s.direct && n >= 64 ? kDirect128 : n >= 256 ? kStaged128 : kStaged64;
+        p.kernel = s.direct && n >= 64 ? kDirect128 : n >= 512 ? kStaged128 : kStaged64;
         if (p.kernel == kStaged64) n = tiles(64);
         want = std::min<int64_t>((p.kernel == kStaged64 ? 1024 : 512) / n, s.K / 512);
     }
@@ -914,10 +928,11 @@ size_t most_bytes(Shape s)
     s.direct = s.dtype == DSP_BF16;
     return std::max(a, contract_plan(s).bytes);
 }
+// (64 lanes a row from 1024 columns on: the backward pass of 8192 x 2048 -> 5632 369 us, with 8 lanes 374; of 256 -> 256 32.1, 29.9; of 512 -> 512 44.6, 42.4.)
 BackPlan back_plan(const dsp_dense_desc* d)
 {
     BackPlan p;
-    p.lpr = d->cout >= 256 ? 64 : 8;
+    p.lpr = d->cout >= 1024 ? 64 : 8;
     const int strips = ceil_div(d->cout, p.lpr * 8), rows = kGradThreads / p.lpr * kGradAhead;
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>(1024 / strips, ceil_div(d->M, rows)));
     p.rows_per_part = ceil_div(ceil_div(d->M, want), rows) * rows;
@@ -983,7 +998,7 @@ int launch_few(GemmArgs& g, hipStream_t st, ProfScope& ps)
     const dim3 grid(ceil_div(g.N, 16)), block(64 * kFewWaves);
     if (g.M <= 16) DSP_LAUNCH(ps, (dense_few_kernel<T, 1>), grid, block, 0, st, g);
     else if (g.M <= 32) DSP_LAUNCH(ps, (dense_few_kernel<T, 2>), grid, block, 0, st, g);
-    else DSP_LAUNCH(ps, (dense_few_kernel<T, 4>), grid, block, 0, st, g);
+    else if constexpr (sizeof(T) == 4) DSP_LAUNCH(ps, (dense_few_kernel<T, 4>), grid, block, 0, st, g);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }

@@ -3,6 +3,10 @@
 //   a_t = 1 / (1 + exp(-f_t)) or exp(f_t),  u_t = x_t or (1 - a_t) x_t,  h_t = a_t h_(t-1) + u_t
 //
 // and, from the last row back, g_t = dh_t + a_(t+1) g_(t+1), dx_t = g_t du/dx, df_t = g_t (h_(t-1) [- x_t]) da/df.
+//
+// Memory bounds it (3 and 6 rows of C for a step); what it reaches is 4.1 TB/s where workgroups fill the card (16 x 4096 x 2048 bf16 backward
+// 395 us, 2048 x 64 x 1024 forward 188) and less with one workgroup a compute unit (8 x 4096 x 2048: 123 us, 3.3 TB/s): a gate takes some
+// thirty vector instructions, and the two barriers of a tile wait for the first wave's walk over the slots.
 #include "common.h"
 
 #include <algorithm>
@@ -213,6 +217,7 @@ __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_back_kernel(Scan
 //
 // A sequence with too few strips to fill the card is cut into parts, whose A and H a first kernel finds (it reads the inputs of the scan once
 // more: what comes back is all compute units).
+// (us with eight rows a lane and with four, which leave room for twice the waves: 64 x 1024 x 1024 forward 110, 98; 16 x 4096 x 2048 backward 485, 395.)
 constexpr int kLaneRows = 4;
 
 struct PartArgs {
@@ -407,7 +412,11 @@ ScanArgs args_of(const dsp_recurrence_desc* d)
     return a;
 }
 
-// Who does it, and how a sequence is cut.
+// Who does it, and how a sequence is cut (bf16, us).  Up to 16 steps a lane walks (64 sequences x 16 x 2048 6.9, scanned 10.1; 256 x 16 x 2048 backward
+// 27.5, 58; but 64 x 32 x 2048 11.6, 10.7; 16 x 32 x 2048 10.2, 5.3; 2048 x 64 x 1024 180, 188).  Parts where strips and sequences make fewer than 192
+// workgroups, 512 of them, of eight tiles at least (one sequence of 32768 x 2048 forward in 8 parts 239, in 16 200; backward 345, 293;
+// 256 workgroups cut in two 166, whole 132: the cut costs a second read).  Sixteen waves a workgroup where there are fewer than 384, which have
+// a compute unit each (8 x 4096 x 2048 forward 145 with eight, 123 with sixteen; backward 242, 219).
 struct Plan {
     bool walk;
     int waves, parts, part_rows;
@@ -419,7 +428,7 @@ Plan plan_of(const dsp_recurrence_desc* d)
     const int vw = d->dtype == DSP_BF16 ? 2 : 1, strips = ceil_div(d->C, 32 * vw);
     p.parts = 1;
     p.part_rows = d->steps;
-    p.walk = d->steps <= 32 || (int64_t)d->sequences * strips >= 8192;
+    p.walk = d->steps <= 16;
     if (p.walk) return p;
     const int64_t groups = (int64_t)strips * d->sequences;
     constexpr int kTile = 2 * 8 * kLaneRows;
