@@ -4,7 +4,7 @@
 //   L = sum over rows of w (max(-A rho, -A clip(rho)) + kl (exp(ref - lp) - (ref - lp) - 1) - entropy H)
 //   dL/dz_j = w / T (c (1[j = label] - p_j) + entropy p_j (log p_j + H)),  c = -A rho [not clipped] + kl (1 - exp(ref - lp))
 //
-// Memory bounds it: a row is read once and its gradient written once, 4096 x 32000 bf16 in 108 us and 4 more for the sum over the rows (4.7 TB/s).  Longer
+// Memory bounds it: a row is read once and its gradient written once, 4096 x 32000 bf16 in 114 us with the sum over the rows (4.6 TB/s).  Longer
 // rows are read twice (1024 x 100000: 114 us, 3.6 TB/s of what is counted).  Rows of odd length, whose 16-byte runs lie across lines, cost a tenth more.
 #include "common.h"
 
