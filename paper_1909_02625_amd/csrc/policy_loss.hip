@@ -30,12 +30,7 @@ struct RowGrad {
     float inv_sum, c0, c1, at_label;
 };
 
-// exp(x) and exp(x) - 1, each to a few units of itself; and exp(x) - 1 - x: by the series from x^2 on below 0.35 (the next terms are 2e-8 of it).
-__device__ inline float exp_any(float x)
-{
-    const float e = exp_of_minus(fabsf(x));
-    return x > 0.f ? __builtin_amdgcn_rcpf(e) : e;
-}
+// exp(x) - 1 - x by the series from x^2 on, below 0.35 (the next terms are 2e-8 of it).
 __device__ inline float series2(float x)
 {
     return x * x * (1.f / 2 + x * (1.f / 6 + x * (1.f / 24 + x * (1.f / 120 + x * (1.f / 720 + x * (1.f / 5040 + x * (1.f / 40320)))))));

@@ -25,17 +25,17 @@ struct ScanArgs {
     int sequences, steps, C, decay, coupled;
 };
 
-// a and 1 - a, each to its own last digits: a sequence of thousands of steps whose decay is close to 1 depends on what it lacks.
+// a and 1 - a, each to its own last digits: a sequence of thousands of steps whose decay is close to 1 depends on what it lacks.  (The sigmoid's are 0
+// below 2^-126.  With the exponential that goes on below, as exp(f) does: 8 x 4096 x 2048 forward 128 us instead of 121, one sequence of 32768 214, 196.)
 __device__ inline void gate_of(int decay, float f, float& a, float& b)
 {
-    const float e = exp_of_minus(fabsf(f));
     if (decay == DSP_DECAY_SIGMOID) {
-        const float q = __builtin_amdgcn_rcpf(1.f + e), r = e * q;
+        const float e = exp_of_minus(fabsf(f)), q = __builtin_amdgcn_rcpf(1.f + e), r = e * q;
         a = f >= 0.f ? q : r;
         b = f >= 0.f ? r : q;
         return;
     }
-    a = f > 0.f ? __builtin_amdgcn_rcpf(e) : e;
+    a = exp_any(f);
     // exp(f) - 1 by its series up to f^7 where the difference would cancel (the next term is 2e-8 of it there)
     const float s = f * (1.f + f * (1.f / 2 + f * (1.f / 6 + f * (1.f / 24 + f * (1.f / 120 + f * (1.f / 720 + f * (1.f / 5040)))))));
     b = fabsf(f) < 0.35f ? -s : 1.f - a;

@@ -1,0 +1,41 @@
+"""The policy loss and the token log probabilities at their ends.
+
+U = 2^-24 is half a step of fp32; what lp may be off by is derived in test_gpu_policy_loss."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1909_02625_amd as D
+from tests import plain_branch as P
+from tests.test_gpu_dense import Rows, rounded
+from tests.test_gpu_policy_loss import HIGH, LOW, TYPES, U, f32, problem
+
+pytestmark = pytest.mark.gpu
+
+
+def loss_of(p, dtype, z, labels, old=None, ref=None, weight=None, kl=0.0, ent=0.0, T=1.0):
+    """token_logprob's lp and H, policy_loss's loss, lp, terms and gradient"""
+    R, V = z.shape
+    code, td, _ = TYPES[dtype]
+    desc = D.make_policy_loss_desc(R, V, code, LOW, HIGH, kl, ent, T)
+    dz, at = Rows(np.zeros((R, V)), td), Rows(z, td)
+    lab = torch.from_numpy(labels.astype(np.int32)).cuda()
+    lp, H, lp2, terms, loss = (torch.zeros(n, device="cuda") for n in (R, R, R, 4 * R, 5))
+    D.dsp_token_logprob(desc, at.view, lab, lp, H)
+    D.dsp_policy_loss(desc, at.view, lab, f32(old), f32(ref), f32(p["adv"]), f32(weight), loss, lp2, terms, dz.view)
+    return [t.cpu().numpy().astype(np.float64) for t in (lp, H, loss, lp2, terms.view(4, R))] + [dz.get()]
+
+
+def test_ratios_next_to_the_largest_float():
+    """rho = exp(lp - old) and exp(ref - lp) up to 3e38: a relative error of what lp is off by (|lp| < 8, 50 terms: 40 U), of the difference's
+    rounding (89 U) and of the exponential (3 U)."""
+    R, V = 24, 50
+    p = problem(R, V, "fp32")
+    _, lp, _, _, _ = P.policy(p["z"], p["labels"], None, None, np.zeros(R), None, LOW, HIGH, 0, 0, 1.0)
+    d = np.linspace(86.5, 88.65, R)
+    old, ref = rounded(lp - d, torch.float32), rounded(lp + d, torch.float32)
+    p["adv"] = rounded(np.full(R, -2.0 ** -30), torch.float32)
+    got = loss_of(p, "fp32", p["z"], p["labels"], old, ref)
+    _, _, _, rt, rdz = P.policy(p["z"], p["labels"], old, ref, p["adv"], None, *(float(np.float32(v)) for v in (LOW, HIGH)), 0.0, 0.0, 1.0)
+    assert (np.abs(got[4][:2] - rt[:2]) <= 150 * U * np.abs(rt[:2])).all() and not got[4][3].any()
+    assert (np.abs(got[5] - rdz) <= 250 * U * np.abs(rdz).max(1, keepdims=True)).all()
