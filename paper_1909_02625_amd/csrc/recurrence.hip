@@ -10,6 +10,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace dsp {
 namespace {
@@ -64,7 +65,7 @@ struct Lane4;
 template <>
 struct Lane4<float> {
     static constexpr int VW = 1;
-    static constexpr uint32_t kInfinity = 0x7f800000u;
+    static constexpr uint32_t kInfinity = 0x7f800000u, kSigns = 0x80000000u;
     __device__ static inline void unpack(uint32_t r, float (&v)[1]) { v[0] = __uint_as_float(r); }
     __device__ static inline uint32_t pack(const float (&v)[1]) { return __float_as_uint(v[0]); }
     __device__ static inline uint32_t load(const float* p, bool) { return __float_as_uint(*p); }
@@ -73,7 +74,7 @@ struct Lane4<float> {
 template <>
 struct Lane4<bf16_t> {
     static constexpr int VW = 2;
-    static constexpr uint32_t kInfinity = 0x7f807f80u;
+    static constexpr uint32_t kInfinity = 0x7f807f80u, kSigns = 0x80008000u;
     __device__ static inline void unpack(uint32_t r, float (&v)[2])
     {
         v[0] = __uint_as_float(r << 16);
@@ -215,38 +216,61 @@ __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_back_kernel(Scan
 // LDS what each one starts from; (3) every slot goes through its rows once more, which it still has in registers.  Backward the same from
 // the last row on, with r = a g in the place of h.  Rows behind the end are steps that change nothing (a = 1, u = 0).
 //
+// Products of decays may leave the floats where no state does (decays above 1; large states that are forgotten).  A tile in which one did, or in which a state
+// is not finite, is gone through a second time, slot after slot by its rows: what then comes out is what row by row gives.
+//
 // A sequence with too few strips to fill the card is cut into parts, whose A and H a first kernel finds (it reads the inputs of the scan once
-// more: what comes back is all compute units).
+// more: what comes back is all compute units).  The scan of a part begins with the state that those in front of it leave; where one of their products has left the
+// floats it goes through that part's rows.  Outputs in the place of what it would read there: a kernel between the two finds those states.
 // (us with eight rows a lane and with four, which leave room for twice the waves: 64 x 1024 x 1024 forward 110, 98; 16 x 4096 x 2048 backward 485, 395.)
 constexpr int kLaneRows = 4;
 
+enum ScanMode { kScan, kParts, kStates };
+
 struct PartArgs {
-    float* sums;      // [sequences][parts - 1][3][C]: a, c, H of each part but the last
+    float* sums;      // [sequences][parts - 1][4][C]: what each part but the last does, h -> (m + c) 2^e h + H: m, c, e, and H, in whose place the state behind it comes
     float* state;     // [sequences][C]: the state that goes in (the call may overwrite it)
     int parts, part_rows;
+    bool found;       // the states between the parts are there
 };
 
-// LDS of a workgroup: what the slots do, and what they start from.
+// A product of decays below kFaint has lost digits, or all of them, to the end of the floats.  That counts where it leaves more of the state than the sum beside
+// it hides.
+constexpr float kFaint = 0x1p-100f;
+__device__ inline bool lost_digits(float a, float h, float in) { return a < kFaint && fabsf(in) > 1.f && fabsf(h) < fabsf(in) * 0x1p-120f; }
+__device__ inline bool finite_state(float h) { return fabsf(h) < INFINITY; }
+
+// LDS of a workgroup: what the slots do, and what they start from (the last: the state behind the tile).
 template <int SLOTS, int W>
 struct Slots {
-    float a[SLOTS][W], c[SLOTS][W], h[SLOTS][W], in[SLOTS][W];
+    float a[SLOTS][W], c[SLOTS][W], h[SLOTS][W], in[SLOTS + 1][W];
+    int watch;  // some product of the tile is below kFaint (kParts: some decay of it may be above 1)
+    int lost;   // 1: its states are found row by row; 2: the slots are asked
+    int asked;  // their answer
+    int part;   // the part that is scanned next
 };
 
-// MODE 0: the scan; 1: what each part does, for the kernel behind.
 template <typename T, int WAVES, bool BACK, int DECAY, bool COUPLED, int MODE>
 __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
 {
     typedef Lane4<T> L;
     constexpr int VW = L::VW, W = 32 * VW, TT = kLaneRows, SLOTS = 2 * WAVES, TILE = SLOTS * TT;
-    constexpr uint32_t kNone = DECAY == DSP_DECAY_SIGMOID ? L::kInfinity : 0u;  // the f of a = 1
+    constexpr uint32_t kNone = DECAY == DSP_DECAY_SIGMOID ? L::kInfinity : L::kSigns;  // the f of a = 1: infinity, or -0
     __shared__ Slots<SLOTS, W> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = wave * 2 + lane / 32;
-    const int s = blockIdx.y, part = blockIdx.z, c = blockIdx.x * W + lane % 32 * VW;
+    const int s = blockIdx.y, c = blockIdx.x * W + lane % 32 * VW;
     const bool in = c < p.C, both = c + VW <= p.C;
+    if (tid == 0) lds.watch = lds.asked = 0;
+    lds_barrier();
     int whole;
     const int64_t first = rows_of(p, s, whole);
-    // the rows of this part, in the order of the scan: k = 0 .. n - 1 is row k, or backward row whole - 1 - k
-    const int begin = part * q.part_rows, n = whole - begin < q.part_rows ? whole - begin : q.part_rows;
+    // the rows of a part, in the order of the scan: k = 0 .. n - 1 is row begin + k, or backward row whole - 1 - (begin + k)
+    int begin = 0, n = 0;
+    auto choose = [&](int part) {
+        begin = part * q.part_rows;
+        n = whole - begin < q.part_rows ? whole - begin : q.part_rows;
+    };
+    choose(MODE == kStates ? 0 : blockIdx.z);
     const T* const x = (const T*)p.x + first * p.xs + c;
     const T* const f = (const T*)p.f + first * p.fs + c;
     const T* const h = (const T*)p.h + first * p.hs + c;
@@ -266,7 +290,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
             const int64_t row = row_of(k);
             r.f[i] = L::load(f + row * p.fs, both);
             r.u[i] = BACK ? L::load(d + row * p.hs, both) : L::load(x + row * p.xs, both);
-            if (BACK && MODE == 0) {
+            if (BACK && MODE == kScan) {
                 if (COUPLED) r.x[i] = L::load(x + row * p.xs, both);
                 if (row > 0) r.h[i] = L::load(h + (row - 1) * p.hs, both);
             }
@@ -276,112 +300,248 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
     // the state that the first wave carries: lane l's channel l of the strip
     const int cc = blockIdx.x * W + lane;
     const bool mine = wave == 0 && lane < W && cc < p.C;
+    float* const sums = q.sums + (int64_t)s * (q.parts - 1) * 4 * p.C + cc;
     float carry = 0.f, pa = 1.f, pc = 0.f;
-    if (MODE == 0 && mine) {
-        const float* from = q.parts > 1 ? q.state : BACK ? p.dlast : p.state;
+    int pe = 0;
+    bool guess = false;  // kParts: a product below kFaint is in pa, which is then a bound of what it should be
+    if (MODE != kParts && mine) {
+        const float* from = MODE == kScan && q.parts > 1 ? q.state : BACK ? p.dlast : p.state;
         if (from) carry = from[(int64_t)s * p.C + cc];
-        const float* sums = q.sums + (int64_t)s * (q.parts - 1) * 3 * p.C + cc;
-        for (int j = 0; j < part; ++j, sums += 3 * p.C) carry = step_of(sums[0], sums[p.C], carry, sums[2 * p.C]);
+        if (MODE == kStates) q.state[(int64_t)s * p.C + cc] = carry;
     }
-    if (MODE == 1 && mine && part == 0) {
+    if (MODE == kParts && mine && blockIdx.z == 0 && !q.found) {
         const float* from = BACK ? p.dlast : p.state;
         q.state[(int64_t)s * p.C + cc] = from ? from[(int64_t)s * p.C + cc] : 0.f;
     }
     float before[VW] = {};  // the state in front of the first row, which h_(t-1) is there
-    if (BACK && MODE == 0 && p.state) {
+    if (BACK && MODE == kScan && p.state) {
 #pragma unroll
         for (int v = 0; v < VW; ++v)
             if (c + v < p.C) before[v] = p.state[(int64_t)s * p.C + c + v];
     }
 
-    Raw next;
-    if (n > 0) load(0, next);
-    for (int t0 = 0; t0 < n; t0 += TILE) {
-        const Raw r = next;
-        if (t0 + TILE < n) load(t0 + TILE, next);
-        float a[TT][VW], rest[TT][VW], u[TT][VW], A[VW], B[VW], H[VW];
+    auto scan = [&](bool keep) {
+        Raw next;
+        if (n > 0) load(0, next);
+        for (int t0 = 0; t0 < n; t0 += TILE) {
+            const Raw r = next;
+            if (t0 + TILE < n) load(t0 + TILE, next);
+            float a[TT][VW], rest[TT][VW], u[TT][VW], A[VW], B[VW], H[VW];
 #pragma unroll
-        for (int v = 0; v < VW; ++v) A[v] = 1.f, B[v] = H[v] = 0.f;
+            for (int v = 0; v < VW; ++v) A[v] = 1.f, B[v] = H[v] = 0.f;
 #pragma unroll
-        for (int i = 0; i < TT; ++i) {
-            float fv[VW], xv[VW];
-            L::unpack(r.f[i], fv);
-            L::unpack(r.u[i], xv);
+            for (int i = 0; i < TT; ++i) {
+                float fv[VW], xv[VW];
+                L::unpack(r.f[i], fv);
+                L::unpack(r.u[i], xv);
+#pragma unroll
+                for (int v = 0; v < VW; ++v) {
+                    float b;
+                    gate_of(DECAY, fv[v], a[i][v], b);
+                    rest[i][v] = rest_of(a[i][v], b);
+                    u[i][v] = BACK || !COUPLED ? xv[v] : b * xv[v];
+                    B[v] = fmaf(A[v], b, B[v]);
+                    A[v] *= a[i][v];
+                    H[v] = BACK ? step_of(a[i][v], rest[i][v], H[v] + xv[v], 0.f) : step_of(a[i][v], rest[i][v], H[v], u[i][v]);
+                }
+            }
+            bool watch = MODE != kParts && (VW == 2 ? fminf(A[0], A[VW - 1]) : A[0]) < kFaint;
+            if (DECAY == DSP_DECAY_EXP && (r.f[0] & r.f[1] & r.f[2] & r.f[3] & L::kSigns) != L::kSigns) {
+                // some decay may be above 1: a product that lost its digits on the way and rose again is none
+                static_assert(TT == 4, "four rows");
+                watch |= MODE == kParts;
+#pragma unroll
+                for (int v = 0; v < VW; ++v)
+                    if (fminf(a[0][v] * a[1][v], a[0][v] * a[1][v] * a[2][v]) < kFaint) A[v] = NAN;
+            }
 #pragma unroll
             for (int v = 0; v < VW; ++v) {
-                float b;
-                gate_of(DECAY, fv[v], a[i][v], b);
-                rest[i][v] = rest_of(a[i][v], b);
-                u[i][v] = BACK || !COUPLED ? xv[v] : b * xv[v];
-                B[v] = fmaf(A[v], b, B[v]);
-                A[v] *= a[i][v];
-                H[v] = BACK ? step_of(a[i][v], rest[i][v], H[v] + xv[v], 0.f) : step_of(a[i][v], rest[i][v], H[v], u[i][v]);
+                const int w = lane % 32 * VW + v;
+                lds.a[slot][w] = A[v];
+                lds.c[slot][w] = rest_of(A[v], B[v]);
+                lds.h[slot][w] = H[v];
             }
-        }
-#pragma unroll
-        for (int v = 0; v < VW; ++v) {
-            const int w = lane % 32 * VW + v;
-            lds.a[slot][w] = A[v];
-            lds.c[slot][w] = rest_of(A[v], B[v]);
-            lds.h[slot][w] = H[v];
-        }
-        lds_barrier();
-        if (wave == 0 && lane < W) {
+            if ((MODE != kParts || DECAY == DSP_DECAY_EXP) && watch) lds.watch = 1;
+            lds_barrier();
+            if (wave == 0 && lane < W) {
+                const int watched = lds.watch;
+                if (MODE == kParts) {
+                    // (pa + pc) (ja + jc), to twice the digits of either
+                    auto times = [&](float ja, float jc) {
+                        const float m = pa * ja;
+                        pc = fmaf(pa, ja, -m) + fmaf(pa, jc, pc * ja);
+                        pa = m;
+                    };
+                    auto exponent_apart = [&]() {
+                        const int e = __builtin_amdgcn_frexp_expf(pa);
+                        pa = __builtin_amdgcn_ldexpf(pa, -e);
+                        pc = __builtin_amdgcn_ldexpf(pc, -e);
+                        pe += e;
+                    };
+                    if (DECAY == DSP_DECAY_EXP && __builtin_amdgcn_readfirstlane(watched)) {
+#pragma unroll 1
+                        for (int j = 0; j < SLOTS; ++j) {
+                            float ja = lds.a[j][lane], jc = lds.c[j][lane];
+                            carry = step_of(ja, jc, carry, lds.h[j][lane]);
+                            if (ja < kFaint) {
+                                guess = true;
+                                ja = (ja + 0x1p-148f) * 0x1p100f;
+                                jc = 0.f;
+                                pe -= 100;
+                            }
+                            times(ja, jc);
+                            exponent_apart();
+                        }
+                    } else {
 #pragma unroll 4
-            for (int j = 0; j < SLOTS; ++j) {
-                const float ja = lds.a[j][lane], jc = lds.c[j][lane], jh = lds.h[j][lane];
-                lds.in[j][lane] = carry;
-                carry = step_of(ja, jc, carry, jh);
-                if (MODE == 1) {  // (pa + pc) (ja + jc), to twice the digits of either
-                    const float m = pa * ja;
-                    pc = fmaf(pa, ja, -m) + fmaf(pa, jc, pc * ja);
-                    pa = m;
+                        for (int j = 0; j < SLOTS; ++j) {
+                            const float ja = lds.a[j][lane], jc = lds.c[j][lane];
+                            carry = step_of(ja, jc, carry, lds.h[j][lane]);
+                            times(ja, jc);
+                        }
+                        if (pa < kFaint) {  // (of decays not above 1: what each of these products has lost, half a step of 2^-149, has not grown)
+                            guess = true;
+                            pa += 0x1p-138f;
+                        }
+                        if (DECAY == DSP_DECAY_EXP) exponent_apart();
+                    }
+                } else {
+                    const float front = carry;
+#pragma unroll 4
+                    for (int j = 0; j < SLOTS; ++j) {
+                        const float ja = lds.a[j][lane], jc = lds.c[j][lane], jh = lds.h[j][lane];
+                        lds.in[j][lane] = carry;
+                        carry = step_of(ja, jc, carry, jh);
+                    }
+                    // (no step makes a state finite again; NaN it stays)
+                    const bool lost = __any(front == front && !finite_state(carry));
+                    if (lane == 0) lds.lost = lost ? 1 : watched ? 2 : 0;
+                }
+                if (lane == 0) lds.watch = 0;
+            }
+            lds_barrier();
+            if (MODE == kParts) continue;
+            // a row's step: backward `u` is dh
+            auto step = [&](int i, int v, float st) {
+                return BACK ? step_of(a[i][v], rest[i][v], u[i][v] + st, 0.f) : step_of(a[i][v], rest[i][v], st, u[i][v]);
+            };
+            float st[VW];
+#pragma unroll
+            for (int v = 0; v < VW; ++v) st[v] = lds.in[slot][lane % 32 * VW + v];
+            int lost = __builtin_amdgcn_readfirstlane(lds.lost);
+            if (lost == 2) {
+                bool here = false;
+#pragma unroll
+                for (int v = 0; v < VW; ++v) here |= lost_digits(A[v], H[v], st[v]);
+                if (here) lds.asked = 1;
+                lds_barrier();
+                lost = __builtin_amdgcn_readfirstlane(lds.asked);
+            }
+            if (lost) {
+#pragma unroll 1
+                for (int j = 0; j < SLOTS; ++j) {
+                    if (slot == j)
+#pragma unroll
+                        for (int v = 0; v < VW; ++v) {
+                            const int w = lane % 32 * VW + v;
+                            float left = st[v] = lds.in[j][w];
+#pragma unroll
+                            for (int i = 0; i < TT; ++i) left = step(i, v, left);
+                            lds.in[j + 1][w] = left;
+                        }
+                    lds_barrier();
+                }
+                if (wave == 0 && lane < W) carry = lds.in[SLOTS][lane];
+                if (tid == 0) lds.asked = 0;
+            }
+            if (MODE == kStates || !keep) continue;
+#pragma unroll
+            for (int i = 0; i < TT; ++i) {
+                const int k = t0 + slot * TT + i;
+                const int64_t row = row_of(k);
+                float o[VW], o2[VW], xv[VW], hv[VW];
+                if (BACK) {
+                    L::unpack(r.x[i], xv);
+                    L::unpack(r.h[i], hv);
+                }
+#pragma unroll
+                for (int v = 0; v < VW; ++v) {
+                    const float g = u[i][v] + st[v];
+                    st[v] = step(i, v, st[v]);
+                    if (!BACK) {
+                        o[v] = st[v];
+                    } else {
+                        const float b = (1.f - a[i][v]) - rest[i][v], hp = row == 0 ? before[v] : hv[v];
+                        o[v] = COUPLED ? b * g : g;
+                        o2[v] = (DECAY == DSP_DECAY_SIGMOID ? a[i][v] * b : a[i][v]) * g * (COUPLED ? hp - xv[v] : hp);
+                    }
+                }
+                if (!in || k >= n) continue;
+                if (!BACK) {
+                    L::store((T*)p.out + (first + row) * p.hs + c, L::pack(o), both);
+                } else {
+                    if (p.dx) L::store((T*)p.dx + (first + row) * p.xs + c, L::pack(o), both);
+                    if (p.df) L::store((T*)p.df + (first + row) * p.fs + c, L::pack(o2), both);
                 }
             }
         }
-        lds_barrier();
-        if (MODE == 1) continue;
-        float st[VW];
+    };
+
+    if (MODE == kParts || q.parts == 1) {
+        scan(true);
+    } else {
+        // from part to part by what each does, and through the rows of one whose product, or the state behind it, is not to be had that way
+        const int to = MODE == kScan ? blockIdx.z : q.parts - 1;
+        int j = 0;
+        if (MODE == kScan && q.found && to > 0) {
+            if (mine) carry = sums[((int64_t)(to - 1) * 4 + 3) * p.C];
+            j = to;
+        }
+        for (bool end = false; !end; ++j) {
+            if (j < to) {
+                if (wave == 0) {
+                    constexpr int AHEAD = 8;
+                    const float* const from = q.sums + (int64_t)s * (q.parts - 1) * 4 * p.C + (cc < p.C ? cc : p.C - 1);
+                    for (bool on = true; on && j < to;) {
+                        float v[AHEAD][4];
 #pragma unroll
-        for (int v = 0; v < VW; ++v) st[v] = lds.in[slot][lane % 32 * VW + v];
+                        for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-        for (int i = 0; i < TT; ++i) {
-            const int k = t0 + slot * TT + i;
-            const int64_t row = row_of(k);
-            float o[VW], o2[VW], xv[VW], hv[VW], dv[VW];
-            if (BACK) {
-                L::unpack(r.x[i], xv);
-                L::unpack(r.h[i], hv);
-                L::unpack(r.u[i], dv);
-            }
+                            for (int k = 0; k < 4; ++k) v[i][k] = from[((int64_t)(j + i < to ? j + i : j) * 4 + k) * p.C];
 #pragma unroll
-            for (int v = 0; v < VW; ++v) {
-                if (!BACK) {
-                    st[v] = step_of(a[i][v], rest[i][v], st[v], u[i][v]);
-                    o[v] = st[v];
-                } else {
-                    const float g = dv[v] + st[v], b = (1.f - a[i][v]) - rest[i][v], hp = row == 0 ? before[v] : hv[v];
-                    st[v] = step_of(a[i][v], rest[i][v], g, 0.f);
-                    o[v] = COUPLED ? b * g : g;
-                    o2[v] = (DECAY == DSP_DECAY_SIGMOID ? a[i][v] * b : a[i][v]) * g * (COUPLED ? hp - xv[v] : hp);
+                        for (int i = 0; i < AHEAD; ++i) {
+                            const float m = v[i][0], H = v[i][3], left = __builtin_amdgcn_ldexpf(fmaf(fabsf(m), carry, v[i][1] * carry), (int)v[i][2]);
+                            const float next = m < 0.f && carry == carry ? H : left + H;  // (m < 0: a bound of it)
+                            const bool lost = !finite_state(next) || (m < 0.f && !(fabsf(left) < 0x1p-127f || fabsf(left) < fabsf(H) * 0x1p-26f));
+                            on = on && j < to && !__any(mine && lost && carry == carry);
+                            if (on) {
+                                carry = next;
+                                if (MODE == kStates && mine) sums[((int64_t)j * 4 + 3) * p.C] = carry;
+                                ++j;
+                            }
+                        }
+                    }
+                    if (lane == 0) lds.part = j;
                 }
+                __syncthreads();
+                j = __builtin_amdgcn_readfirstlane(lds.part);
+                __syncthreads();
             }
-            if (!in || k >= n) continue;
-            if (!BACK) {
-                L::store((T*)p.out + (first + row) * p.hs + c, L::pack(o), both);
-            } else {
-                if (p.dx) L::store((T*)p.dx + (first + row) * p.xs + c, L::pack(o), both);
-                if (p.df) L::store((T*)p.df + (first + row) * p.fs + c, L::pack(o2), both);
-            }
+            end = j == to;
+            if (MODE == kStates && end) break;
+            choose(j);
+            scan(end);
+            if (MODE == kStates && mine) sums[((int64_t)j * 4 + 3) * p.C] = carry;
         }
     }
     if (!mine) return;
-    if (MODE == 1) {
-        float* to = q.sums + ((int64_t)s * (q.parts - 1) + part) * 3 * p.C + cc;
-        to[0] = pa;
-        to[p.C] = pc;
-        to[2 * p.C] = carry;
-    } else if (part == q.parts - 1 && p.left) {
+    if (MODE == kParts) {
+        float* const to = sums + (int64_t)blockIdx.z * 4 * p.C;
+        to[0] = guess ? -pa : pa;
+        to[p.C] = guess ? 0.f : pc;
+        to[2 * p.C] = (float)pe;
+        to[3 * p.C] = carry;
+    } else if ((int)blockIdx.z == q.parts - 1 && p.left) {
         p.left[(int64_t)s * p.C + cc] = carry;
     }
 }
@@ -437,7 +597,7 @@ Plan plan_of(const dsp_recurrence_desc* d)
     p.parts = ceil_div(d->steps, p.part_rows);
     p.waves = groups * p.parts >= 384 ? 8 : 16;
     if (p.parts > 1) {
-        p.sums = (size_t)d->sequences * (p.parts - 1) * 3 * d->C * sizeof(float);
+        p.sums = (size_t)d->sequences * (p.parts - 1) * 4 * d->C * sizeof(float);
         p.bytes = (p.sums + (size_t)d->sequences * d->C * sizeof(float) + 15) / 16 * 16;
     }
     return p;
@@ -449,11 +609,16 @@ int scan_by(const ScanArgs& a, const PartArgs& q, hipStream_t st, const char* na
     const dim3 grid(ceil_div(a.C, 32 * Lane4<T>::VW), a.sequences, q.parts), block(64 * WAVES);
     if (q.parts > 1) {
         ProfScope ps("recurrence_parts", bytes * 2 / (BACK ? 6 : 3), 1);
-        DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, 1>), dim3(grid.x, grid.y, grid.z - 1), block, 0, st, a, q);
+        DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, kParts>), dim3(grid.x, grid.y, grid.z - 1), block, 0, st, a, q);
         DSP_HIP(hipGetLastError());
+        if (q.found) {
+            ProfScope pt("recurrence_states", 20.0 * (q.parts - 1) * a.sequences * a.C, 1);
+            DSP_LAUNCH(pt, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, kStates>), dim3(grid.x, grid.y), block, 0, st, a, q);
+            DSP_HIP(hipGetLastError());
+        }
     }
     ProfScope ps(name, bytes, 1);
-    DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, 0>), grid, block, 0, st, a, q);
+    DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, kScan>), grid, block, 0, st, a, q);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
@@ -482,6 +647,7 @@ int run(const dsp_recurrence_desc* d, const ScanArgs& a, void* workspace, hipStr
     q.state = (float*)((char*)workspace + p.sums);
     q.parts = p.parts;
     q.part_rows = p.part_rows;
+    q.found = BACK && (a.dx == a.dh || a.df == a.f);
     if (d->decay == DSP_DECAY_SIGMOID)
         return d->coupled ? scan<T, BACK, DSP_DECAY_SIGMOID, true>(a, q, p.waves, st, name, bytes) : scan<T, BACK, DSP_DECAY_SIGMOID, false>(a, q, p.waves, st, name, bytes);
     return d->coupled ? scan<T, BACK, DSP_DECAY_EXP, true>(a, q, p.waves, st, name, bytes) : scan<T, BACK, DSP_DECAY_EXP, false>(a, q, p.waves, st, name, bytes);
