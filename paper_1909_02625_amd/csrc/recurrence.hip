@@ -55,9 +55,11 @@ __device__ inline int64_t rows_of(const ScanArgs& p, int s, int& length)
 }
 
 // The decay of a step or of many: what h is multiplied by is a + c, where c is the part of 1 - (1 - a) that a has no digits for.  h (a + c) + u are two
-// operations; only where a is the larger of the two does c hold anything.
-__device__ inline float rest_of(float a, float b) { return b < 0.5f ? (1.f - a) - b : 0.f; }
+// operations; only where a is the larger of the two, and 1 - a smaller than either, does c hold anything.  An infinite h has no use for it, and no
+// product with c = 0: a row's step takes the largest float there.
+__device__ inline float rest_of(float a, float b) { return fabsf(b) < 0.5f ? (1.f - a) - b : 0.f; }
 __device__ inline float step_of(float a, float c, float h, float u) { return fmaf(a, h, fmaf(c, h, u)); }
+__device__ inline float row_step(float a, float c, float h, float u) { return fmaf(a, h, fmaf(c, __builtin_amdgcn_fmed3f(h, -3.40282347e38f, 3.40282347e38f), u)); }
 
 // ---- four bytes of a row: a lane's channels -----------------------------------------------------------
 template <typename T>
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_kernel(ScanArgs 
         for (int v = 0; v < VW; ++v) {
             float a, b;
             gate_of(p.decay, fv[v], a, b);
-            h[v] = step_of(a, rest_of(a, b), h[v], p.coupled ? b * xv[v] : xv[v]);
+            h[v] = row_step(a, rest_of(a, b), h[v], p.coupled ? b * xv[v] : xv[v]);
         }
         return L::pack(h);
     };
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_back_kernel(Scan
             float a, b;
             gate_of(p.decay, fv[v], a, b);
             const float g = dv[v] + r[v], hp = t ? hv[v] : before[v];
-            r[v] = step_of(a, rest_of(a, b), g, 0.f);
+            r[v] = row_step(a, rest_of(a, b), g, 0.f);
             fv[v] = (p.decay == DSP_DECAY_SIGMOID ? a * b : a) * g * (p.coupled ? hp - xv[v] : hp);
             xv[v] = p.coupled ? b * g : g;
         }
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
             if (MODE == kParts) continue;
             // a row's step: backward `u` is dh
             auto step = [&](int i, int v, float st) {
-                return BACK ? step_of(a[i][v], rest[i][v], u[i][v] + st, 0.f) : step_of(a[i][v], rest[i][v], st, u[i][v]);
+                return BACK ? row_step(a[i][v], rest[i][v], u[i][v] + st, 0.f) : row_step(a[i][v], rest[i][v], st, u[i][v]);
             };
             float st[VW];
 #pragma unroll
