@@ -52,16 +52,18 @@ __device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top
     const float q = (m - 1.f) / (m + 1.f), q2 = q * q, log_m = 2.f * q * (1.f + q2 * (1.f / 3 + q2 * (1.f / 5 + q2 * (1.f / 7 + q2 * (1.f / 9)))));
     const double logs = ex * 0.69314718055994531 + (double)log_m;
     const double lp = ((double)at_label - (double)top) * a.inv_t - logs;
-    const float spread = dsum / sum * (float)a.inv_t, H = (float)logs + spread;
+    // (no lp: the label names no token, or the row holds NaN or infinity.  Nothing that is made of the row is a number then, whatever does not need lp.)
+    const bool none = !(lp == lp);
+    const float spread = dsum / sum * (float)a.inv_t, H = none ? NAN : (float)logs + spread;
     if (a.logp) a.logp[row] = (float)lp;
     if (a.entropy) a.entropy[row] = H;
     RowGrad g = {0.f, 0.f, 0.f, 0.f};
     if (!a.full) return g;
-    const float A = a.advantage[row], rho = a.old ? exp_any((float)(lp - (double)a.old[row])) : 1.f;
+    const float A = a.advantage[row], rho = a.old ? exp_any((float)(lp - (double)a.old[row])) : none ? NAN : 1.f;
     const float bounded = rho < a.low ? a.low : rho > a.high ? a.high : rho;
     const float free = -A * rho, held = -A * bounded;
     const bool clipped = held > free;
-    float c = clipped ? 0.f : free, kl = 0.f;
+    float c = clipped ? 0.f : free, kl = none ? NAN : 0.f;
     if (a.ref) {
         const float d = (float)((double)a.ref[row] - lp);
         const bool near = fabsf(d) < 0.35f;
@@ -72,7 +74,7 @@ __device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top
     a.terms[row] = clipped ? held : free;
     a.terms[(int64_t)a.R + row] = kl;
     a.terms[2 * (int64_t)a.R + row] = H;
-    a.terms[3 * (int64_t)a.R + row] = clipped ? 1.f : 0.f;
+    a.terms[3 * (int64_t)a.R + row] = none ? NAN : clipped ? 1.f : 0.f;
     const float w = (a.weight ? a.weight[row] : 1.f / a.R) * (float)a.inv_t;
     g.inv_sum = 1.f / sum;
     g.at_label = w * c;

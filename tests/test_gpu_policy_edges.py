@@ -39,3 +39,27 @@ def test_ratios_next_to_the_largest_float():
     _, _, _, rt, rdz = P.policy(p["z"], p["labels"], old, ref, p["adv"], None, *(float(np.float32(v)) for v in (LOW, HIGH)), 0.0, 0.0, 1.0)
     assert (np.abs(got[4][:2] - rt[:2]) <= 150 * U * np.abs(rt[:2])).all() and not got[4][3].any()
     assert (np.abs(got[5] - rdz) <= 250 * U * np.abs(rdz).max(1, keepdims=True)).all()
+
+
+@pytest.mark.parametrize("V", [3, 30, 1000, 4099, 40000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_labels_of_no_token_make_their_rows_nan(dtype, V):
+    """Whatever is given beside them: the old model's and the reference's log probabilities, both, neither."""
+    p = problem(7, V, dtype)
+    z = p["z"].copy()
+    z[5, V // 2], z[6, V - 1] = np.nan, np.inf
+    labels = p["labels"].copy()
+    labels[1], labels[3], labels[4] = V, 1 << 30, -1
+    for old in (None, p["old"]):
+        for ref in (None, p["ref"]):
+            for ent in (0.0, 0.01):
+                kl = 0.1 if ref is not None else 0.0
+                lp, H, loss, lp2, terms, dz = loss_of(p, dtype, z, labels, old, ref, None, kl, ent)
+                clean = loss_of(p, dtype, p["z"], p["labels"], old, ref, None, kl, ent)
+                for r in (1, 3, 5, 6):
+                    assert np.isnan([lp[r], H[r], lp2[r]]).all() and np.isnan(terms[:, r]).all() and np.isnan(dz[r]).all(), (r, old is None, ref is None)
+                assert np.isnan(loss).all()
+                for r in (0, 2):
+                    assert all(np.array_equal(a[..., r], b[..., r]) for a, b in zip((lp, H, lp2, terms), (clean[0], clean[1], clean[3], clean[4])))
+                    assert np.array_equal(dz[r], clean[5][r])
+                assert lp[4] == H[4] == lp2[4] == 0 and not terms[:, 4].any() and not dz[4].any()
