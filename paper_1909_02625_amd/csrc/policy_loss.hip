@@ -82,13 +82,14 @@ __device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top
     g.c1 = w * a.ent * (float)a.inv_t;
     return g;
 }
-// A row without a token, or without a logit that is not -infinity: it has no part in the loss.
+// A row without a token, or without a logit that is not -infinity: it has no part in the loss, whatever its weight is.  The sum over the rows knows it by the
+// sign of its entropy (no other row's is -0), which it takes away.
 __device__ inline void empty_row(const PolicyArgs& a, int64_t row)
 {
     if (a.logp) a.logp[row] = 0.f;
     if (a.entropy) a.entropy[row] = 0.f;
     if (a.full)
-        for (int k = 0; k < 4; ++k) a.terms[k * (int64_t)a.R + row] = 0.f;
+        for (int k = 0; k < 4; ++k) a.terms[k * (int64_t)a.R + row] = k == 2 ? -0.f : 0.f;
 }
 
 // A row lies with WAVES waves; with one of them a workgroup has four rows, otherwise one.
@@ -363,14 +364,18 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a, f
             const int64_t r = r0 + i * kSumThreads;
             const bool in = r < a.R;
             w[i] = in ? (a.weight ? a.weight[r] : 1.f) : 0.f;
-            if (in && a.labels[r] < 0) w[i] = 0.f;  // (whatever its weight is)
 #pragma unroll
             for (int k = 0; k < 4; ++k) t[i][k] = in ? a.terms[k * (int64_t)a.R + r] : 0.f;
         }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
+        for (int i = 0; i < AHEAD; ++i) {
+            if (__float_as_uint(t[i][2]) == 0x80000000u) {
+                w[i] = 0.f;
+                a.terms[2 * (int64_t)a.R + r0 + i * kSumThreads] = 0.f;
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[k] += (double)w[i] * (double)t[i][k];
+        }
     }
     if (!a.weight)
 #pragma unroll

@@ -63,3 +63,20 @@ def test_labels_of_no_token_make_their_rows_nan(dtype, V):
                     assert all(np.array_equal(a[..., r], b[..., r]) for a, b in zip((lp, H, lp2, terms), (clean[0], clean[1], clean[3], clean[4])))
                     assert np.array_equal(dz[r], clean[5][r])
                 assert lp[4] == H[4] == lp2[4] == 0 and not terms[:, 4].any() and not dz[4].any()
+
+
+@pytest.mark.parametrize("V", [30, 1000, 40000])
+def test_weights_of_rows_without_a_part(V):
+    """A row of nothing but -infinity and a row without a token have no part in the loss, whatever their weights are."""
+    p = problem(6, V, "fp32")
+    z, labels, w = p["z"].copy(), p["labels"].copy(), p["weight"].copy()
+    z[1], z[2], labels[4], labels[5] = -np.inf, -np.inf, -1, -7
+    calm = w.copy()
+    w[[1, 4]], w[[2, 5]] = np.inf, np.nan
+    calm[[1, 2, 4, 5]] = 0.0
+    got, want = (loss_of(p, "fp32", z, labels, p["old"], p["ref"], v, 0.1, 0.01) for v in (w, calm))
+    assert np.isfinite(got[2]).all() and all(np.array_equal(a, b) for a, b in zip(got, want))
+    assert not np.signbit(got[4]).any(axis=0)[[1, 2, 4, 5]].any()
+    # a weight of a row that does count: infinite or NaN as it is
+    w[0] = np.nan
+    assert np.isnan(loss_of(p, "fp32", z, labels, p["old"], p["ref"], w, 0.1, 0.01)[2][0])
