@@ -25,7 +25,7 @@ struct PolicyArgs {
     float k, low, high, kl, ent;  // k = log2(e) / T
 };
 
-// What of a row's loss its gradient needs: dz_j = p_j (c0 - c1 d_j), d_j = max - z_j, and `at_label` more at the label.
+// What of a row's loss its gradient needs: dz_j = p_j (c0 - c1 t_j), t_j = log2(e) (max - z_j) / T, and `at_label` more at the label.
 struct RowGrad {
     float inv_sum, c0, c1, at_label;
 };
@@ -36,7 +36,7 @@ __device__ inline float series2(float x)
     return x * x * (1.f / 2 + x * (1.f / 6 + x * (1.f / 24 + x * (1.f / 120 + x * (1.f / 720 + x * (1.f / 5040 + x * (1.f / 40320)))))));
 }
 
-// A row's results from its largest logit, sum of exponentials and sum of exponentials times top - z; by one thread.  The log probability is added
+// A row's results from its largest logit, sum of exponentials and sum of exponentials times their t; by one thread.  The log probability is added
 // up in 64 bits and its differences to the old and the reference's are taken there: a KL term of a difference of a tenth keeps five digits of it.
 // All that is left is small and goes in floats (the library's logarithm and exponentials of 64 bits would take the registers in which the
 // row is held).
@@ -54,7 +54,8 @@ __device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top
     const double lp = ((double)at_label - (double)top) * a.inv_t - logs;
     // (no lp: the label names no token, or the row holds NaN or infinity.  Nothing that is made of the row is a number then, whatever does not need lp.)
     const bool none = !(lp == lp);
-    const float spread = dsum / sum * (float)a.inv_t, H = none ? NAN : (float)logs + spread;
+    constexpr float kLn2 = 0.693147182f;
+    const float spread = dsum / sum * kLn2, H = none ? NAN : (float)logs + spread;
     if (a.logp) a.logp[row] = (float)lp;
     if (a.entropy) a.entropy[row] = H;
     RowGrad g = {0.f, 0.f, 0.f, 0.f};
@@ -79,7 +80,7 @@ __device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top
     g.inv_sum = 1.f / sum;
     g.at_label = w * c;
     g.c0 = w * (a.ent * spread - c);
-    g.c1 = w * a.ent * (float)a.inv_t;
+    g.c1 = w * a.ent * kLn2;
     return g;
 }
 // A row without a token, or without a logit that is not -infinity: it has no part in the loss, whatever its weight is.  The sum over the rows knows it by the
@@ -125,11 +126,12 @@ struct RowGroup {
     }
 };
 
-// exp(-d / T) of a difference d >= 0 to the largest logit, k = log2(e) / T: a product and the hardware's power of two, off by 2 d U + 2 U of
-// itself.  What that makes of a row's probabilities goes by the spread of d under them, a few units.
-__device__ inline float exp_below(float d, float k) { return __builtin_amdgcn_exp2f(-d * k); }
-// (A product of e = 0 with the difference to a logit of -infinity is 0; where e is NaN so is the product.)
-__device__ inline float finite(float d) { return fminf(d, 1e30f); }
+// exp(-d / T) of a difference d >= 0 to the largest logit is 2^-t, t = d log2(e) / T: a product and the hardware's power of two, off by 2 t U + 2 U of
+// itself.  What that makes of a row's probabilities goes by the spread of t under them, a few units.  (All that is made of d is made of t, which is
+// a number of some size at any temperature.)
+__device__ inline float power_below(float t) { return __builtin_amdgcn_exp2f(-t); }
+// (A product of 2^-t = 0 with the t of a logit of -infinity is 0; where 2^-t is NaN so is the product.)
+__device__ inline float finite(float t) { return fminf(t, 1024.f); }
 
 // The row in registers stays as it was loaded: the compiler may keep nothing that it made of it on the way (floats, exponentials).
 template <int NV>
@@ -213,9 +215,9 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_held_kernel(Pol
         unpack_run16<T>(raw[i], v);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float d = top - v[e], x = exp_below(d, a.k);
+            const float t = (top - v[e]) * a.k, x = power_below(t);
             sum += x;
-            dsum = fmaf(x, finite(d), dsum);
+            dsum = fmaf(x, finite(t), dsum);
         }
     }
     group.template reduce<false>(sum, dsum);
@@ -242,8 +244,8 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_held_kernel(Pol
         unpack_run16<T>(raw[i], v);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float d = top - v[e];
-            v[e] = exp_below(d, a.k) * fmaf(-c1, finite(d), c0);
+            const float t = (top - v[e]) * a.k;
+            v[e] = power_below(t) * fmaf(-c1, finite(t), c0);
         }
         if (label >= j && label < j + E) {
 #pragma unroll
@@ -288,8 +290,8 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel
 #pragma unroll
                 for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
                 if (m > top) {  // (from nothing: both sums are 0)
-                    const float d = finite(m - top), x = exp_below(d, a.k);
-                    dsum = fmaf(sum, d, dsum) * x;
+                    const float t = finite((m - top) * a.k), x = power_below(t);
+                    dsum = fmaf(sum, t, dsum) * x;
                     sum *= x;
                     top = m;
                 }
@@ -300,9 +302,9 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel
                 }
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float d = top - v[e], x = exp_below(d, a.k);
+                    const float t = (top - v[e]) * a.k, x = power_below(t);
                     sum += x;
-                    dsum = fmaf(x, finite(d), dsum);
+                    dsum = fmaf(x, finite(t), dsum);
                 }
             }
         }
@@ -315,8 +317,8 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel
                 store_run16<T>(dz + j, a.V - j < E ? (int)(a.V - j) : E, u32x4_t{0, 0, 0, 0});
         return;
     }
-    const float d = finite(high - top), x = exp_below(d, a.k);
-    dsum = fmaf(sum, d, dsum) * x;
+    const float t = finite((high - top) * a.k), x = power_below(t);
+    dsum = fmaf(sum, t, dsum) * x;
     sum *= x;
     if (some == 1.f) sum = NAN;  // (a thread that saw nothing but -infinity beside it kept no sum of it)
     group.template reduce<false>(sum, dsum);
@@ -336,8 +338,8 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_streamed_kernel
             unpack_run16<T>(raw[i], v);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float below = high - v[e];
-                v[e] = exp_below(below, a.k) * fmaf(-c1, finite(below), c0);
+                const float t = (high - v[e]) * a.k;
+                v[e] = power_below(t) * fmaf(-c1, finite(t), c0);
             }
             if (label >= j && label < j + E) {
 #pragma unroll

@@ -80,3 +80,18 @@ def test_weights_of_rows_without_a_part(V):
     # a weight of a row that does count: infinite or NaN as it is
     w[0] = np.nan
     assert np.isnan(loss_of(p, "fp32", z, labels, p["old"], p["ref"], w, 0.1, 0.01)[2][0])
+
+
+@pytest.mark.parametrize("V", [40, 1003, 40000])
+@pytest.mark.parametrize("T", [1e-6, 1e-3, 1e6, 1e30])
+def test_temperatures_far_from_one(T, V):
+    """Logits of the temperature's size, some of them -infinity, an entropy bonus: every result is as finite as its definition.  An exponential is off by 3 U
+    of itself and of its argument, a sum of V terms by V U at most."""
+    p = problem(5, V, "fp32", banned=0.3)
+    z = rounded(p["z"] * T, torch.float32)
+    T = float(np.float32(T))
+    got = loss_of(p, "fp32", z, p["labels"], p["old"], p["ref"], p["weight"], 0.1, 0.01, T)
+    _, rlp, rH, rt, rdz = P.policy(z, p["labels"], p["old"], p["ref"], p["adv"], p["weight"], *(float(np.float32(v)) for v in (LOW, HIGH, 0.1, 0.01)), T)
+    off = (V + 200) * U
+    assert (np.abs(got[0] - rlp) <= off).all() and (np.abs(got[1] - rH) <= 20 * off).all()
+    assert (np.abs(got[5] - rdz) <= 40 * off * np.abs(rdz).max(1, keepdims=True)).all() and not got[5][np.isneginf(z)].any()
