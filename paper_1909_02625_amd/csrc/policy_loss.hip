@@ -42,20 +42,22 @@ __device__ inline float series2(float x)
 // row is held).
 __device__ inline RowGrad row_result(const PolicyArgs& a, int64_t row, float top, float at_label, float sum, float dsum)
 {
-    // log(sum) = log(2) exponent + log(m), m in [sqrt(1/2), sqrt(2)): 2 artanh((m - 1) / (m + 1)), the next term is 3e-9
+    // log(sum) = log(2) exponent + log(m), m in [sqrt(1/2), sqrt(2)): 2 artanh((m - 1) / (m + 1)), the next term is 5e-13; the quotient from the hardware's
+    // reciprocal and one step of Newton's, to 2^-45
     int ex = __builtin_amdgcn_frexp_expf(sum);
     float m = __builtin_amdgcn_frexp_mantf(sum);
     if (m < 0.707106781f) {
         m *= 2.f;
         --ex;
     }
-    const float q = (m - 1.f) / (m + 1.f), q2 = q * q, log_m = 2.f * q * (1.f + q2 * (1.f / 3 + q2 * (1.f / 5 + q2 * (1.f / 7 + q2 * (1.f / 9)))));
-    const double logs = ex * 0.69314718055994531 + (double)log_m;
+    const double n = m - 1.f, d = 1.0 + m, r = __builtin_amdgcn_rcpf(m + 1.f), q0 = n * r, q = fma(fma(-q0, d, n), r, q0), q2 = q * q;
+    const double log_m = 2 * q * (1 + q2 * (1.0 / 3 + q2 * (1.0 / 5 + q2 * (1.0 / 7 + q2 * (1.0 / 9 + q2 * (1.0 / 11 + q2 * (1.0 / 13)))))));
+    const double logs = ex * 0.69314718055994531 + log_m;
     const double lp = ((double)at_label - (double)top) * a.inv_t - logs;
     // (no lp: the label names no token, or the row holds NaN or infinity.  Nothing that is made of the row is a number then, whatever does not need lp.)
     const bool none = !(lp == lp);
     constexpr float kLn2 = 0.693147182f;
-    const float spread = dsum / sum * kLn2, H = none ? NAN : (float)logs + spread;
+    const float spread = dsum / sum * kLn2, H = none ? NAN : (float)(logs + (double)spread);
     if (a.logp) a.logp[row] = (float)lp;
     if (a.entropy) a.entropy[row] = H;
     RowGrad g = {0.f, 0.f, 0.f, 0.f};

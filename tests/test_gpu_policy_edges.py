@@ -95,3 +95,19 @@ def test_temperatures_far_from_one(T, V):
     off = (V + 200) * U
     assert (np.abs(got[0] - rlp) <= off).all() and (np.abs(got[1] - rH) <= 20 * off).all()
     assert (np.abs(got[5] - rdz) <= 40 * off * np.abs(rdz).max(1, keepdims=True)).all() and not got[5][np.isneginf(z)].any()
+
+
+@pytest.mark.parametrize("V", [256, 4096, 40000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logarithms_of_sums_that_are_exact(dtype, V):
+    """Row n has n equal logits, the others are -infinity: the sum is n, the log probability and the entropy are its logarithm, taken in 64 bits (to 1e-10) and
+    rounded once: half a step of the floats at it."""
+    n = np.unique(np.concatenate([np.arange(1, 200), np.linspace(200, V, 400).astype(int)]))
+    n = n[n <= V]
+    z = np.where(np.arange(V)[None, :] < n[:, None], 1.5, -np.inf)
+    lp, H, _, lp2, _, _ = loss_of({"adv": np.ones(len(n))}, dtype, z, np.zeros(len(n)))
+    ref = np.log(n.astype(float))
+    half = np.spacing(ref.astype(np.float32)).astype(float) / 2 + 1e-10
+    assert np.array_equal(lp, lp2)
+    assert (np.abs(lp + ref) <= half).all(), float(np.max(np.abs(lp + ref) / half))
+    assert (np.abs(H - ref) <= half).all()
