@@ -245,6 +245,36 @@ __device__ inline unsigned xcd_order(unsigned b, unsigned nb)
     return xcd * q + (xcd < r ? xcd : r) + b / 8;
 }
 
+// 32 rows of COLS results of a wave in LDS, one by one: a lane has one column, the lanes side by side.
+template <typename T, int COLS, int ROW>
+__device__ inline void finish_rows(const OutArgs& o, const float* tile, int64_t m0, int n0, int lane)
+{
+    constexpr int RPP = 64 / COLS, AHEAD = 8;
+    static_assert(COLS == 32 || COLS == 64, "rows of half a wave or of one");
+    const int col = lane % COLS, n = n0 + col;
+    if (n >= o.N) return;
+    const float bias = o.bias ? o.bias[n] : 0.f;
+    const int64_t left = o.M - m0;
+#pragma unroll 1
+    for (int r0 = lane / COLS; r0 < 32; r0 += RPP * AHEAD) {
+        const int64_t at = (m0 + r0) * o.stride + n, step = RPP * o.stride;
+        T res[AHEAD];
+        if (o.residual) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) res[i] = ((const T*)o.residual)[r0 + i * RPP < left ? at + i * step : 0];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (r0 + i * RPP >= left) break;
+            float u = tile[(r0 + i * RPP) * ROW + col] + bias;
+            if (o.pre) ((T*)o.pre)[at + i * step] = from_float<T>(u);
+            u = act_of(o.act, u);
+            if (o.residual) u += to_float<T>(res[i]);
+            ((T*)o.out)[at + i * step] = from_float<T>(u);
+        }
+    }
+}
+
 // The accumulators hold the transposed tile: a lane has, for row lane % 32 of a block, runs of four consecutive columns.  Through LDS,
 // 32 rows of a wave at a time, they become runs of eight, whole lines of a row.  WHOLE: all runs are, on 16-byte addresses, and the
 // activation is ACT.  Then the residual of the next 32 rows is on its way meanwhile.  (Code that runs once a tile is fetched once a tile: with all four
@@ -291,8 +321,6 @@ __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const O
                 float* to = o.partial + ((int64_t)blockIdx.y * o.M + m) * partial_stride(o.N) + n;
                 *(F4*)to = u;
                 *(F4*)(to + 4) = w;
-            } else if constexpr (!WHOLE) {
-                finish_single<T>(o, m, n, v);
             } else {
                 const int64_t at = m * o.stride + n;
 #pragma unroll
@@ -306,7 +334,9 @@ __device__ inline void finish_tile(char* smem, const F16 (&acc)[TM][TN], const O
                 store8<T>((T*)o.out + at, v);
             }
         };
-        if constexpr (RES) {
+        if constexpr (!WHOLE && !PART) {
+            finish_rows<T, TN * 32, ROW>(o, mine, m0 + i * 32, n0, lane);
+        } else if constexpr (RES) {
 #pragma unroll
             for (int q = 0; q < PASSES; ++q) pass(q, res[i & 1][q]);
         } else {
