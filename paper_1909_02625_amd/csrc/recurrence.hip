@@ -349,12 +349,15 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
             }
             bool watch = MODE != kParts && (VW == 2 ? fminf(A[0], A[VW - 1]) : A[0]) < kFaint;
             if (DECAY == DSP_DECAY_EXP && (r.f[0] & r.f[1] & r.f[2] & r.f[3] & L::kSigns) != L::kSigns) {
-                // some decay may be above 1: a product that lost its digits on the way and rose again is none
+                // Some decay may be above 1.  A product that lost its digits on the way and rose again is none; and with large factors B is a difference of
+                // what they lack of 1 and has itself no digits that A has not.
                 static_assert(TT == 4, "four rows");
                 watch |= MODE == kParts;
 #pragma unroll
-                for (int v = 0; v < VW; ++v)
+                for (int v = 0; v < VW; ++v) {
                     if (fminf(a[0][v] * a[1][v], a[0][v] * a[1][v] * a[2][v]) < kFaint) A[v] = NAN;
+                    if (fmaxf(fmaxf(a[0][v], a[1][v]), fmaxf(a[2][v], a[3][v])) > 1.25f) B[v] = 1.f;
+                }
             }
 #pragma unroll
             for (int v = 0; v < VW; ++v) {

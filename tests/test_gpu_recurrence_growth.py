@@ -67,6 +67,31 @@ def test_decays_above_one(dtype, path, lengths, C):
         call(problem(path, lengths, C, dtype, coupled), dtype, len(set(lengths)) > 1)
 
 
+def by_turns(size):
+    """One row up, one row down."""
+    return lambda n: -20.0 + size * (np.arange(n + 1) % 2)
+
+
+def wandering(n):
+    """Steps of any size, back from the ends."""
+    rng = np.random.default_rng(n)
+    level = [0.0]
+    for _ in range(n):
+        to = level[-1] + 6.0 * rng.standard_normal()
+        level.append(-120.0 - to if to < -60.0 else 160.0 - to if to > 80.0 else to)
+    return np.array(level)
+
+
+@pytest.mark.parametrize("lengths,C", [([12], 33), ([700], 72), ([9000], 8)])
+@pytest.mark.parametrize("path", [by_turns(1.0), by_turns(4.0), by_turns(9.0), by_turns(14.0), by_turns(17.0), wandering],
+                         ids=["1", "4", "9", "14", "17", "wandering"])
+def test_growth_and_decay_by_turns(path, lengths, C):
+    """Products of decays next to 1 whose factors are not: what they lack of 1 is no sum of what the factors lack."""
+    for dtype in TYPES:
+        for coupled in (False, True):
+            call(problem(path, lengths, C, dtype, coupled), dtype, False)
+
+
 def test_nothing_goes_in_and_nothing_comes_out():
     """Zeros stay zeros under decays whose product no float holds."""
     for n, f in ((12, 23.0), (40, 23.0), (700, 80.0), (9000, 0.3)):
