@@ -246,7 +246,8 @@ __device__ inline bool finite_state(float h) { return fabsf(h) < INFINITY; }
 template <int SLOTS, int W>
 struct Slots {
     float a[SLOTS][W], c[SLOTS][W], h[SLOTS][W], in[SLOTS + 1][W];
-    int watch;  // some product of the tile is below kFaint (kParts: some decay of it may be above 1)
+    int watch;  // some product of the tile is below kFaint
+    int grows;  // kParts: some decay of it may be above 1
     int lost;   // 1: its states are found row by row; 2: the slots are asked
     int asked;  // their answer
     int part;   // the part that is scanned next
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = wave * 2 + lane / 32;
     const int s = blockIdx.y, c = blockIdx.x * W + lane % 32 * VW;
     const bool in = c < p.C, both = c + VW <= p.C;
-    if (tid == 0) lds.watch = lds.asked = 0;
+    if (tid == 0) lds.watch = lds.grows = lds.asked = 0;
     lds_barrier();
     int whole;
     const int64_t first = rows_of(p, s, whole);
@@ -305,6 +306,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
     float* const sums = q.sums + (int64_t)s * (q.parts - 1) * 4 * p.C + cc;
     float carry = 0.f, pa = 1.f, pc = 0.f;
     int pe = 0;
+    bool none = false;   // kParts: H is not to be had from the slots
     bool guess = false;  // kParts: a product below kFaint is in pa, which is then a bound of what it should be
     if (MODE != kParts && mine) {
         const float* from = MODE == kScan && q.parts > 1 ? q.state : BACK ? p.dlast : p.state;
@@ -347,12 +349,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                     H[v] = BACK ? step_of(a[i][v], rest[i][v], H[v] + xv[v], 0.f) : step_of(a[i][v], rest[i][v], H[v], u[i][v]);
                 }
             }
-            bool watch = MODE != kParts && (VW == 2 ? fminf(A[0], A[VW - 1]) : A[0]) < kFaint;
+            const bool watch = (VW == 2 ? fminf(A[0], A[VW - 1]) : A[0]) < kFaint;
             if (DECAY == DSP_DECAY_EXP && (r.f[0] & r.f[1] & r.f[2] & r.f[3] & L::kSigns) != L::kSigns) {
                 // Some decay may be above 1.  A product that lost its digits on the way and rose again is none; and with large factors B is a difference of
                 // what they lack of 1 and has itself no digits that A has not.
                 static_assert(TT == 4, "four rows");
-                watch |= MODE == kParts;
+                if (MODE == kParts) lds.grows = 1;
 #pragma unroll
                 for (int v = 0; v < VW; ++v) {
                     if (fminf(a[0][v] * a[1][v], a[0][v] * a[1][v] * a[2][v]) < kFaint) A[v] = NAN;
@@ -366,10 +368,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                 lds.c[slot][w] = rest_of(A[v], B[v]);
                 lds.h[slot][w] = H[v];
             }
-            if ((MODE != kParts || DECAY == DSP_DECAY_EXP) && watch) lds.watch = 1;
+            if (watch) lds.watch = 1;
             lds_barrier();
             if (wave == 0 && lane < W) {
-                const int watched = lds.watch;
+                const int watched = lds.watch, grows = MODE == kParts && DECAY == DSP_DECAY_EXP ? lds.grows : 0;
                 if (MODE == kParts) {
                     // (pa + pc) (ja + jc), to twice the digits of either
                     auto times = [&](float ja, float jc) {
@@ -383,7 +385,16 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                         pc = __builtin_amdgcn_ldexpf(pc, -e);
                         pe += e;
                     };
-                    if (DECAY == DSP_DECAY_EXP && __builtin_amdgcn_readfirstlane(watched)) {
+                    if (__builtin_amdgcn_readfirstlane(watched)) {  // H begins at 0, but what comes in may be large
+                        float at = carry;
+#pragma unroll 2
+                        for (int j = 0; j < SLOTS; ++j) {
+                            const float ja = lds.a[j][lane], jh = lds.h[j][lane];
+                            none |= lost_digits(ja, jh, at);
+                            at = step_of(ja, lds.c[j][lane], at, jh);
+                        }
+                    }
+                    if (DECAY == DSP_DECAY_EXP && __builtin_amdgcn_readfirstlane(grows)) {
 #pragma unroll 1
                         for (int j = 0; j < SLOTS; ++j) {
                             float ja = lds.a[j][lane], jc = lds.c[j][lane];
@@ -422,7 +433,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                     const bool lost = __any(front == front && !finite_state(carry));
                     if (lane == 0) lds.lost = lost ? 1 : watched ? 2 : 0;
                 }
-                if (lane == 0) lds.watch = 0;
+                if (lane == 0) lds.watch = lds.grows = 0;
             }
             lds_barrier();
             if (MODE == kParts) continue;
@@ -545,7 +556,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
         to[0] = guess ? -pa : pa;
         to[p.C] = guess ? 0.f : pc;
         to[2 * p.C] = (float)pe;
-        to[3 * p.C] = carry;
+        to[3 * p.C] = none ? NAN : carry;
     } else if ((int)blockIdx.z == q.parts - 1 && p.left) {
         p.left[(int64_t)s * p.C + cc] = carry;
     }

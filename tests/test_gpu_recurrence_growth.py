@@ -141,3 +141,21 @@ def test_large_states_are_forgotten_by_their_rows():
                 rh, _, oh, _ = P.scan(decay, False, zero, f, state[0])
                 got = h.cpu().numpy().astype(np.float64)
                 assert (np.abs(got - rh) <= 1.01 * U * oh + 2.0 ** -126).all(), (decay, n, f0)
+
+
+@pytest.mark.parametrize("decay", [P.SIGMOID, P.EXP], ids=["sigmoid", "exp"])
+@pytest.mark.parametrize("n", [40, 700, 9000])
+def test_what_is_left_of_a_large_input_goes_on(decay, n):
+    """e^80 comes in with one row, four rows together forget e^-140 of it and the others next to nothing; the same on the way back."""
+    C = 40
+    rng = np.random.default_rng(n)
+    keep = -1e-3 if decay == P.EXP else 7.0
+    for at in range(8, 16, 2):
+        f, x, dh = np.full((n, C), keep), np.zeros((n, C)), np.zeros((n, C))
+        for first in (at, n - 1 - at - 3):
+            f[first:first + 4] = -35.0
+        x[at - 4] = rng.standard_normal(C) * np.exp(80.0)
+        dh[n - 1 - at + 4] = rng.standard_normal(C) * np.exp(80.0)
+        p = {"lengths": [n], "rows": n, "C": C, "decay": decay, "coupled": False, "x": rounded(x, torch.float32), "f": rounded(f, torch.float32),
+             "dh": rounded(dh, torch.float32), "state": np.zeros((1, C)), "dlast": np.zeros((1, C))}
+        call(p, "fp32", False)
