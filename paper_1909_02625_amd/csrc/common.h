@@ -534,16 +534,14 @@ __device__ inline float exp_of_minus(float a)
 }
 
 // exp(x) over all of the floats: up to the largest (then infinity) and down to those below 2^-126 (then 0), which the hardware's power of two does
-// not have.  That is taken 2^32 nearer to 1 and the result brought back.  at - s is the exponent that was taken, exactly, whichever of
-// the two sums was rounded; what it lacks of x is a factor, as above: relative error 4 * 2^-24, below 2^-126 half a step more.
+// not have: as the square of exp(x / 2).  What the rounded exponent lacks is a factor, as above: relative error 8 * 2^-24, below 2^-126 half a step more.
+// (Where x is infinite, or so large that its exponent is, the factor is no number or any; bounded, it changes nothing there.)
 __device__ inline float exp_any(float x)
 {
-#pragma clang fp contract(off)
-    constexpr float kLn2 = 0.693147182f, kRest = -1.90465421e-9f;
-    x = x > 100.f ? 100.f : x;
-    const float s = x < 0.f ? 32.f : -32.f, near = x * 1.44269504f, at = near + s, hi = at - s, p = __builtin_amdgcn_exp2f(at);
-    const float off = fminf(fmaf(hi, -kRest, fmaf(hi, -kLn2, x)), 1.f);
-    return fmaf(p, off, p) * (x < 0.f ? 0x1p-32f : 0x1p32f);
+    constexpr float kLn2 = 1.386294365f, kRest = -3.80930860e-9f;  // 2 ln(2) = kLn2 + kRest
+    const float half = x * 0.72134752f, p = __builtin_amdgcn_exp2f(half);
+    const float lacks = __builtin_amdgcn_fmed3f(fmaf(half, -kRest, 1.f + fmaf(half, -kLn2, x)), 0.5f, 2.f);
+    return p * (p * lacks);
 }
 
 // n / d for n < 2^31 with precomputed mul = floor(2^32 * (2^sh - d) / d) + 1, sh = ceil(log2 d).

@@ -27,7 +27,7 @@ struct ScanArgs {
 };
 
 // a and 1 - a, each to its own last digits: a sequence of thousands of steps whose decay is close to 1 depends on what it lacks.  (The sigmoid's are 0
-// below 2^-126.  With the exponential that goes on below, as exp(f) does: 8 x 4096 x 2048 forward 128 us instead of 121, one sequence of 32768 214, 196.)
+// below 2^-126.  With an exponential that goes on below, as exp(f) does: 8 x 4096 x 2048 forward 128 us instead of 121, one sequence of 32768 214, 196.)
 __device__ inline void gate_of(int decay, float f, float& a, float& b)
 {
     if (decay == DSP_DECAY_SIGMOID) {
@@ -37,8 +37,8 @@ __device__ inline void gate_of(int decay, float f, float& a, float& b)
         return;
     }
     a = exp_any(f);
-    // exp(f) - 1 by its series up to f^7 where the difference would cancel (the next term is 2e-8 of it there)
-    const float s = f * (1.f + f * (1.f / 2 + f * (1.f / 6 + f * (1.f / 24 + f * (1.f / 120 + f * (1.f / 720 + f * (1.f / 5040)))))));
+    // exp(f) - 1 by its series up to f^7 where the difference would cancel (the next term is 2e-8 of it there; 1 / 720 is 7 / 5040)
+    const float s = f * (1.f + f * (1.f / 2 + f * (1.f / 6 + f * (1.f / 24 + f * (1.f / 120 + f * (1.f / 5040) * (7.f + f))))));
     b = fabsf(f) < 0.35f ? -s : 1.f - a;
 }
 // The rows of a sequence: whatever the offsets hold, rows that there are and no more than `steps` of them.
@@ -227,7 +227,8 @@ __global__ __launch_bounds__(kWalkThreads) void recurrence_walk_back_kernel(Scan
 // (us with eight rows a lane and with four, which leave room for twice the waves: 64 x 1024 x 1024 forward 110, 98; 16 x 4096 x 2048 backward 485, 395.)
 constexpr int kLaneRows = 4;
 
-enum ScanMode { kScan, kParts, kStates };
+// A sequence as it is; the scan of a part; what each part does; the states between them.
+enum ScanMode { kWhole, kScan, kParts, kStates };
 
 struct PartArgs {
     float* sums;      // [sequences][parts - 1][4][C]: what each part but the last does, h -> (m + c) 2^e h + H: m, c, e, and H, in whose place the state behind it comes
@@ -246,15 +247,17 @@ __device__ inline bool finite_state(float h) { return fabsf(h) < INFINITY; }
 template <int SLOTS, int W>
 struct Slots {
     float a[SLOTS][W], c[SLOTS][W], h[SLOTS][W], in[SLOTS + 1][W];
-    int watch;  // some product of the tile is below kFaint
+    int watch;  // the number of the latest tile some product of which was below kFaint (before the first: any; to ask costs time alone)
     int grows;  // kParts: some decay of it may be above 1
     int lost;   // 1: its states are found row by row; 2: the slots are asked
     int asked;  // their answer
     int part;   // the part that is scanned next
 };
 
+// (Many whole sequences by eight waves each: four workgroups a compute unit forward, three backward without x, two with it.  64 x 1024 x 1024 bf16 forward, exp
+// decays, us with four 103, with three 116; 512 x 64 x 1024 backward without x with three 89, with two 98.)
 template <typename T, int WAVES, bool BACK, int DECAY, bool COUPLED, int MODE>
-__global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
+__global__ __launch_bounds__(64 * WAVES, MODE != kWhole || WAVES == 16 ? 4 : !BACK ? 8 : COUPLED ? 4 : 6) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
 {
     typedef Lane4<T> L;
     constexpr int VW = L::VW, W = 32 * VW, TT = kLaneRows, SLOTS = 2 * WAVES, TILE = SLOTS * TT;
@@ -263,8 +266,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = wave * 2 + lane / 32;
     const int s = blockIdx.y, c = blockIdx.x * W + lane % 32 * VW;
     const bool in = c < p.C, both = c + VW <= p.C;
-    if (tid == 0) lds.watch = lds.grows = lds.asked = 0;
-    lds_barrier();
+    if (MODE == kParts) {
+        if (tid == 0) lds.watch = lds.grows = 0;
+        lds_barrier();
+    }
     int whole;
     const int64_t first = rows_of(p, s, whole);
     // the rows of a part, in the order of the scan: k = 0 .. n - 1 is row begin + k, or backward row whole - 1 - (begin + k)
@@ -273,7 +278,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
         begin = part * q.part_rows;
         n = whole - begin < q.part_rows ? whole - begin : q.part_rows;
     };
-    choose(MODE == kStates ? 0 : blockIdx.z);
+    choose(MODE == kScan || MODE == kParts ? blockIdx.z : 0);
     const T* const x = (const T*)p.x + first * p.xs + c;
     const T* const f = (const T*)p.f + first * p.fs + c;
     const T* const h = (const T*)p.h + first * p.hs + c;
@@ -293,7 +298,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
             const int64_t row = row_of(k);
             r.f[i] = L::load(f + row * p.fs, both);
             r.u[i] = BACK ? L::load(d + row * p.hs, both) : L::load(x + row * p.xs, both);
-            if (BACK && MODE == kScan) {
+            if (BACK && (MODE == kWhole || MODE == kScan)) {
                 if (COUPLED) r.x[i] = L::load(x + row * p.xs, both);
                 if (row > 0) r.h[i] = L::load(h + (row - 1) * p.hs, both);
             }
@@ -309,7 +314,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
     bool none = false;   // kParts: H is not to be had from the slots
     bool guess = false;  // kParts: a product below kFaint is in pa, which is then a bound of what it should be
     if (MODE != kParts && mine) {
-        const float* from = MODE == kScan && q.parts > 1 ? q.state : BACK ? p.dlast : p.state;
+        const float* from = MODE == kScan ? q.state : BACK ? p.dlast : p.state;
         if (from) carry = from[(int64_t)s * p.C + cc];
         if (MODE == kStates) q.state[(int64_t)s * p.C + cc] = carry;
     }
@@ -318,7 +323,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
         q.state[(int64_t)s * p.C + cc] = from ? from[(int64_t)s * p.C + cc] : 0.f;
     }
     float before[VW] = {};  // the state in front of the first row, which h_(t-1) is there
-    if (BACK && MODE == kScan && p.state) {
+    if (BACK && (MODE == kWhole || MODE == kScan) && p.state) {
 #pragma unroll
         for (int v = 0; v < VW; ++v)
             if (c + v < p.C) before[v] = p.state[(int64_t)s * p.C + c + v];
@@ -330,6 +335,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
         for (int t0 = 0; t0 < n; t0 += TILE) {
             const Raw r = next;
             if (t0 + TILE < n) load(t0 + TILE, next);
+            const bool grows = DECAY == DSP_DECAY_EXP && (r.f[0] & r.f[1] & r.f[2] & r.f[3] & L::kSigns) != L::kSigns;
             float a[TT][VW], rest[TT][VW], u[TT][VW], A[VW], B[VW], H[VW];
 #pragma unroll
             for (int v = 0; v < VW; ++v) A[v] = 1.f, B[v] = H[v] = 0.f;
@@ -350,17 +356,6 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                 }
             }
             const bool watch = (VW == 2 ? fminf(A[0], A[VW - 1]) : A[0]) < kFaint;
-            if (DECAY == DSP_DECAY_EXP && (r.f[0] & r.f[1] & r.f[2] & r.f[3] & L::kSigns) != L::kSigns) {
-                // Some decay may be above 1.  A product that lost its digits on the way and rose again is none; and with large factors B is a difference of
-                // what they lack of 1 and has itself no digits that A has not.
-                static_assert(TT == 4, "four rows");
-                if (MODE == kParts) lds.grows = 1;
-#pragma unroll
-                for (int v = 0; v < VW; ++v) {
-                    if (fminf(a[0][v] * a[1][v], a[0][v] * a[1][v] * a[2][v]) < kFaint) A[v] = NAN;
-                    if (fmaxf(fmaxf(a[0][v], a[1][v]), fmaxf(a[2][v], a[3][v])) > 1.25f) B[v] = 1.f;
-                }
-            }
 #pragma unroll
             for (int v = 0; v < VW; ++v) {
                 const int w = lane % 32 * VW + v;
@@ -368,10 +363,22 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                 lds.c[slot][w] = rest_of(A[v], B[v]);
                 lds.h[slot][w] = H[v];
             }
-            if (watch) lds.watch = 1;
+            if (grows) {
+                // Some decay may be above 1.  A product that lost its digits on the way and rose again is none; and with large factors B is a difference of
+                // what they lack of 1 and has itself no digits that A has not.
+                static_assert(TT == 4, "four rows");
+                if (MODE == kParts) lds.grows = 1;
+#pragma unroll
+                for (int v = 0; v < VW; ++v) {
+                    const int w = lane % 32 * VW + v;
+                    if (fminf(a[0][v] * a[1][v], a[0][v] * a[1][v] * a[2][v]) < kFaint) lds.a[slot][w] = NAN;
+                    if (fmaxf(fmaxf(a[0][v], a[1][v]), fmaxf(a[2][v], a[3][v])) > 1.25f) lds.c[slot][w] = 0.f;
+                }
+            }
+            if (watch) lds.watch = t0 + 1;
             lds_barrier();
             if (wave == 0 && lane < W) {
-                const int watched = lds.watch, grows = MODE == kParts && DECAY == DSP_DECAY_EXP ? lds.grows : 0;
+                const int watched = lds.watch == t0 + 1, grows = MODE == kParts && DECAY == DSP_DECAY_EXP ? lds.grows : 0;
                 if (MODE == kParts) {
                     // (pa + pc) (ja + jc), to twice the digits of either
                     auto times = [&](float ja, float jc) {
@@ -431,9 +438,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                     }
                     // (no step makes a state finite again; NaN it stays)
                     const bool lost = __any(front == front && !finite_state(carry));
-                    if (lane == 0) lds.lost = lost ? 1 : watched ? 2 : 0;
+                    if (lane == 0) {
+                        lds.lost = lost ? 1 : watched ? 2 : 0;
+                        lds.asked = 0;
+                    }
                 }
-                if (lane == 0) lds.watch = lds.grows = 0;
+                if (MODE == kParts && lane == 0) lds.watch = lds.grows = 0;
             }
             lds_barrier();
             if (MODE == kParts) continue;
@@ -448,7 +458,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
             if (lost == 2) {
                 bool here = false;
 #pragma unroll
-                for (int v = 0; v < VW; ++v) here |= lost_digits(A[v], H[v], st[v]);
+                for (int v = 0; v < VW; ++v) {
+                    const int w = lane % 32 * VW + v;
+                    here |= lost_digits(lds.a[slot][w], lds.h[slot][w], lds.in[slot][w]);
+                }
                 if (here) lds.asked = 1;
                 lds_barrier();
                 lost = __builtin_amdgcn_readfirstlane(lds.asked);
@@ -468,7 +481,6 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
                     lds_barrier();
                 }
                 if (wave == 0 && lane < W) carry = lds.in[SLOTS][lane];
-                if (tid == 0) lds.asked = 0;
             }
             if (MODE == kStates || !keep) continue;
 #pragma unroll
@@ -503,7 +515,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
         }
     };
 
-    if (MODE == kParts || q.parts == 1) {
+    if (MODE == kWhole || MODE == kParts) {
         scan(true);
     } else {
         // from part to part by what each does, and through the rows of one whose product, or the state behind it, is not to be had that way
@@ -557,7 +569,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_scan_kernel(ScanArgs
         to[p.C] = guess ? 0.f : pc;
         to[2 * p.C] = (float)pe;
         to[3 * p.C] = none ? NAN : carry;
-    } else if ((int)blockIdx.z == q.parts - 1 && p.left) {
+    } else if ((MODE == kWhole || (int)blockIdx.z == q.parts - 1) && p.left) {
         p.left[(int64_t)s * p.C + cc] = carry;
     }
 }
@@ -634,7 +646,8 @@ int scan_by(const ScanArgs& a, const PartArgs& q, hipStream_t st, const char* na
         }
     }
     ProfScope ps(name, bytes, 1);
-    DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, kScan>), grid, block, 0, st, a, q);
+    if (q.parts > 1) DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, kScan>), grid, block, 0, st, a, q);
+    else DSP_LAUNCH(ps, (recurrence_scan_kernel<T, WAVES, BACK, DECAY, COUPLED, kWhole>), grid, block, 0, st, a, q);
     DSP_HIP(hipGetLastError());
     return DSP_OK;
 }
