@@ -534,14 +534,15 @@ __device__ inline float exp_of_minus(float a)
 }
 
 // exp(x) over all of the floats: up to the largest (then infinity) and down to those below 2^-126 (then 0), which the hardware's power of two does
-// not have: as the square of exp(x / 2).  What the rounded exponent lacks is a factor, as above: relative error 8 * 2^-24, below 2^-126 half a step more.
-// (Where x is infinite, or so large that its exponent is, the factor is no number or any; bounded, it changes nothing there.)
+// not have: beyond 64 as the square of exp(x / 2).  What the rounded exponent lacks is a factor, as above: relative error 4 * 2^-24, beyond 64 8 * 2^-24, and
+// below 2^-126 half a step more.  (Where x is infinite, or so large that its exponent is, the factor is no number or any; bounded, it changes nothing there.)
 __device__ inline float exp_any(float x)
 {
-    constexpr float kLn2 = 1.386294365f, kRest = -3.80930860e-9f;  // 2 ln(2) = kLn2 + kRest
-    const float half = x * 0.72134752f, p = __builtin_amdgcn_exp2f(half);
-    const float lacks = __builtin_amdgcn_fmed3f(fmaf(half, -kRest, 1.f + fmaf(half, -kLn2, x)), 0.5f, 2.f);
-    return p * (p * lacks);
+    constexpr float kLn2 = 0.693147182f, kRest = -1.90465421e-9f;
+    const bool far = fabsf(x) > 64.f;
+    const float all = x * 1.44269504f, p = __builtin_amdgcn_exp2f(far ? 0.5f * all : all);
+    const float lacks = __builtin_amdgcn_fmed3f(fmaf(all, -kRest, 1.f + fmaf(all, -kLn2, x)), 0.5f, 2.f);
+    return p * lacks * (far ? p : 1.f);
 }
 
 // n / d for n < 2^31 with precomputed mul = floor(2^32 * (2^sh - d) / d) + 1, sh = ceil(log2 d).
