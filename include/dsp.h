@@ -608,7 +608,8 @@ int dsp_norm_residual_backward(const dsp_norm_residual_desc* desc, const void* d
  * identity, relu, gelu (p times the normal distribution function of p) or silu (p / (1 + exp(-p))).  Sums, bias, activation and residual are taken
  * in float and rounded once.  (dsp_linear_forward is the float product of a classifier's head, without any of this.)
  * Strides are the elements from one row to the next (x_stride: x and dx, 0: cin; y_stride: y, residual, pre and dy, 0: cout).  Buffers are
- * aligned to their elements and no more; rows of whole 16-byte runs on 16-byte addresses are read and written fastest.
+ * aligned to their elements and no more; rows of whole 16-byte runs on 16-byte addresses are read and written fastest.  A product of more than
+ * 2^23 tiles of 64 x 64 results is refused.
  */
 typedef enum dsp_act_kind { DSP_ACT_IDENTITY = 0, DSP_ACT_RELU = 1, DSP_ACT_GELU = 2, DSP_ACT_SILU = 3 } dsp_act_kind;
 typedef struct dsp_dense_desc {
@@ -646,6 +647,9 @@ int dsp_dense_backward(const dsp_dense_desc* desc, const void* d_dy, const void*
  * went in), NULL: not kept; they may be the same buffer.  One step of serving is steps = 1 with both.
  * Strides are the elements from one row to the next (0: C); a gradient has the stride of its tensor (dx: x, df: f, dh: h).  Buffers are
  * aligned to their elements and no more.  d_h may not be d_x or d_f.
+ * Decays may be above 1 (exp(f), f > 0): h is what the formula makes of it row by row, whatever the product of many decays does, and so is an infinite
+ * h.  Where the product of the decays of a tile or a part leaves the floats it is gone through again by its rows, which takes several
+ * times as long.  (1 / (1 + exp(-f)) and what it lacks of 1 are 0 below 2^-126.)  Up to 65535 sequences.
  */
 typedef enum dsp_decay_kind { DSP_DECAY_SIGMOID = 0, DSP_DECAY_EXP = 1 } dsp_decay_kind;
 typedef struct dsp_recurrence_desc {
@@ -679,8 +683,8 @@ int dsp_recurrence_backward(const dsp_recurrence_desc* desc, const void* d_dh, c
  * dsp_token_logprob gives lp and H (the old and the reference model's, say; the clip range and the coefficients are not looked at).
  * dsp_policy_loss gives L and its gradient, reading every logit once (twice in rows of more than 64 KiB).  A row with a negative
  * label (a prompt, padding) has no part in L: its lp, terms and gradient are 0, and so are those of a row whose logits are all
- * -infinity.  A logit of -infinity has probability 0.  A label of vocab or more indexes nothing: its row's results are NaN, as
- * are those of a row that holds NaN or +infinity.
+ * -infinity, whatever their weights are.  A logit of -infinity has probability 0.  A label of vocab or more indexes nothing: its row's
+ * results, and L with them, are NaN, as are those of a row that holds NaN or +infinity.
  */
 typedef struct dsp_policy_loss_desc {
     int32_t rows, vocab;

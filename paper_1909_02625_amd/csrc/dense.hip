@@ -7,8 +7,8 @@
 //
 // The matrix unit bounds large ones: bf16 on 256 x 256 tiles 1334 TFLOP/s inside a tile (8192 x 4096 rows with k from 4096 to 8192), 1260 with k = 8192,
 // 1190 with 4096 (the libraries' product of 8192^3 1369); a tile's beginning and end have its compute unit to themselves.  8192 x 2048 -> 5632 with bias,
-// gelu and both outputs takes 195 us (970 TFLOP/s, three rounds of 256 tiles of which the last is three quarters full), its backward pass 370.
-// fp32: 127 TFLOP/s at 4096^3 of 153.  One row reads its filters in 8.3 us (2.8 TB/s, the launch included).
+// gelu and both outputs takes 196 to 208 us by card (964 TFLOP/s, three rounds of 256 tiles of which the last is three quarters full), its backward pass 372.
+// fp32: 127 TFLOP/s at 4096^3 of 153.  One row reads its filters in 8.4 us (2.8 TB/s, the launch included).
 #include "common.h"
 
 #include <algorithm>
@@ -26,7 +26,7 @@ typedef short S4 __attribute__((ext_vector_type(4)));
 
 // ---- activations ---------------------------------------------------------------------------------
 // Phi(x) = erfc(-x / sqrt 2) / 2 for x <= 0 as t P(t) exp(-x^2 / 2), t = 1 / (1 + 0.4 |x| / sqrt 2): P is a polynomial fitted to
-// erfc(z) exp(z^2) / (2 t) with the least largest relative error over z >= 0, 1.3e-7; in floats, with the exponential, 12 * 2^-24.
+// erfc(z) exp(z^2) / (2 t) with the least largest relative error over z >= 0, 1.3e-7; in floats, with the exponential, 20 * 2^-24.
 // exp(-x^2 / 2) is given: the derivative of gelu wants it too.
 __device__ inline float normal_below(float ax, float e)
 {
@@ -127,7 +127,8 @@ __device__ inline void store8(T* p, const float (&v)[8])
         float t[VW];
 #pragma unroll
         for (int i = 0; i < VW; ++i) t[i] = v[h * VW + i];
-        // (marked as streamed: 8192 x 2048 -> 5632 with two outputs 213 -> 195 us, 4096 x 2048 -> 32000 497 -> 470)
+        // (marked as streamed, us with and without: 8192 x 2048 -> 5632 with two outputs 196, 215; 4096 x 2048 -> 32000 467, 482; the backward pass 372, 375.  Where the
+        // next product reads the result, 2048 -> 5632 -> 2048: 8192 rows 358, 360; but 4096 222, 218; 1024 107, 102)
         __builtin_nontemporal_store(pack_run16<T>(t), (u32x4_t*)p + h);
     }
 }
@@ -671,7 +672,8 @@ struct GradArgs {
 constexpr int kGradThreads = 256, kGradAhead = 4;
 
 // A workgroup has LPR lanes of eight columns side by side, the rest of it rows, and a part of the rows.  g is rounded to the storage type because
-// the matrix instructions read that; the column sums are of the values before.  Behind the last column g's rows are filled up with zeros.
+// the matrix instructions read that (bf16 dx and dW are off by 2.3e-3 of themselves, with an unrounded g 1.7e-3); the column sums are of the values before.
+// Behind the last column g's rows are filled up with zeros.
 template <typename T, int LPR>
 __global__ __launch_bounds__(kGradThreads) void dense_grad_kernel(GradArgs a)
 {
@@ -898,12 +900,13 @@ size_t rounded16(size_t n) { return (n + 15) / 16 * 16; }
 enum Kernel { kFew, kDirect256, kDirect192, kDirect128, kStaged128, kStaged64 };
 
 // Who forms a contraction, and into how many parts its k is cut (us).
-//   few rows: bf16 32 rows of 2048 -> 5632 13.5, by tiles 14.3; 64 rows 21.0, 15.3, of 5632 -> 2048 26.9, 16.3; fp32 48 rows of 1000 -> 1000 11.4, 38.1.
-//   direct 256 x 256 from 128 workgroups on: 2048 x 2048 -> 4096 39.9, on 128 x 128 44.8; 2048 x 1024 -> 4096 22.7, 25.2.  8192 x 5632 x 2048 on 128 x 128: 312, 176.
-//   192 rows where the rounds are done first: the filters' gradient 5632 x 2048 over 8192 rows 195, 171 (176 tiles of 256 rows, 240 of 192).
+//   few rows: bf16 32 rows of 2048 -> 5632 13.5, by tiles 14.3; 64 rows 21.0, 15.3, of 5632 -> 2048 26.4, 15.5; fp32 48 rows of 1000 -> 1000 11.0, 34.6.
+//   large tiles from 128 workgroups of 256 x 256 on: 2048 x 2048 -> 4096 41.1, on 128 x 128 45.6; 2048 x 1024 -> 4096 23.9, 25.8; 8192 x 5632 -> 2048 178, 296.
+//   192 rows where the rounds are done first: the filters' gradient 5632 x 2048 over 8192 rows 171, of 256 195 (240 and 176 tiles); 4096 x 2048 -> 5632 121, 129 (two
+//   rounds either way); 2048 x 2048 -> 4096 41.2, 41.1; but 3000 x 2048 -> 4096 53.0, 49.4 (one round either way, which 192-row tiles fill).
 //   parts of 2048 elements for large tiles: backward of 8192 x 1024 -> 4096 250, with two parts 218; of 4096 x 2048 -> 2048 135, 117.
-//   staged 128 x 128 from 512 tiles on: 2048 x 2000 -> 2001 bf16 (256 tiles) 58.4, on 64 x 64 47.5; 2048^3 fp32 163, 167.
-//   parts of the staged ones: the odd fp32 backward (1913 x 1431 -> 777) 171 with none, 136.
+//   staged 128 x 128 from 512 tiles on: 8000 x 2001 -> 2003 bf16 126, on 64 x 64 178; but 2048 x 2000 -> 2001 (256 tiles) 52.5, 40.5; 2048^3 fp32 162.4, 162.3.
+//   parts of the staged ones: the odd fp32 backward (1913 x 1431 -> 777) 173 with none, 137; 64 x 5632 -> 2048 bf16 85, 15.5.
 struct ContractPlan {
     Kernel kernel;
     int parts, part_k;

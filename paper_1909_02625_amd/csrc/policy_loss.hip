@@ -4,8 +4,8 @@
 //   L = sum over rows of w (max(-A rho, -A clip(rho)) + kl (exp(ref - lp) - (ref - lp) - 1) - entropy H)
 //   dL/dz_j = w / T (c (1[j = label] - p_j) + entropy p_j (log p_j + H)),  c = -A rho [not clipped] + kl (1 - exp(ref - lp))
 //
-// Memory bounds it: a row is read once and its gradient written once, 4096 x 32000 bf16 in 114 us with the sum over the rows (4.6 TB/s).  Longer
-// rows are read twice (1024 x 100000: 114 us, 3.6 TB/s of what is counted).  Rows of odd length, whose 16-byte runs lie across lines, cost a tenth more.
+// Memory bounds it: a row is read once and its gradient written once, 4096 x 32000 bf16 in 111 us with the sum over the rows (4.7 TB/s).  Longer
+// rows are read twice (1024 x 100000: 112 us, 3.7 TB/s of what is counted).  Rows of odd length, whose 16-byte runs lie across lines, cost a tenth more.
 #include "common.h"
 
 #include <algorithm>
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(RowGroup<WAVES>::BLOCK) void policy_held_kernel(Pol
     }
 }
 
-// Rows that no workgroup holds, and calls that want no gradient: the sums follow the largest logit so far.  For the gradient the row is read once more.
+// Rows that no workgroup holds: the sums follow the largest logit so far.  For the gradient the row is read once more.
 constexpr int kStreamAhead = 4;
 
 template <typename T, int WAVES>
@@ -442,7 +442,8 @@ int streamed(const PolicyArgs& a, hipStream_t st, ProfScope& ps)
 }
 
 // Rows of up to 4096 runs are held (32768 bf16 elements by eight waves); longer ones take so many registers that streaming them is faster (us, held and
-// streamed: 2048 x 40000 137, 126; 2048 x 60000 155, 145; 512 x 70000 75, 51; 1024 x 100000 141, 119; the log probabilities of 2048 x 60000 84, 74).
+// streamed: 2048 x 40000 125, 118; 2048 x 60000 140, 137; 512 x 70000 55, 44; 1024 x 100000 119, 112; the log probabilities of 2048 x 60000 82, 69; but
+// 4096 x 32000 124, 170).
 // What a call is asked for makes no difference, so that the log probabilities of both entry points are the same bits.
 template <typename T>
 int rows_t(const PolicyArgs& a, hipStream_t st, ProfScope& ps)

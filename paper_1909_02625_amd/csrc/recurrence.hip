@@ -5,8 +5,9 @@
 // and, from the last row back, g_t = dh_t + a_(t+1) g_(t+1), dx_t = g_t du/dx, df_t = g_t (h_(t-1) [- x_t]) da/df.
 //
 // Memory bounds it (3 and 6 rows of C for a step); what it reaches is 4.1 TB/s where workgroups fill the card (16 x 4096 x 2048 bf16 backward
-// 395 us, 2048 x 64 x 1024 forward 188) and less with one workgroup a compute unit (8 x 4096 x 2048: 123 us, 3.3 TB/s): a gate takes some
-// thirty vector instructions, and the two barriers of a tile wait for the first wave's walk over the slots.
+// 400 us, 2048 x 64 x 1024 forward 194) and less with one workgroup a compute unit (8 x 4096 x 2048: 127 us, 3.2 TB/s): a gate takes some
+// thirty vector instructions, and the two barriers of a tile wait for the first wave's walk over the slots.  To look after products of decays that leave
+// the floats is 2 to 5 % of it (8 x 4096 x 2048 121 us without).
 #include "common.h"
 
 #include <algorithm>
@@ -255,7 +256,7 @@ struct Slots {
 };
 
 // (Many whole sequences by eight waves each: four workgroups a compute unit forward, three backward without x, two with it.  64 x 1024 x 1024 bf16 forward, exp
-// decays, us with four 103, with three 116; 512 x 64 x 1024 backward without x with three 89, with two 98.)
+// decays, us with four 106, with three 118; 512 x 64 x 1024 backward without x with three 88, with two 97.)
 template <typename T, int WAVES, bool BACK, int DECAY, bool COUPLED, int MODE>
 __global__ __launch_bounds__(64 * WAVES, MODE != kWhole || WAVES == 16 ? 4 : !BACK ? 8 : COUPLED ? 4 : 6) void recurrence_scan_kernel(ScanArgs p, PartArgs q)
 {
@@ -600,11 +601,11 @@ ScanArgs args_of(const dsp_recurrence_desc* d)
     return a;
 }
 
-// Who does it, and how a sequence is cut (bf16, us).  Up to 16 steps a lane walks (64 sequences x 16 x 2048 6.9, scanned 10.1; 256 x 16 x 2048 backward
-// 27.5, 58; but 64 x 32 x 2048 11.6, 10.7; 16 x 32 x 2048 10.2, 5.3; 2048 x 64 x 1024 180, 188).  Parts where strips and sequences make fewer than 192
-// workgroups, 512 of them, of eight tiles at least (one sequence of 32768 x 2048 forward in 8 parts 239, in 16 200; backward 345, 293;
-// 256 workgroups cut in two 166, whole 132: the cut costs a second read).  Sixteen waves a workgroup where there are fewer than 384, which have
-// a compute unit each (8 x 4096 x 2048 forward 145 with eight, 123 with sixteen; backward 242, 219).
+// Who does it, and how a sequence is cut (bf16, us).  Up to 16 steps a lane walks (64 sequences x 16 x 2048 7.8, scanned 10.7; 256 x 16 x 2048 backward
+// 27.5, 60; but 64 x 32 x 2048 13.5, 11.5; 16 x 32 x 2048 12.3, 5.2; 2048 x 64 x 1024 181, 193).  Parts where strips and sequences make fewer than 192
+// workgroups, 512 of them, of eight tiles at least (one sequence of 32768 x 2048 forward in 8 parts 234, in 16 202; backward 321, 294;
+// 256 workgroups cut in two 173, whole 127: the cut costs a second read).  Sixteen waves a workgroup where there are fewer than 384, which have
+// a compute unit each (8 x 4096 x 2048 forward 155 with eight, 127 with sixteen; backward 255, 225).
 struct Plan {
     bool walk;
     int waves, parts, part_rows;
