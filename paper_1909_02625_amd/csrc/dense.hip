@@ -246,7 +246,8 @@ __device__ inline unsigned xcd_order(unsigned b, unsigned nb)
     return xcd * q + (xcd < r ? xcd : r) + b / 8;
 }
 
-// 32 rows of COLS results of a wave in LDS, one by one: a lane has one column, the lanes side by side.
+// 32 rows of COLS results of a wave in LDS, one by one: a lane has one column, the lanes side by side.  (With eight in a row a lane, as whole runs have them, 3199 x 102 ->
+// 1192 fp32 with residual and p took 52 us, so 20; 3602 x 320 -> 551 33, 25.)
 template <typename T, int COLS, int ROW>
 __device__ inline void finish_rows(const OutArgs& o, const float* tile, int64_t m0, int n0, int lane)
 {
